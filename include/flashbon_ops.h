@@ -108,6 +108,58 @@ flashbon_status flashbon_op_unpatch_sde(int32_t n, int32_t C, int32_t H, int32_t
                                         const float *v, float *z, float t_cur, float t_next, float a,
                                         uint64_t seed, int32_t step, int32_t row0, void *stream);
 
+/* ---- 8-bit layers: drafts are only ranked, and may take their linear layers in 8-bit integers.  A DiT branch runs as
+ *   flashbon_op_norm_residual (int8 rows of the modulated norm) -> flashbon_op_linear_i8 (GELU) ->
+ *   flashbon_op_quant_rows -> flashbon_op_linear_i8 -> flashbon_op_norm_residual (the next branch's rows),
+ * on weights that flashbon_op_quant_rows made once.  There is no training path, as in the rest of the library.
+ * Addresses need no more alignment than their elements (rows of odd length included); 16 bytes, K % 16 == 0 and
+ * N % 8 == 0 are fastest. */
+
+/* Rows to 8-bit integers with a scale each: scale[m] = max(max_k |x[m][k]| / 127, 2^-126), rounded once to fp32, and
+ * q[m][k] = x[m][k] / scale[m] to the nearest integer (ties to even), decided exactly.  -128 does not occur.  A row
+ * whose maximum is not finite gets scale NaN and codes 0, so that every output made of it is NaN.
+ * x: device, act of `dtype`, row m at x + m * x_row_stride (elements, >= K): activations [M][K], a slice of fused rows,
+ * or the weights [N][K] of a layer (then the scale is one of an output channel).  q: device [M][K] dense, scale: device
+ * fp32 [M]; neither may overlap x.  M >= 1, 1 <= K <= 65536. */
+flashbon_status flashbon_op_quant_rows(int32_t dtype, int32_t M, int32_t K, const void *x, int64_t x_row_stride,
+                                       int8_t *q, float *scale, void *stream);
+
+/* Linear layer on 8-bit integers: acc[m][n] = a_scale[m] w_scale[n] sum_k A[m][k] W[n][k], then an epilogue of
+ * flashbon_op_linear (FLASHBON_EPI_RESIDUAL adds to residual_in, NULL: to out itself).  The sum is exact; it is
+ * converted to fp32, multiplied by w_scale[n], and by a_scale[m] and added to the bias in one rounding.  So a row's
+ * bits do not depend on the other rows, and no workspace is needed.
+ * A: device int8 [M][K], W: device int8 [N][K], dense (every value from -128 to 127 is taken); a_scale: device fp32 [M];
+ * w_scale: device fp32 [N]; bias, gate, cache_out, out as in flashbon_op_linear, act of `dtype` where the epilogue
+ * stores act; residual_in: device fp32 [M][N], read only, out itself or disjoint from it.  gate, residual_in and
+ * cache_out are for FLASHBON_EPI_RESIDUAL and ignored by the others; cache_out must not overlap anything else.
+ * M >= 1, 1 <= N <= 2^20, 1 <= K <= 65536. */
+flashbon_status flashbon_op_linear_i8(int32_t dtype, int32_t M, int32_t N, int32_t K, const int8_t *A,
+                                      const float *a_scale, const int8_t *W, const float *w_scale, const float *bias,
+                                      int32_t epilogue, void *out, const float *gate, const float *residual_in,
+                                      float *cache_out, void *stream);
+
+enum {
+  FLASHBON_NORM_NONE = 0,  /* the row as it is                                                  */
+  FLASHBON_NORM_LAYER = 1, /* (v - mean) / sqrt(biased variance + eps), not affine              */
+  FLASHBON_NORM_RMS = 2    /* v / sqrt(mean of squares + eps)                                   */
+};
+
+/* The seam between two blocks in one pass over the rows: the norm after a block, its gate and the residual update, and
+ * the modulated norm before the next block:
+ *   h[m][d] = alpha x[m][d] + gate[d] (post_norm(y[m])[d] post_gain[d])         -> x_out (fp32)
+ *   a[m][d] = pre_norm(h[m])[d] (1 + scale[d]) + shift[d]                        -> out (act), or q and q_scale
+ * pre_norm reads h as it is rounded to fp32.  q and q_scale are what flashbon_op_quant_rows would make of a's exact
+ * rows: statistics are held in 64 bits, and with q the values too, so the codes do not depend on the kernel's order.
+ * x: device fp32 [M][D]; y: device act [M][D], or NULL (no branch: h = alpha x; post_norm, post_gain and gate are
+ * ignored); post_gain, gate, scale, shift: device fp32 [D], each may be NULL (gain and gate 1, scale and shift 0).
+ * x_out: device fp32 [M][D], may be x itself, or NULL.  Of out (device act [M][D]) and q (device int8 [M][D], with
+ * q_scale device fp32 [M]) at most one is given; at least one of x_out, out and q.  Outputs must not overlap inputs
+ * otherwise.  alpha finite, eps positive and finite.  M >= 1, 1 <= D <= 6144. */
+flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, float eps, const float *x, float alpha,
+                                          const void *y, int32_t post_norm, const float *post_gain, const float *gate,
+                                          float *x_out, int32_t pre_norm, const float *shift, const float *scale,
+                                          void *out, int8_t *q, float *q_scale, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

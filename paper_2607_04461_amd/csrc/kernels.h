@@ -130,4 +130,36 @@ hipError_t launch_head_update(int n, int C, int H, int W, int p, const float *v,
 hipError_t launch_normals(int64_t count, uint32_t cand, uint32_t step, uint64_t seed, uint32_t *words,
                           float *normals, hipStream_t s);
 
+// ---- 8-bit layers
+// Rows x [M][K] (act, row stride in elements) to q [M][K] = nearest-even(x / scale[m]), scale[m] = max(max |x| / 127,
+// 2^-126); a row with an infinity or NaN: scale NaN, codes 0.  1 <= K <= 65536.
+hipError_t launch_quant_rows(ActType t, int M, int K, const void *x, int64_t x_row_stride, int8_t *q, float *scale,
+                             hipStream_t s);
+
+// C[m][n] = a_scale[m] w_scale[n] sum_k A[m][k] W[n][k] (+ epilogue; every one but EULER), the sum exact in 32 bits
+// (K <= 65536).  A [M][K], W [N][K]; any M, N, K >= 1 and any alignment of A and W.
+struct I8Args {
+  const int8_t *A = nullptr, *W = nullptr;
+  const float *a_scale = nullptr, *w_scale = nullptr;
+};
+hipError_t launch_linear_i8(ActType t, int epi, int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s);
+
+// The seam between two blocks: h = alpha x + gate (post(y) gain) -> x_out, then pre(h) (1 + scale) + shift -> out (act)
+// or q, q_scale (as launch_quant_rows).  y null: h = alpha x; null vectors: gain, gate 1, scale, shift 0; x_out, out and
+// q may be null, out and q are not both given.  x_out may be x itself.  1 <= D <= 6144.
+enum Norms { NORM_NONE = 0, NORM_LAYER = 1, NORM_RMS = 2 };
+struct SeamArgs {
+  int D;
+  int post, pre;                 // Norms
+  float alpha, eps;
+  const float *x;                // [M][D]
+  const void *y;                 // act [M][D]
+  const float *gain, *gate, *scale, *shift;   // [D]
+  float *x_out;                  // [M][D]
+  void *out;                     // act [M][D]
+  int8_t *q;                     // [M][D]
+  float *q_scale;                // [M]
+};
+hipError_t launch_norm_residual(ActType t, int M, const SeamArgs &a, hipStream_t s);
+
 }  // namespace fb

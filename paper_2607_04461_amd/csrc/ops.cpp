@@ -153,4 +153,58 @@ flashbon_status flashbon_op_unpatch_sde(int32_t n, int32_t C, int32_t H, int32_t
                   "unpatch_sde");
 }
 
+flashbon_status flashbon_op_quant_rows(int32_t dtype, int32_t M, int32_t K, const void *x, int64_t x_row_stride,
+                                       int8_t *q, float *scale, void *stream) {
+  if (dtype != FLASHBON_FP32 && dtype != FLASHBON_BF16) return fail(FLASHBON_EINVAL, "bad dtype");
+  if (M < 1 || K < 1 || K > 65536) return fail(FLASHBON_ESHAPE, "need M, K >= 1 and K <= 65536");
+  if (x_row_stride < K) return fail(FLASHBON_ESHAPE, "x_row_stride must be at least K");
+  if (!x || !q || !scale) return fail(FLASHBON_EINVAL, "x, q and scale are required");
+  ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
+  return launched(launch_quant_rows(t, M, K, x, x_row_stride, q, scale, (hipStream_t)stream), "quant_rows");
+}
+
+flashbon_status flashbon_op_linear_i8(int32_t dtype, int32_t M, int32_t N, int32_t K, const int8_t *A,
+                                      const float *a_scale, const int8_t *W, const float *w_scale, const float *bias,
+                                      int32_t epilogue, void *out, const float *gate, const float *residual_in,
+                                      float *cache_out, void *stream) {
+  if (dtype != FLASHBON_FP32 && dtype != FLASHBON_BF16) return fail(FLASHBON_EINVAL, "bad dtype");
+  if (M < 1 || N < 1 || K < 1 || N > (1 << 20) || K > 65536)
+    return fail(FLASHBON_ESHAPE, "need M, N, K >= 1, N <= 2^20 and K <= 65536");
+  if (!A || !a_scale || !W || !w_scale || !out) return fail(FLASHBON_EINVAL, "A, a_scale, W, w_scale and out are required");
+  if (epilogue < FLASHBON_EPI_STORE || epilogue > FLASHBON_EPI_RESIDUAL) return fail(FLASHBON_EINVAL, "bad epilogue");
+  I8Args g;
+  g.A = A; g.W = W; g.a_scale = a_scale; g.w_scale = w_scale;
+  EpiArgs e;
+  e.out = out; e.ldo = N; e.bias = bias;
+  if (epilogue == FLASHBON_EPI_RESIDUAL) {
+    e.gate = gate; e.cache = cache_out;
+    if (residual_in != out) e.res_in = residual_in;
+  }
+  ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
+  return launched(launch_linear_i8(t, epilogue, M, N, K, g, e, (hipStream_t)stream), "linear_i8");
+}
+
+flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, float eps, const float *x, float alpha,
+                                          const void *y, int32_t post_norm, const float *post_gain, const float *gate,
+                                          float *x_out, int32_t pre_norm, const float *shift, const float *scale,
+                                          void *out, int8_t *q, float *q_scale, void *stream) {
+  if (dtype != FLASHBON_FP32 && dtype != FLASHBON_BF16) return fail(FLASHBON_EINVAL, "bad dtype");
+  if (M < 1 || D < 1 || D > 6144) return fail(FLASHBON_ESHAPE, "need M >= 1, 1 <= D <= 6144");
+  if (!x) return fail(FLASHBON_EINVAL, "x is required");
+  if (!x_out && !out && !q) return fail(FLASHBON_EINVAL, "one of x_out, out and q is required");
+  if (out && q) return fail(FLASHBON_EINVAL, "out and q exclude each other");
+  if ((q == nullptr) != (q_scale == nullptr)) return fail(FLASHBON_EINVAL, "q and q_scale go together");
+  if (post_norm < FLASHBON_NORM_NONE || post_norm > FLASHBON_NORM_RMS || pre_norm < FLASHBON_NORM_NONE ||
+      pre_norm > FLASHBON_NORM_RMS)
+    return fail(FLASHBON_EINVAL, "bad norm");
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(FLASHBON_EINVAL, "eps must be positive and finite");
+  if (!std::isfinite(alpha)) return fail(FLASHBON_EINVAL, "alpha must be finite");
+  SeamArgs a;
+  a.D = D; a.post = post_norm; a.pre = pre_norm; a.alpha = alpha; a.eps = eps;
+  a.x = x; a.y = y; a.gain = post_gain; a.gate = gate; a.scale = scale; a.shift = shift;
+  a.x_out = x_out; a.out = out; a.q = q; a.q_scale = q_scale;
+  ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
+  return launched(launch_norm_residual(t, M, a, (hipStream_t)stream), "norm_residual");
+}
+
 }  // extern "C"

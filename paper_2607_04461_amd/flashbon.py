@@ -20,6 +20,7 @@ OK, EINVAL, ESHAPE, ENOMEM, EHIP, ESTATE = 0, -1, -2, -3, -4, -5
 FP32, BF16 = 0, 1
 COMPUTE, SKIP, PROXY = 0, 1, 2
 EPI_STORE, EPI_GELU, EPI_STORE_F32, EPI_RESIDUAL = 0, 1, 2, 3
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
 SITES = ["qkv", "attn_self", "out", "cross_q", "attn_cross", "out_cross", "mlp_up", "mlp_down", "norm",
          "proxy", "embed", "head", "time", "text"]
 
@@ -71,6 +72,7 @@ EXPORTS = [
     "flashbon_last_error", "flashbon_set_timing", "flashbon_read_timing", "flashbon_op_linear", "flashbon_op_linear_residual", "flashbon_op_linear_plan", "flashbon_op_attention", "flashbon_op_ln_mod",
     "flashbon_op_proxy", "flashbon_op_normals", "flashbon_op_unpatch_sde", "flashbon_select",
     "flashbon_refine_step_noalloc", "flashbon_op_linear_ws",
+    "flashbon_op_quant_rows", "flashbon_op_linear_i8", "flashbon_op_norm_residual",
 ]
 NOALLOC_SCRATCH_BYTES = 128 << 20
 
@@ -137,6 +139,12 @@ def load() -> ctypes.CDLL:
     L.flashbon_op_unpatch_sde.argtypes = [i32, i32, i32, i32, i32, vp, vp, f32, f32, f32, ctypes.c_uint64,
                                           i32, i32, vp]
     L.flashbon_op_unpatch_sde.restype = i32
+    L.flashbon_op_quant_rows.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp]
+    L.flashbon_op_quant_rows.restype = i32
+    L.flashbon_op_linear_i8.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+    L.flashbon_op_linear_i8.restype = i32
+    L.flashbon_op_norm_residual.argtypes = [i32, i32, i32, f32, vp, f32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    L.flashbon_op_norm_residual.restype = i32
     L.flashbon_select.argtypes = [i32, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, ctypes.c_double,
                                   ctypes.c_double, JUDGE_FN, vp, ctypes.POINTER(ctypes.c_int32),
                                   ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)]
@@ -518,3 +526,113 @@ def flashbon_op_normals(count, candidate, step, seed, words=None, normals=None, 
 def flashbon_op_unpatch_sde(n, C, H, W, p, v, z, t_cur, t_next, a, seed, step, row0=0, stream=None):
     _check(load().flashbon_op_unpatch_sde(n, C, H, W, p, _ptr(v), _ptr(z), t_cur, t_next, a, seed, step, row0,
                                           _stream(stream)), "flashbon_op_unpatch_sde")
+
+
+# 8-bit layers.  Sizes are given, as in the calls above; every tensor is checked against them.
+
+def _act(dtype):
+    import torch
+    if dtype not in (FP32, BF16):
+        raise ValueError("dtype must be FP32 or BF16")
+    return torch.bfloat16 if dtype == BF16 else torch.float32
+
+
+def _check_sized(dtype, count: int, device: Optional[int], required: bool, **tensors) -> None:
+    """Every tensor: of ``dtype``, contiguous, of at least ``count`` elements, on the GPU ``device`` (None: anywhere)."""
+    for name, t in tensors.items():
+        if t is None:
+            if required:
+                raise ValueError(f"{name} is required")
+            continue
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if t.numel() < count:
+            raise ValueError(f"{name} holds {t.numel()} elements, needs {count}")
+        if device is not None and (not t.is_cuda or t.device.index != device):
+            raise ValueError(f"{name} must be on the current device (cuda:{device}), got {t.device}")
+
+
+def _current_device(require_device: bool) -> Optional[int]:
+    import torch
+    return torch.cuda.current_device() if require_device else None
+
+
+def validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale, *, require_device: bool = True) -> None:
+    """Raise ValueError unless the tensors are what flashbon_op_quant_rows reads and writes.  ``x`` may be a view of
+    wider rows: 2-D with a unit column stride."""
+    import torch
+    device = _current_device(require_device)
+    if M < 1 or K < 1 or x_row_stride < K:
+        raise ValueError(f"need M, K >= 1 and a row stride of at least K, got {M}, {K}, {x_row_stride}")
+    if x.dtype != _act(dtype):
+        raise ValueError(f"x must be {_act(dtype)}, got {x.dtype}")
+    if x.is_contiguous():
+        if x.numel() < (M - 1) * x_row_stride + K:
+            raise ValueError(f"x holds {x.numel()} elements, {M} rows of {K} at stride {x_row_stride} need more")
+    elif x.dim() != 2 or x.stride(1) != 1 or x.stride(0) != x_row_stride or x.shape[0] < M or x.shape[1] < K:
+        raise ValueError(f"x must be contiguous or [{M}, {K}] with strides ({x_row_stride}, 1), got "
+                         f"{tuple(x.shape)} with {x.stride()}")
+    if device is not None and (not x.is_cuda or x.device.index != device):
+        raise ValueError(f"x must be on the current device (cuda:{device}), got {x.device}")
+    _check_sized(torch.int8, M * K, device, True, q=q)
+    _check_sized(torch.float32, M, device, True, scale=scale)
+
+
+def flashbon_op_quant_rows(dtype, M, K, x, q, scale, x_row_stride=None, stream=None):
+    """Rows x [M][K] to int8 codes q and one scale a row; ``x_row_stride`` in elements (None: a matrix's own, else K)."""
+    if x_row_stride is None:
+        x_row_stride = int(x.stride(0)) if x.dim() == 2 and x.shape[0] > 1 else K
+    validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale)
+    _check(load().flashbon_op_quant_rows(dtype, M, K, _ptr(x), x_row_stride, _ptr(q), _ptr(scale), _stream(stream)),
+           "flashbon_op_quant_rows")
+
+
+def validate_linear_i8(dtype, M, N, K, A, a_scale, W, w_scale, bias, epilogue, out, gate=None, residual_in=None,
+                       cache_out=None, *, require_device: bool = True) -> None:
+    """Raise ValueError unless the tensors are what flashbon_op_linear_i8 reads and writes."""
+    import torch
+    f32, device = torch.float32, _current_device(require_device)
+    _check_sized(torch.int8, M * K, device, True, A=A)
+    _check_sized(torch.int8, N * K, device, True, W=W)
+    _check_sized(f32, M, device, True, a_scale=a_scale)
+    _check_sized(f32, N, device, True, w_scale=w_scale)
+    _check_sized(f32, N, device, False, bias=bias)
+    act = _act(dtype)
+    _check_sized(act if epilogue in (EPI_STORE, EPI_GELU) else f32, M * N, device, True, out=out)
+    if epilogue == EPI_RESIDUAL:
+        _check_sized(f32, N, device, False, gate=gate)
+        _check_sized(f32, M * N, device, False, residual_in=residual_in, cache_out=cache_out)
+
+
+def flashbon_op_linear_i8(dtype, M, N, K, A, a_scale, W, w_scale, bias, epilogue, out, gate=None, residual_in=None,
+                          cache_out=None, stream=None):
+    """Linear layer on int8 rows A [M][K] and weights W [N][K] with a scale a token and an output channel."""
+    validate_linear_i8(dtype, M, N, K, A, a_scale, W, w_scale, bias, epilogue, out, gate, residual_in, cache_out)
+    _check(load().flashbon_op_linear_i8(dtype, M, N, K, _ptr(A), _ptr(a_scale), _ptr(W), _ptr(w_scale), _ptr(bias),
+                                        epilogue, _ptr(out), _ptr(gate), _ptr(residual_in), _ptr(cache_out),
+                                        _stream(stream)), "flashbon_op_linear_i8")
+
+
+def validate_norm_residual(dtype, M, D, x, y=None, out=None, q=None, q_scale=None, x_out=None, post_gain=None, gate=None,
+                           shift=None, scale=None, *, require_device: bool = True) -> None:
+    """Raise ValueError unless the tensors are what flashbon_op_norm_residual reads and writes."""
+    import torch
+    f32, device, act = torch.float32, _current_device(require_device), _act(dtype)
+    _check_sized(f32, M * D, device, True, x=x)
+    _check_sized(f32, M * D, device, False, x_out=x_out)
+    _check_sized(act, M * D, device, False, y=y, out=out)
+    _check_sized(f32, D, device, False, post_gain=post_gain, gate=gate, shift=shift, scale=scale)
+    _check_sized(torch.int8, M * D, device, False, q=q)
+    _check_sized(f32, M, device, False, q_scale=q_scale)
+
+
+def flashbon_op_norm_residual(dtype, M, D, eps, x, y=None, *, alpha=1.0, post_norm=NORM_NONE, post_gain=None, gate=None,
+                              x_out=None, pre_norm=NORM_LAYER, shift=None, scale=None, out=None, q=None, q_scale=None,
+                              stream=None):
+    """h = alpha x + gate (post_norm(y) post_gain) -> x_out; pre_norm(h) (1 + scale) + shift -> out, or q and q_scale."""
+    validate_norm_residual(dtype, M, D, x, y, out, q, q_scale, x_out, post_gain, gate, shift, scale)
+    _check(load().flashbon_op_norm_residual(dtype, M, D, eps, _ptr(x), alpha, _ptr(y), post_norm, _ptr(post_gain),
+                                            _ptr(gate), _ptr(x_out), pre_norm, _ptr(shift), _ptr(scale), _ptr(out),
+                                            _ptr(q), _ptr(q_scale), _stream(stream)), "flashbon_op_norm_residual")
