@@ -201,6 +201,28 @@ def test_linear_options(M, N, K, kw):
     _linear(M, N, K, "bf16", "residual", **kw)
 
 
+TILES = ["split:16x16", "split:32x16", "split:32x32", "split:64x32", "any", "256x256", "128x256", "128x128:two", "128x128"]
+
+
+# a K of one, two, three and more of the ring's K tiles, K tails of 16 to 112, rows and columns on and beside the tiles' edges
+@pytest.mark.parametrize("M,N,K", [(1, 8, 16), (129, 136, 112), (260, 264, 128), (255, 256, 240), (257, 512, 256), (300, 520, 400),
+                                   (128, 248, 528), (513, 264, 1040)])
+@pytest.mark.parametrize("epi", ["store", "gelu", "residual"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_every_kernel_gives_the_same_bits(M, N, K, epi, dtype, monkeypatch):
+    first = None
+    for tile in TILES:
+        monkeypatch.setenv("FLASHBON_I8_TILE", tile)
+        got = _linear(M, N, K, dtype, epi)
+        first = got if first is None else first
+        assert torch.equal(got, first), tile
+
+
+@pytest.mark.parametrize("M,N", [(2, 40), (40000, 16)])
+def test_more_rows_than_a_launch_takes(M, N):
+    _linear(M, N, 48, "bf16", "residual")
+
+
 @pytest.mark.parametrize("offset", [1, 4, 8])
 @pytest.mark.parametrize("M,N,K", [(70, 72, 80), (5, 48, 512), (300, 264, 256)])
 @pytest.mark.parametrize("epi", ["store", "residual"])
