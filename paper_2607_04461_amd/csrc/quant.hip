@@ -51,11 +51,40 @@ __device__ __forceinline__ void load8(const bf16 *p, int c, int n, float (&v)[8]
     for (int i = 0; i < 8; ++i) v[i] = c + i < n ? (float)p[c + i] : 0.f;
   }
 }
-template <bool TAIL>
+// Eight elements as they are stored.
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+  float v[8];
+  template <bool TAIL> __device__ __forceinline__ void load(const float *p, int c, int n) { load8<TAIL>(p, c, n, v); }
+  __device__ __forceinline__ float operator[](int j) const { return v[j]; }
+};
+template <> struct Piece<bf16> {
+  u32x4 v;
+  template <bool TAIL> __device__ __forceinline__ void load(const bf16 *p, int c, int n) {
+    if (!TAIL || c + 8 <= n) {
+      v = *reinterpret_cast<const u32x4u *>(p + c);
+    } else {
+      v = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < n) v[j >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, p[c + j]) << (16 * (j & 1));
+    }
+  }
+  __device__ __forceinline__ float operator[](int j) const {
+    return __builtin_bit_cast(float, j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16);
+  }
+};
+template <bool TAIL, bool NT = false>
 __device__ __forceinline__ void store8(float *p, int c, int n, const float (&v)[8]) {
   if (!TAIL || c + 8 <= n) {
-    *reinterpret_cast<f32x4u *>(p + c) = f32x4u{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4u *>(p + c + 4) = f32x4u{v[4], v[5], v[6], v[7]};
+    const f32x4u a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+    if constexpr (NT) {   // past the caches
+      __builtin_nontemporal_store(a, reinterpret_cast<f32x4u *>(p + c));
+      __builtin_nontemporal_store(b, reinterpret_cast<f32x4u *>(p + c + 4));
+    } else {
+      *reinterpret_cast<f32x4u *>(p + c) = a;
+      *reinterpret_cast<f32x4u *>(p + c + 4) = b;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -73,14 +102,16 @@ __device__ __forceinline__ void store8(bf16 *p, int c, int n, const float (&v)[8
       if (c + i < n) p[c + i] = (bf16)v[i];
   }
 }
+// Eight codes, each in the low byte of a word.
 template <bool TAIL>
-__device__ __forceinline__ void store_codes(int8_t *p, int c, int n, const int (&q)[8]) {
+__device__ __forceinline__ void store_codes(int8_t *p, int c, int n, const uint32_t (&q)[8]) {
   if (!TAIL || c + 8 <= n) {
     u32x2u w;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      w[i] = (uint32_t)(q[4 * i] & 255) | (uint32_t)(q[4 * i + 1] & 255) << 8 | (uint32_t)(q[4 * i + 2] & 255) << 16 |
-             (uint32_t)q[4 * i + 3] << 24;
+    for (int i = 0; i < 2; ++i) {   // bytes 0 and 4 of a pair, then the two halves
+      const uint32_t lo = __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0c0c0400), hi = __builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x0c0c0400);
+      w[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100);
+    }
     *reinterpret_cast<u32x2u *>(p + c) = w;
   } else {
 #pragma unroll
@@ -89,20 +120,64 @@ __device__ __forceinline__ void store_codes(int8_t *p, int c, int n, const int (
   }
 }
 
-// Threads that share a row: one wave, or a workgroup of its own.
-template <int TR> struct Row {
-  static constexpr int WAVES = TR / 64, BLOCK = TR == 64 ? 256 : TR;
-  static __device__ __forceinline__ int64_t index() {
-    return TR == 64 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
+// Reductions over the 16, 32 or 64 lanes that share a row, by moves between lanes rather than through LDS (a step of
+// which waits some hundred cycles: with the vectors read early one token of 1536 takes 3.9 us in place of 4.8).  In a group of
+// 2, 4 and 8 lanes that already hold their result the mirrored lane belongs to the other half of the next larger one; rows
+// of 16 and halves of 32 lanes come together by gfx950's swaps.  Both sides of an exchange add the same two numbers.
+template <int CTRL> __device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+template <int CTRL> __device__ __forceinline__ double moved(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)moved<CTRL>((uint32_t)(u >> 32)) << 32 | moved<CTRL>((uint32_t)u));
+}
+template <bool WIDE> __device__ __forceinline__ void both(uint32_t v, uint32_t &a, uint32_t &b) {
+  const auto r = WIDE ? __builtin_amdgcn_permlane32_swap(v, v, false, false) : __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  a = r[0];
+  b = r[1];
+}
+template <bool WIDE> __device__ __forceinline__ void both(double v, double &a, double &b) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  uint32_t al, ah, bl, bh;
+  both<WIDE>((uint32_t)u, al, bl);
+  both<WIDE>((uint32_t)(u >> 32), ah, bh);
+  a = __builtin_bit_cast(double, (uint64_t)ah << 32 | al);
+  b = __builtin_bit_cast(double, (uint64_t)bh << 32 | bl);
+}
+template <int LANES, typename V, typename Op> __device__ __forceinline__ V reduced(V v, Op op) {
+  v = op(v, moved<0xb1>(v));    // lanes 1 0 3 2
+  v = op(v, moved<0x4e>(v));    // 2 3 0 1
+  v = op(v, moved<0x141>(v));   // mirrored within 8
+  v = op(v, moved<0x140>(v));   // within 16
+  V a, b;
+  if constexpr (LANES >= 32) {
+    both<false>(v, a, b);
+    v = op(a, b);
   }
-  static __device__ __forceinline__ int lane() { return TR == 64 ? threadIdx.x & 63 : threadIdx.x; }
+  if constexpr (LANES >= 64) {
+    both<true>(v, a, b);
+    v = op(a, b);
+  }
+  return v;
+}
+
+// Threads that share a row: 16, 32 or 64 lanes of a wave, or the TR threads of a workgroup of its own.
+template <int TR> struct Row {
+  static constexpr int WAVES = TR <= 64 ? 1 : TR / 64, BLOCK = TR <= 64 ? 256 : TR, ROWS = BLOCK / TR;
+  static __device__ __forceinline__ int64_t index() { return (int64_t)blockIdx.x * ROWS + threadIdx.x / TR; }
+  static __device__ __forceinline__ int lane() { return threadIdx.x % TR; }
+  static unsigned blocks(int M) { return (unsigned)(((int64_t)M + ROWS - 1) / ROWS); }
+  static constexpr int LANES = TR < 64 ? TR : 64;
 };
 
 }  // namespace
 
 // ------------------------------------------------------------------------------------- rows to codes
 // TR threads a row, NV pieces of eight elements each, held in registers between the maximum and the codes, so that
-// a row is read once.  Bound by HBM (M K (2 or 4 + 1) bytes).
+// a row is read once.  Bound by HBM (M K (2 or 4 + 1) bytes): 24960 x 8960 bf16 130 us, 5.2 TB/s (what a large copy reaches);
+// 13824 x 5120 fp32 65 us, 5.5 TB/s; 1 x 1536 3.0 us, a launch's latency.  With five operations an element the codes hide
+// behind the loads; the threads of a row are the fewest that hold it with eight pieces or less, so that little of the
+// last pass is idle (8960 on 256 x 8 pieces 155 us, on 256 x 5 136).
 template <typename T, int TR, int NV, bool TAIL>
 __global__ __launch_bounds__(Row<TR>::BLOCK) void k_quant_rows(int M, int K, const T *__restrict__ x, int64_t xs,
                                                                int8_t *__restrict__ q, float *__restrict__ scale) {
@@ -124,8 +199,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_quant_rows(int M, int K, con
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = max(top, __builtin_bit_cast(uint32_t, v[i][j]) & 0x7fffffffu);
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  top = reduced<R::LANES>(top, [](uint32_t a, uint32_t b) { return max(a, b); });
   if constexpr (R::WAVES > 1) {
     __shared__ uint32_t part[R::WAVES];
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
@@ -141,19 +215,21 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_quant_rows(int M, int K, con
   for (int i = 0; i < NV; ++i) {
     const int c = 8 * (R::lane() + TR * i);
     if (c >= K) break;
-    int code[8];
-    bool near = false;
+    // v inv, rounded once, to the nearest integer: added to 1.5 2^23 the integer is what the low bits hold.  It is off v / s
+    // by less than 127 2^-24 < 8e-6: further than that from a border it decides.
+    constexpr float kRound = 12582912.0f;
+    uint32_t code[8];
+    float far = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      // v inv is off v / s by less than 127 (2^-23 + 2^-24) < 3e-5: further than that from a border it decides
-      const float t = v[i][j] * inv, r = __builtin_rintf(t);
-      near |= fabsf(t - r) > 0.49995f;
-      code[j] = (int)r;
+      const float r = fmaf(v[i][j], inv, kRound);
+      far = fmaxf(far, fabsf(fmaf(v[i][j], inv, kRound - r)));
+      code[j] = __builtin_bit_cast(uint32_t, r);
     }
-    if (near) {
+    if (far > 0.49998f) {
       // two numbers of 24 bits whose quotient is no border are further from one than 64 bits round
 #pragma unroll
-      for (int j = 0; j < 8; ++j) code[j] = (int)__builtin_rint((double)v[i][j] / (double)s);
+      for (int j = 0; j < 8; ++j) code[j] = (uint32_t)(int)__builtin_rint((double)v[i][j] / (double)s);
     }
     if (bad) {
 #pragma unroll
@@ -165,25 +241,21 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_quant_rows(int M, int K, con
 
 template <typename T, int TR, int NV>
 static hipError_t quant_rows(int M, int K, const T *x, int64_t xs, int8_t *q, float *scale, hipStream_t s) {
-  const unsigned blocks = TR == 64 ? (unsigned)(((int64_t)M + 3) / 4) : (unsigned)M;
-  if (K % 8)
-    hipLaunchKernelGGL((k_quant_rows<T, TR, NV, true>), dim3(blocks), dim3(Row<TR>::BLOCK), 0, s, M, K, x, xs, q, scale);
-  else
-    hipLaunchKernelGGL((k_quant_rows<T, TR, NV, false>), dim3(blocks), dim3(Row<TR>::BLOCK), 0, s, M, K, x, xs, q, scale);
+  const dim3 grid(Row<TR>::blocks(M)), block(Row<TR>::BLOCK);
+  if (K % 8) hipLaunchKernelGGL((k_quant_rows<T, TR, NV, true>), grid, block, 0, s, M, K, x, xs, q, scale);
+  else hipLaunchKernelGGL((k_quant_rows<T, TR, NV, false>), grid, block, 0, s, M, K, x, xs, q, scale);
   return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t quant_rows_of(int M, int K, const T *x, int64_t xs, int8_t *q, float *scale, hipStream_t s) {
   const int pieces = (K + 7) / 8;
-  if (pieces <= 64) return quant_rows<T, 64, 1>(M, K, x, xs, q, scale, s);
-  if (pieces <= 128) return quant_rows<T, 64, 2>(M, K, x, xs, q, scale, s);
-  if (pieces <= 256) return quant_rows<T, 64, 4>(M, K, x, xs, q, scale, s);
-  if (pieces <= 512) return quant_rows<T, 256, 2>(M, K, x, xs, q, scale, s);
-  if (pieces <= 1024) return quant_rows<T, 256, 4>(M, K, x, xs, q, scale, s);
-  if (pieces <= 2048) return quant_rows<T, 256, 8>(M, K, x, xs, q, scale, s);
-  if (pieces <= 4096) return quant_rows<T, 1024, 4>(M, K, x, xs, q, scale, s);
-  return quant_rows<T, 1024, 8>(M, K, x, xs, q, scale, s);
+#define FB_ROWS(TR, NV) if (pieces <= TR * NV) return quant_rows<T, TR, NV>(M, K, x, xs, q, scale, s);
+  FB_ROWS(16, 1) FB_ROWS(32, 1) FB_ROWS(64, 1) FB_ROWS(64, 2) FB_ROWS(64, 3) FB_ROWS(64, 4)
+  FB_ROWS(256, 2) FB_ROWS(256, 3) FB_ROWS(256, 4) FB_ROWS(256, 5) FB_ROWS(256, 6) FB_ROWS(256, 8)
+  FB_ROWS(1024, 3) FB_ROWS(1024, 4) FB_ROWS(1024, 6) FB_ROWS(1024, 8)
+#undef FB_ROWS
+  return hipErrorInvalidValue;
 }
 
 // Launches take less than 2^32 threads: rows in parts.
@@ -207,19 +279,19 @@ hipError_t launch_quant_rows(ActType t, int M, int K, const void *x, int64_t x_r
 // come from one pass of sums in 64 bits over the row less its first element (the pivot), so that a large common offset
 // costs no digits: the variance is off by about 2^-53 (1 + (mean - pivot)^2 / variance) of itself.  Codes are decided on
 // values in 64 bits as well.
-// Bound by HBM: (4 + e) M D bytes read, 4 M D + (e or 1) M D written.
+// Bound by HBM: (4 + e) M D bytes read, 4 M D + (e or 1) M D written: 24960 x 1536 bf16 to codes 99 us (4.2 TB/s) and to
+// activations 98 (4.7), 16384 x 5120 to activations 212 (4.7), one token of 1536 3.9 us.  The 64-bit arithmetic, some 30
+// instructions an element at the rate of 32-bit ones, hides behind that, as long as registers leave five waves a SIMD:
+// y stays as it is stored and values are formed anew from h (held in 64 bits instead, 105 us).
 namespace {
 
-// Sums over the row of two numbers and, for codes, a maximum.  Every call has LDS of its own, so that one barrier does.
-template <int TR> __device__ __forceinline__ void row_sums(double &a, double &b) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    a += __shfl_xor(a, o, 64);
-    b += __shfl_xor(b, o, 64);
-  }
-}
-template <int TR> __device__ __forceinline__ void join_sums(double &a, double &b, double (*part)[2]) {
-  if constexpr (Row<TR>::WAVES > 1) {
+// The row's two sums, for all its threads.  part: LDS that this call alone uses, so that one barrier does.
+template <int TR> __device__ __forceinline__ void row_sums(double &a, double &b, double (*part)[2]) {
+  using R = Row<TR>;
+  const auto sum = [](double p, double q) { return p + q; };
+  a = reduced<R::LANES>(a, sum);
+  b = reduced<R::LANES>(b, sum);
+  if constexpr (R::WAVES > 1) {
     if ((threadIdx.x & 63) == 0) {
       part[threadIdx.x >> 6][0] = a;
       part[threadIdx.x >> 6][1] = b;
@@ -227,164 +299,184 @@ template <int TR> __device__ __forceinline__ void join_sums(double &a, double &b
     __syncthreads();
     a = b = 0;
 #pragma unroll
-    for (int w = 0; w < Row<TR>::WAVES; ++w) {
+    for (int w = 0; w < R::WAVES; ++w) {
       a += part[w][0];
       b += part[w][1];
     }
   }
 }
 
-struct Norm {
-  double mean, rstd;
+// A row's norm, (v - mean) by, in type V; from the sums of v - pivot and of its square over D elements (pivot 0 but for
+// LayerNorm's, whose mean is pivot + sum / D).
+template <typename V> struct Norm;
+template <> struct Norm<double> {
+  double by = 1.0, plus = 0.0;
+  __device__ __forceinline__ Norm(int kind, double pivot, double sum, double sq, int D, double eps) {
+    if (kind == NORM_NONE) return;
+    const double n = D, m = kind == NORM_LAYER ? sum / n : 0.0, var = sq / n - m * m;
+    by = 1.0 / sqrt((var < 0 ? 0 : var) + eps);   // NaN stays
+    plus = -(pivot + m) * by;
+  }
+  __device__ __forceinline__ double operator()(float v) const { return fma((double)v, by, plus); }
 };
-// From the sums of (v - pivot) and its square over D elements.
-__device__ __forceinline__ Norm norm_of(int kind, double pivot, double sum, double sq, int D, double eps) {
-  const double n = D, m = kind == NORM_LAYER ? sum / n : 0.0;
-  double var = sq / n - m * m;
-  var = var < 0 ? 0 : var;   // NaN stays
-  return {kind == NORM_LAYER ? pivot + m : 0.0, 1.0 / sqrt(var + eps)};
+template <> struct Norm<float> {   // the mean in two parts, so that it costs no digits of v - mean
+  float by, mean, rest;
+  __device__ __forceinline__ Norm(int kind, double pivot, double sum, double sq, int D, double eps) {
+    const Norm<double> n(kind, pivot, sum, sq, D, eps);
+    const double m = kind == NORM_LAYER ? pivot + sum / (double)D : 0.0;
+    by = (float)n.by;
+    mean = (float)m;
+    rest = (float)(m - (double)mean);
+  }
+  __device__ __forceinline__ float operator()(float v) const { return ((v - mean) - rest) * by; }
+};
+
+// Elements c .. c + 7 of a vector, or eight times `otherwise` for none.
+template <bool TAIL>
+__device__ __forceinline__ void load8_or(const float *p, float otherwise, int c, int n, float (&v)[8]) {
+  if (p) {
+    load8<TAIL>(p, c, n, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = otherwise;
+  }
 }
 
 }  // namespace
 
 enum { SEAM_NONE = 0, SEAM_ACT = 1, SEAM_I8 = 2 };
 
-template <typename T, int TR, int NV, bool TAIL, int OUT>
+template <typename T, int TR, int NV, bool TAIL, int OUT, bool NT>
 __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArgs a) {
   using R = Row<TR>;
   using V = std::conditional_t<OUT == SEAM_I8, double, float>;   // of the elements
-  __shared__ double part[R::WAVES > 1 ? 2 * R::WAVES : 1][2], tops[R::WAVES];
+  __shared__ double part[2 * R::WAVES][2], tops[R::WAVES];
   const int64_t row = R::index();
   if (row >= M) return;
   const int D = a.D;
   const float *xr = a.x + row * D;
   const T *yr = (const T *)a.y + row * D;
+  const V alpha = (V)a.alpha;
   float h[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = 8 * (R::lane() + TR * i);
+    if (c < D) load8<TAIL>(xr, c, D, h[i]);
+  }
+  // one piece a thread: what it needs of the vectors is on its way before the sums
+  constexpr bool EARLY = NV == 1;
+  float gain[8], gate[8], scale[8], shift[8];
+  if (EARLY && 8 * R::lane() < D) {
+    load8_or<TAIL>(a.gain, 1.f, 8 * R::lane(), D, gain);
+    load8_or<TAIL>(a.gate, 1.f, 8 * R::lane(), D, gate);
+    load8_or<TAIL>(a.scale, 0.f, 8 * R::lane(), D, scale);
+    load8_or<TAIL>(a.shift, 0.f, 8 * R::lane(), D, shift);
+  }
   if (a.y) {
-    float y[NV][8];
-    Norm n = {0.0, 1.0};
+    Piece<T> y[NV];
     const double pivot = a.post == NORM_LAYER ? (double)to_f32(yr[0]) : 0.0;
     double sum = 0, sq = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
-      if (c < D) {
-        load8<TAIL>(yr, c, D, y[i]);
-        load8<TAIL>(xr, c, D, h[i]);
-        if (a.post != NORM_NONE) {
+      if (c >= D) break;
+      y[i].template load<TAIL>(yr, c, D);
+      if (a.post == NORM_NONE) continue;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if (TAIL && c + j >= D) break;
-            const double d = (double)y[i][j] - pivot;
-            sum += d;
-            sq = fma(d, d, sq);
-          }
-        }
+      for (int j = 0; j < 8; ++j) {
+        if (TAIL && c + j >= D) break;
+        const double d = (double)y[i][j] - pivot;
+        sum += d;
+        sq = fma(d, d, sq);
       }
     }
-    if (a.post != NORM_NONE) {
-      row_sums<TR>(sum, sq);
-      join_sums<TR>(sum, sq, part);
-      n = norm_of(a.post, pivot, sum, sq, D, a.eps);
-    }
-    const V mean = (V)n.mean, rstd = (V)n.rstd, alpha = (V)a.alpha;
+    if (a.post != NORM_NONE) row_sums<TR>(sum, sq, part);
+    const Norm<V> norm(a.post, pivot, sum, sq, D, a.eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
       if (c >= D) break;
-      float gain[8], gate[8];
-      if (a.gain) load8<TAIL>(a.gain, c, D, gain);
-      if (a.gate) load8<TAIL>(a.gate, c, D, gate);
+      if constexpr (!EARLY) {
+        load8_or<TAIL>(a.gain, 1.f, c, D, gain);
+        load8_or<TAIL>(a.gate, 1.f, c, D, gate);
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        V u = ((V)y[i][j] - mean) * rstd;
-        if (a.gain) u *= (V)gain[j];
-        h[i][j] = (float)(a.gate ? fma((V)gate[j], u, alpha * (V)h[i][j]) : alpha * (V)h[i][j] + u);
+        if (TAIL && c + j >= D) break;
+        h[i][j] = (float)fma((V)gate[j] * (V)gain[j], norm(y[i][j]), alpha * (V)h[i][j]);
       }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = 8 * (R::lane() + TR * i);
-      if (c >= D) break;
-      load8<TAIL>(xr, c, D, h[i]);
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[i][j] = a.alpha * h[i][j];
-    }
   }
   if (a.x_out) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
-      if (c < D) store8<TAIL>(a.x_out + row * D, c, D, h[i]);
+      if (c < D) store8<TAIL, NT>(a.x_out + row * D, c, D, h[i]);
     }
   }
   if constexpr (OUT != SEAM_NONE) {
-    Norm n = {0.0, 1.0};
-    if (a.pre != NORM_NONE) {
-      // the row's first element: of lane 0, for rows of several waves through LDS (read by all at the sums' barrier)
-      double pivot = 0, sum = 0, sq = 0;
-      if (a.pre == NORM_LAYER) {
-        float first = h[0][0];
-        if constexpr (R::WAVES > 1) {
-          if (threadIdx.x == 0) tops[0] = first;
-          __syncthreads();
-          first = (float)tops[0];
-        }
-        pivot = (double)__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, first)));
-      }
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = 8 * (R::lane() + TR * i);
-        if (c < D) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if (TAIL && c + j >= D) break;
-            const double d = (double)h[i][j] - pivot;
-            sum += d;
-            sq = fma(d, d, sq);
-          }
-        }
-      }
-      row_sums<TR>(sum, sq);
-      join_sums<TR>(sum, sq, part + (R::WAVES > 1 ? R::WAVES : 0));
-      n = norm_of(a.pre, pivot, sum, sq, D, a.eps);
-    }
-    const V mean = (V)n.mean, rstd = (V)n.rstd;
+    double pivot = 0, sum = 0, sq = 0;
     V v[NV][8], top = 0;
+    if (a.pre == NORM_LAYER) {
+      // the row's first element: of its first lane, for rows of several waves through LDS (read by all at the sums' barrier)
+      float first = __shfl(h[0][0], TR < 64 ? (int)(threadIdx.x & 63 & ~(TR - 1)) : 0, 64);
+      if constexpr (R::WAVES > 1) {
+        if (threadIdx.x == 0) tops[0] = first;
+        __syncthreads();
+        first = (float)tops[0];
+      }
+      pivot = (double)first;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = 8 * (R::lane() + TR * i);
+      if (c >= D) break;
+      if (a.pre == NORM_NONE) continue;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (TAIL && c + j >= D) break;
+        const double d = (double)h[i][j] - pivot;
+        sum += d;
+        sq = fma(d, d, sq);
+      }
+    }
+    if (a.pre != NORM_NONE) row_sums<TR>(sum, sq, part + R::WAVES);
+    const Norm<V> norm(a.pre, pivot, sum, sq, D, a.eps);
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
       if (c >= D) break;
-      float scale[8], shift[8];
-      if (a.scale) load8<TAIL>(a.scale, c, D, scale);
-      if (a.shift) load8<TAIL>(a.shift, c, D, shift);
+      if constexpr (!EARLY) {
+        load8_or<TAIL>(a.scale, 0.f, c, D, scale);
+        load8_or<TAIL>(a.shift, 0.f, c, D, shift);
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (TAIL && c + j >= D) break;
-        V w = ((V)h[i][j] - mean) * rstd;
-        if (a.scale) w *= (V)1 + (V)scale[j];
-        if (a.shift) w += (V)shift[j];
-        v[i][j] = w;
+        v[i][j] = fma(norm(h[i][j]), (V)1 + (V)scale[j], (V)shift[j]);
         if constexpr (OUT == SEAM_I8) {
-          top = fmax(top, fabs(w));
-          bad |= w != w;   // the maximum leaves NaN out
+          top = fmax(top, fabs(v[i][j]));
+          bad |= v[i][j] != v[i][j];   // the maximum leaves NaN out
         }
       }
       if constexpr (OUT == SEAM_ACT) store8<TAIL>((T *)a.out + row * D, c, D, v[i]);
     }
     if constexpr (OUT == SEAM_I8) {
       top = bad ? (double)INFINITY : top;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) top = fmax(top, __shfl_xor(top, o, 64));
+      top = reduced<R::LANES>(top, [](double p, double q) { return fmax(p, q); });
       if constexpr (R::WAVES > 1) {
         if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < R::WAVES; ++w) top = fmax(top, tops[w]);
       }
-      float s = fmaxf((float)(top / 127.0), kTinyScale);
+      const float s = fmaxf((float)(top / 127.0), kTinyScale);
       bad = !(s < INFINITY);
       const double inv = 1.0 / (double)s;
       if (R::lane() == 0) a.q_scale[row] = bad ? __builtin_nanf("") : s;
@@ -392,9 +484,12 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
       for (int i = 0; i < NV; ++i) {
         const int c = 8 * (R::lane() + TR * i);
         if (c >= D) break;
-        int code[8];
+        uint32_t code[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) code[j] = bad || (TAIL && c + j >= D) ? 0 : (int)__builtin_rint(v[i][j] * inv);
+        for (int j = 0; j < 8; ++j) {   // the nearest integer is what the low bits hold
+          const double r = fma(v[i][j], inv, 6755399441055744.0);   // 1.5 2^52
+          code[j] = bad || (TAIL && c + j >= D) ? 0u : (uint32_t)__builtin_bit_cast(uint64_t, r);
+        }
         store_codes<TAIL>(a.q + row * D, c, D, code);
       }
     }
@@ -403,20 +498,26 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 
 template <typename T, int TR, int NV, int OUT>
 static hipError_t norm_rows(int M, const SeamArgs &a, hipStream_t s) {
-  const unsigned blocks = TR == 64 ? (unsigned)(((int64_t)M + 3) / 4) : (unsigned)M;
-  if (a.D % 8) hipLaunchKernelGGL((k_norm_residual<T, TR, NV, true, OUT>), dim3(blocks), dim3(Row<TR>::BLOCK), 0, s, M, a);
-  else hipLaunchKernelGGL((k_norm_residual<T, TR, NV, false, OUT>), dim3(blocks), dim3(Row<TR>::BLOCK), 0, s, M, a);
+  const dim3 grid(Row<TR>::blocks(M)), block(Row<TR>::BLOCK);
+  // a stream of 64 MiB and more is stored non-temporally: nothing reads it soon ((24960, 1536) to codes 105 -> 101 us,
+  // (16384, 5120) to activations 224 -> 219); a smaller one the next kernel may still find in the caches
+  const bool nt = a.x_out && (size_t)M * a.D * 4 >= (size_t)64 << 20;
+  if (a.D % 8) hipLaunchKernelGGL((k_norm_residual<T, TR, NV, true, OUT, false>), grid, block, 0, s, M, a);
+  else if (nt) hipLaunchKernelGGL((k_norm_residual<T, TR, NV, false, OUT, true>), grid, block, 0, s, M, a);
+  else hipLaunchKernelGGL((k_norm_residual<T, TR, NV, false, OUT, false>), grid, block, 0, s, M, a);
   return hipGetLastError();
 }
 
 template <typename T, int OUT>
 static hipError_t norm_rows_of(int M, const SeamArgs &a, hipStream_t s) {
   const int pieces = (a.D + 7) / 8;
-  if (pieces <= 64) return norm_rows<T, 64, 1, OUT>(M, a, s);
-  if (pieces <= 128) return norm_rows<T, 64, 2, OUT>(M, a, s);
-  if (pieces <= 192) return norm_rows<T, 64, 3, OUT>(M, a, s);
-  if (pieces <= 512) return norm_rows<T, 256, 2, OUT>(M, a, s);
-  return norm_rows<T, 256, 3, OUT>(M, a, s);
+#define FB_ROWS(TR, NV) if (pieces <= TR * NV) return norm_rows<T, TR, NV, OUT>(M, a, s);
+  FB_ROWS(16, 1) FB_ROWS(32, 1) FB_ROWS(64, 1)   // several rows a wave: 24960 x 64 10 us, on whole waves 34
+  // few rows wait on a row's own chain, which more threads shorten: 390 x 1536 5.4 us and 7.3, but 24960 x 1536 105 and 99
+  if (M <= 2 * cu_count()) { FB_ROWS(256, 1) }
+  FB_ROWS(64, 2) FB_ROWS(64, 3) FB_ROWS(128, 2) FB_ROWS(192, 2) FB_ROWS(256, 2) FB_ROWS(256, 3)
+#undef FB_ROWS
+  return hipErrorInvalidValue;
 }
 
 hipError_t launch_norm_residual(ActType t, int M, const SeamArgs &a, hipStream_t s) {
