@@ -1,6 +1,7 @@
 // Linear layers on 8-bit integers: C[m][n] = a_scale[m] w_scale[n] sum_k A[m][k] W[n][k] with the epilogues of the other
 // linear layers.  The sum is exact in 32 bits (K <= 65536: at most 2^14 2^16 = 2^30), so every tiling and every order of
 // K gives the same bits, and the choice of kernel changes no output.
+#include <atomic>
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
@@ -637,12 +638,19 @@ hipError_t launch_split(int M, int N, int K, const I8Args &g, const EpiArgs &e, 
 template <int EPI, typename TO, int WTA, int WT, int NST>
 hipError_t launch_ring(int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s) {
   constexpr int BM = 32 * WTA, BN = 64 * WT, LDS = NST * (BM + BN) * ring::BK;
-  auto kern = k_linear_i8_ring<EPI, TO, WTA, WT, NST, 0>;
   const size_t written = (size_t)M * N * (EPI == EPI_STORE || EPI == EPI_GELU ? sizeof(TO) : EPI == EPI_RESIDUAL && e.cache ? 8 : 4);
-  if (written >= kNTBytes) kern = k_linear_i8_ring<EPI, TO, WTA, WT, NST, kStoreNT>;
-  // on every launch: the attribute is one of the function on the current device
-  const hipError_t err = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  const bool nt = written >= kNTBytes;
+  const auto kern = nt ? k_linear_i8_ring<EPI, TO, WTA, WT, NST, kStoreNT> : k_linear_i8_ring<EPI, TO, WTA, WT, NST, 0>;
+  static std::atomic<uint64_t> ready[2];   // devices on which the function has its LDS
+  int dev = 0;
+  hipError_t err = hipGetDevice(&dev);
   if (err != hipSuccess) return err;
+  const uint64_t bit = (uint64_t)1 << (dev & 63);
+  if (dev > 63 || !(ready[nt] & bit)) {
+    err = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    if (err != hipSuccess) return err;
+    ready[nt] |= bit;
+  }
   const int MT = (M + BM - 1) / BM, NT = (N + BN - 1) / BN;
   // row blocks of a tile group: (24960, 1536, 8960) 409 us at 1, 419 at 4, 432 at 8; (16384, 13824, 5120) 985 at 2, 1024 at
   // 1, 1037 at 4; (24960, 4608, 1536) 173 at 8, 183 at 4, 200 at 2; (24960, 8960, 1536) 394 at 4, 397 at 8, 429 at 1

@@ -530,109 +530,122 @@ def flashbon_op_unpatch_sde(n, C, H, W, p, v, z, t_cur, t_next, a, seed, step, r
 
 # 8-bit layers.  Sizes are given, as in the calls above; every tensor is checked against them.
 
+_torch = None
+
+
+def _with_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _act(dtype):
-    import torch
+    torch = _with_torch()
     if dtype not in (FP32, BF16):
         raise ValueError("dtype must be FP32 or BF16")
     return torch.bfloat16 if dtype == BF16 else torch.float32
 
 
-def _check_sized(dtype, count: int, device: Optional[int], required: bool, **tensors) -> None:
-    """Every tensor: of ``dtype``, contiguous, of at least ``count`` elements, on the GPU ``device`` (None: anywhere)."""
-    for name, t in tensors.items():
+def _current_device(require_device: bool) -> Optional[int]:
+    return _with_torch().cuda.current_device() if require_device else None
+
+
+def _raw_stream(stream, device: int) -> int:
+    """``stream``, or torch's current one on ``device`` (its address alone: a tenth of the time of a Stream object)."""
+    return int(stream) if stream is not None else _torch._C._cuda_getCurrentRawStream(device)
+
+
+def _pointers(device: Optional[int], *wanted) -> list:
+    """Addresses of the tensors in ``wanted``, (name, tensor or None, dtype, elements, required) each: of that dtype,
+    contiguous, of at least so many elements, on the GPU ``device`` (None: anywhere)."""
+    found = []
+    for name, t, dtype, count, required in wanted:
         if t is None:
             if required:
                 raise ValueError(f"{name} is required")
+            found.append(None)
             continue
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
         if t.numel() < count:
             raise ValueError(f"{name} holds {t.numel()} elements, needs {count}")
-        if device is not None and (not t.is_cuda or t.device.index != device):
+        if device is not None and t.get_device() != device:
             raise ValueError(f"{name} must be on the current device (cuda:{device}), got {t.device}")
+        found.append(t.data_ptr())
+    return found
 
 
-def _current_device(require_device: bool) -> Optional[int]:
-    import torch
-    return torch.cuda.current_device() if require_device else None
-
-
-def validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale, *, require_device: bool = True) -> None:
-    """Raise ValueError unless the tensors are what flashbon_op_quant_rows reads and writes.  ``x`` may be a view of
-    wider rows: 2-D with a unit column stride."""
-    import torch
-    device = _current_device(require_device)
+def validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale, *, require_device: bool = True) -> list:
+    """Raise ValueError unless the tensors are what flashbon_op_quant_rows reads and writes; their addresses.  ``x`` may
+    be a view of wider rows: 2-D with a unit column stride."""
+    act, device = _act(dtype), _current_device(require_device)
     if M < 1 or K < 1 or x_row_stride < K:
         raise ValueError(f"need M, K >= 1 and a row stride of at least K, got {M}, {K}, {x_row_stride}")
-    if x.dtype != _act(dtype):
-        raise ValueError(f"x must be {_act(dtype)}, got {x.dtype}")
+    if x.dtype is not act:
+        raise ValueError(f"x must be {act}, got {x.dtype}")
     if x.is_contiguous():
         if x.numel() < (M - 1) * x_row_stride + K:
             raise ValueError(f"x holds {x.numel()} elements, {M} rows of {K} at stride {x_row_stride} need more")
     elif x.dim() != 2 or x.stride(1) != 1 or x.stride(0) != x_row_stride or x.shape[0] < M or x.shape[1] < K:
         raise ValueError(f"x must be contiguous or [{M}, {K}] with strides ({x_row_stride}, 1), got "
                          f"{tuple(x.shape)} with {x.stride()}")
-    if device is not None and (not x.is_cuda or x.device.index != device):
+    if device is not None and x.get_device() != device:
         raise ValueError(f"x must be on the current device (cuda:{device}), got {x.device}")
-    _check_sized(torch.int8, M * K, device, True, q=q)
-    _check_sized(torch.float32, M, device, True, scale=scale)
+    return [x.data_ptr()] + _pointers(device, ("q", q, _torch.int8, M * K, True), ("scale", scale, _torch.float32, M, True))
 
 
 def flashbon_op_quant_rows(dtype, M, K, x, q, scale, x_row_stride=None, stream=None):
     """Rows x [M][K] to int8 codes q and one scale a row; ``x_row_stride`` in elements (None: a matrix's own, else K)."""
     if x_row_stride is None:
         x_row_stride = int(x.stride(0)) if x.dim() == 2 and x.shape[0] > 1 else K
-    validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale)
-    _check(load().flashbon_op_quant_rows(dtype, M, K, _ptr(x), x_row_stride, _ptr(q), _ptr(scale), _stream(stream)),
+    px, pq, ps = validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale)
+    _check(load().flashbon_op_quant_rows(dtype, M, K, px, x_row_stride, pq, ps, _raw_stream(stream, x.get_device())),
            "flashbon_op_quant_rows")
 
 
 def validate_linear_i8(dtype, M, N, K, A, a_scale, W, w_scale, bias, epilogue, out, gate=None, residual_in=None,
-                       cache_out=None, *, require_device: bool = True) -> None:
-    """Raise ValueError unless the tensors are what flashbon_op_linear_i8 reads and writes."""
-    import torch
-    f32, device = torch.float32, _current_device(require_device)
-    _check_sized(torch.int8, M * K, device, True, A=A)
-    _check_sized(torch.int8, N * K, device, True, W=W)
-    _check_sized(f32, M, device, True, a_scale=a_scale)
-    _check_sized(f32, N, device, True, w_scale=w_scale)
-    _check_sized(f32, N, device, False, bias=bias)
-    act = _act(dtype)
-    _check_sized(act if epilogue in (EPI_STORE, EPI_GELU) else f32, M * N, device, True, out=out)
+                       cache_out=None, *, require_device: bool = True) -> list:
+    """Raise ValueError unless the tensors are what flashbon_op_linear_i8 reads and writes; their addresses."""
+    act, device = _act(dtype), _current_device(require_device)
+    i8, f32 = _torch.int8, _torch.float32
+    found = _pointers(device, ("A", A, i8, M * K, True), ("a_scale", a_scale, f32, M, True), ("W", W, i8, N * K, True),
+                      ("w_scale", w_scale, f32, N, True), ("bias", bias, f32, N, False),
+                      ("out", out, act if epilogue == EPI_STORE or epilogue == EPI_GELU else f32, M * N, True))
     if epilogue == EPI_RESIDUAL:
-        _check_sized(f32, N, device, False, gate=gate)
-        _check_sized(f32, M * N, device, False, residual_in=residual_in, cache_out=cache_out)
+        return found + _pointers(device, ("gate", gate, f32, N, False), ("residual_in", residual_in, f32, M * N, False),
+                                 ("cache_out", cache_out, f32, M * N, False))
+    return found + [None, None, None]
 
 
 def flashbon_op_linear_i8(dtype, M, N, K, A, a_scale, W, w_scale, bias, epilogue, out, gate=None, residual_in=None,
                           cache_out=None, stream=None):
     """Linear layer on int8 rows A [M][K] and weights W [N][K] with a scale a token and an output channel."""
-    validate_linear_i8(dtype, M, N, K, A, a_scale, W, w_scale, bias, epilogue, out, gate, residual_in, cache_out)
-    _check(load().flashbon_op_linear_i8(dtype, M, N, K, _ptr(A), _ptr(a_scale), _ptr(W), _ptr(w_scale), _ptr(bias),
-                                        epilogue, _ptr(out), _ptr(gate), _ptr(residual_in), _ptr(cache_out),
-                                        _stream(stream)), "flashbon_op_linear_i8")
+    pa, psa, pw, psw, pb, po, pg, pr, pc = validate_linear_i8(dtype, M, N, K, A, a_scale, W, w_scale, bias, epilogue, out,
+                                                              gate, residual_in, cache_out)
+    _check(load().flashbon_op_linear_i8(dtype, M, N, K, pa, psa, pw, psw, pb, epilogue, po, pg, pr, pc,
+                                        _raw_stream(stream, A.get_device())), "flashbon_op_linear_i8")
 
 
 def validate_norm_residual(dtype, M, D, x, y=None, out=None, q=None, q_scale=None, x_out=None, post_gain=None, gate=None,
-                           shift=None, scale=None, *, require_device: bool = True) -> None:
-    """Raise ValueError unless the tensors are what flashbon_op_norm_residual reads and writes."""
-    import torch
-    f32, device, act = torch.float32, _current_device(require_device), _act(dtype)
-    _check_sized(f32, M * D, device, True, x=x)
-    _check_sized(f32, M * D, device, False, x_out=x_out)
-    _check_sized(act, M * D, device, False, y=y, out=out)
-    _check_sized(f32, D, device, False, post_gain=post_gain, gate=gate, shift=shift, scale=scale)
-    _check_sized(torch.int8, M * D, device, False, q=q)
-    _check_sized(f32, M, device, False, q_scale=q_scale)
+                           shift=None, scale=None, *, require_device: bool = True) -> list:
+    """Raise ValueError unless the tensors are what flashbon_op_norm_residual reads and writes; their addresses."""
+    act, device = _act(dtype), _current_device(require_device)
+    f32 = _torch.float32
+    return _pointers(device, ("x", x, f32, M * D, True), ("y", y, act, M * D, False), ("post_gain", post_gain, f32, D, False),
+                     ("gate", gate, f32, D, False), ("x_out", x_out, f32, M * D, False), ("shift", shift, f32, D, False),
+                     ("scale", scale, f32, D, False), ("out", out, act, M * D, False), ("q", q, _torch.int8, M * D, False),
+                     ("q_scale", q_scale, f32, M, False))
 
 
 def flashbon_op_norm_residual(dtype, M, D, eps, x, y=None, *, alpha=1.0, post_norm=NORM_NONE, post_gain=None, gate=None,
                               x_out=None, pre_norm=NORM_LAYER, shift=None, scale=None, out=None, q=None, q_scale=None,
                               stream=None):
     """h = alpha x + gate (post_norm(y) post_gain) -> x_out; pre_norm(h) (1 + scale) + shift -> out, or q and q_scale."""
-    validate_norm_residual(dtype, M, D, x, y, out, q, q_scale, x_out, post_gain, gate, shift, scale)
-    _check(load().flashbon_op_norm_residual(dtype, M, D, eps, _ptr(x), alpha, _ptr(y), post_norm, _ptr(post_gain),
-                                            _ptr(gate), _ptr(x_out), pre_norm, _ptr(shift), _ptr(scale), _ptr(out),
-                                            _ptr(q), _ptr(q_scale), _stream(stream)), "flashbon_op_norm_residual")
+    px, py, pp, pg, ph, psh, psc, po, pq, pqs = validate_norm_residual(dtype, M, D, x, y, out, q, q_scale, x_out, post_gain,
+                                                                       gate, shift, scale)
+    _check(load().flashbon_op_norm_residual(dtype, M, D, eps, px, alpha, py, post_norm, pp, pg, ph, pre_norm, psh, psc, po,
+                                            pq, pqs, _raw_stream(stream, x.get_device())), "flashbon_op_norm_residual")

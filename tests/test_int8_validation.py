@@ -109,4 +109,4 @@ def test_binding_refuses_norm(kw):
 
 def test_binding_wants_the_current_device():
     with pytest.raises(ValueError):
-        fb._check_sized(F, 4, 0, True, x=_t(4, F))
+        fb._pointers(0, ("x", _t(4, F), F, 4, True))
