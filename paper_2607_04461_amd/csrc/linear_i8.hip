@@ -1,8 +1,10 @@
 // Linear layers on 8-bit integers: C[m][n] = a_scale[m] w_scale[n] sum_k A[m][k] W[n][k] with the epilogues of the other
 // linear layers.  The sum is exact in 32 bits (K <= 65536: at most 2^14 2^16 = 2^30), so every tiling and every order of
 // K gives the same bits, and the choice of kernel changes no output.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <type_traits>
@@ -33,8 +35,27 @@ __device__ __forceinline__ void put(const EpiArgs &e, int64_t at, float v, float
   }
 }
 
-// 16 bytes on any address.
-__device__ __forceinline__ i32x4 whole_piece(const int8_t *p) { return __builtin_bit_cast(i32x4, *reinterpret_cast<const u32x4u *>(p)); }
+// The workgroup's barrier for LDS accesses of the waves, not for loads that are still on their way (__syncthreads waits for
+// those too).
+__device__ __forceinline__ void barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// 16 bytes on any address.  BYTES: where it may be off 4 bytes, which a load pays for with three to five times its time
+// (20 x 24 x 11073 28 us, x 11076 8.8): from the five words around them, each of which holds one of the bytes at least.
+template <bool BYTES = false> __device__ __forceinline__ i32x4 whole_piece(const int8_t *p) {
+  if constexpr (!BYTES) return __builtin_bit_cast(i32x4, *reinterpret_cast<const u32x4u *>(p));
+  typedef uint32_t words __attribute__((ext_vector_type(4), aligned(4)));
+  const uintptr_t at = (uintptr_t)p;
+  const u32x4 w = *reinterpret_cast<const words *>(at & ~(uintptr_t)3);
+  const uint32_t last = *reinterpret_cast<const uint32_t *>((at + 15) & ~(uintptr_t)3), by = (uint32_t)at & 3;
+  // an address on 4 bytes has `last` in w already, and shifts by nothing
+  return i32x4{(int)__builtin_amdgcn_alignbyte(w[1], w[0], by), (int)__builtin_amdgcn_alignbyte(w[2], w[1], by),
+               (int)__builtin_amdgcn_alignbyte(w[3], w[2], by), (int)__builtin_amdgcn_alignbyte(last, w[3], by)};
+}
 // Bytes k .. k + 15 of a row of K >= 16, zero past its end, from the 16 bytes at min(k, K - 16).
 __device__ __forceinline__ i32x4 cut_piece(i32x4 v, int k, int K) {
   typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
@@ -59,7 +80,7 @@ __device__ __forceinline__ i32x4 piece(const int8_t *p, int k, int K) {
 // into the products' registers: for layers whose larger tiles would leave most CUs idle, of any size and alignment.  A
 // piece of U of a wave's K, all loaded before their products, is on its way at once.  The waves' sums are added in LDS.
 // Bound by reading W once, below a few us by latency.
-template <int EPI, typename TO, int MF, int NF, int WAVES, int U>
+template <int EPI, typename TO, int MF, int NF, int WAVES, int U, bool BYTES>
 __global__ __launch_bounds__(64 * WAVES) void k_linear_i8_split(int M, int N, int K, I8Args g, EpiArgs e) {
   constexpr int T = 64 * WAVES;
   __shared__ __attribute__((aligned(16))) int sums[WAVES][MF * NF * 256];
@@ -93,9 +114,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_linear_i8_split(int M, int N, in
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int i = 0; i < NF; ++i) fw[u][h][i] = whole_piece(wr[i] + k + 64 * h);
+        for (int i = 0; i < NF; ++i) fw[u][h][i] = whole_piece<BYTES>(wr[i] + k + 64 * h);
 #pragma unroll
-        for (int j = 0; j < MF; ++j) fa[u][h][j] = whole_piece(ar[j] + k + 64 * h);
+        for (int j = 0; j < MF; ++j) fa[u][h][j] = whole_piece<BYTES>(ar[j] + k + 64 * h);
       }
     }
     __builtin_amdgcn_sched_barrier(0);   // no load sinks to its use
@@ -174,15 +195,16 @@ __global__ __launch_bounds__(256, 2) void k_linear_i8_any(int M, int N, int K, I
 #pragma unroll
     for (int x = 0; x < PER; ++x) r[decltype(S)::value][x] = whole_piece((x < PER / 2 ? A0 : W0) + row[x] + k);
   };
-  auto store = [&](auto S, int kt) {
+  auto store = [&](auto S) {
     constexpr int st = decltype(S)::value;
-    char *const to = smem_any + st * STAGE;
-    if ((kt + 1) * BK > K) {
 #pragma unroll
-      for (int x = 0; x < PER; ++x) r[st][x] = cut_piece(r[st][x], kt * BK + 16 * lc, K);
-    }
+    for (int x = 0; x < PER; ++x) *reinterpret_cast<i32x4 *>(smem_any + st * STAGE + at(lr + 32 * x, lc)) = r[st][x];
+  };
+  auto store_last = [&](auto S, int kt) {   // the K tile that K ends in
+    constexpr int st = decltype(S)::value;
 #pragma unroll
-    for (int x = 0; x < PER; ++x) *reinterpret_cast<i32x4 *>(to + at(lr + 32 * x, lc)) = r[st][x];
+    for (int x = 0; x < PER; ++x) r[st][x] = cut_piece(r[st][x], kt * BK + 16 * lc, K);
+    store(S);
   };
   i32x4 acc[4][4] = {};
   auto products = [&](auto S) {
@@ -206,21 +228,35 @@ __global__ __launch_bounds__(256, 2) void k_linear_i8_any(int M, int N, int K, I
   const int KT = (K + BK - 1) / BK;
   load(S0{}, 0);
   load(S1{}, 1);
-  store(S0{}, 0);
-  __syncthreads();
-  for (int kt = 0; kt < KT; kt += 2) {
+  if (KT > 1) store(S0{});
+  else store_last(S0{}, 0);
+  barrier();
+  int kt = 0;
+  for (; kt + 3 < KT; kt += 2) {
     load(S0{}, kt + 2);
     products(S0{});
-    if (kt + 1 >= KT) break;
-    store(S1{}, kt + 1);
-    __syncthreads();
+    store(S1{});
+    barrier();
     load(S1{}, kt + 3);
     products(S1{});
-    if (kt + 2 >= KT) break;
-    store(S0{}, kt + 2);
-    __syncthreads();
+    store(S0{});
+    barrier();
   }
-  __syncthreads();   // every wave has read its last fragments
+  if (KT - kt == 3) load(S0{}, kt + 2);
+  products(S0{});
+  if (KT - kt == 2) {
+    store_last(S1{}, kt + 1);
+    barrier();
+    products(S1{});
+  } else if (KT - kt == 3) {
+    store(S1{});
+    barrier();
+    products(S1{});
+    store_last(S0{}, kt + 2);
+    barrier();
+    products(S0{});
+  }
+  barrier();   // every wave has read its last fragments
   // The wave's 64x64 sums through the freed stages, so that a store covers 64 columns of a row; 16-byte piece c of row r
   // at c ^ (r & 15).
   int *wl = reinterpret_cast<int *>(smem_any) + wave * (64 * 64);
@@ -298,14 +334,6 @@ template <int PER> __device__ __forceinline__ void wait_tiles(int n) {   // but 
     default: wait_loads<2 * PER>(); break;
   }
 }
-// The workgroup's barrier for LDS accesses of the waves, not for loads that are still on their way into LDS.
-__device__ __forceinline__ void barrier() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
 // Workgroup -> tile: contiguous ranges of tiles for each of the 8 XCDs (dispatch is round-robin over them), in groups of
 // `group` row blocks that sweep all column tiles, so that an XCD's workgroups share rows of A and W in its L2.
 __device__ __forceinline__ void tile_of(int bid, int MT, int NT, int group, int &mt, int &nt) {
@@ -556,6 +584,22 @@ __global__ __launch_bounds__(512, 1) void k_linear_i8_ring(int M, int N, int K, 
   ring::tile<EPI, TO, WTA, WT, NST, POL>(M, N, K, g, e, 32 * WTA * mt, 64 * WT * nt, smem_ring);
 }
 
+// The same on MT row blocks of two heights, `tall` of 32 WTA rows and the others of 32 (WTA - 1), spread evenly over the
+// block index (block i is tall where floor((i + 1) tall / MT) > floor(i tall / MT)), 256 columns wide: so that a launch fills
+// whole rounds of the chip.
+template <int EPI, typename TO, int WTA, int POL>
+__global__ __launch_bounds__(512, 1) void k_linear_i8_mix(int M, int N, int K, I8Args g, EpiArgs e, int MT, int NT, int group,
+                                                          int tall) {
+  extern __shared__ __attribute__((aligned(16))) char smem_mix[];
+  int mt, nt;
+  ring::tile_of(blockIdx.x, MT, NT, group, mt, nt);
+  const int before = (int)((int64_t)mt * tall / MT), upto = (int)((int64_t)(mt + 1) * tall / MT);
+  const int m0 = 32 * ((WTA - 1) * mt + before), n0 = 256 * nt;
+  if (m0 >= M) return;   // a forced plan of more blocks than M has
+  if (upto > before) ring::tile<EPI, TO, WTA, 4, 2, POL>(M, N, K, g, e, m0, n0, smem_mix);
+  else ring::tile<EPI, TO, WTA - 1, 4, 2, POL>(M, N, K, g, e, m0, n0, smem_mix);
+}
+
 // ------------------------------------------------------------------------------------------- dispatch
 namespace {
 
@@ -574,40 +618,54 @@ constexpr int kRowsPerLaunch = 1 << 15;   // a grid within 2^32 threads at N <= 
 //     (24960, 1536, 1536) residual 148, 140, 136, 149; (24960, 1536, 8960) residual 394, 381, 410, 480; (4680, 1536,
 //     8960) 117, 75, 81, 97; (1560, 4608, 1536) 22, 17, 16, 18.  What fits one round of 128x128 tiles waits on the latency
 //     of each K tile, which a third stage hides best: (1560, 1536, 8960) 84, 54, 50, 34; (1560, 1536, 1536) 26, 17, 15, 13.
-//   * k_linear_i8_split by the bytes a CU reads, 25 a ns, 15 on rows off 16 bytes, which take several
-//     times the address work: (1, 8960, 1536) 4.9 against 8.6 on 128x128 tiles, (16, 1536, 8960) 9.8 and 27, (390, 256,
-//     256) 2.5 and 4.0, (64, 5120, 5120) 17.3 and 17.3, (512, 1536, 4096) 25 and 15.
-//   * k_linear_i8_any for the larger layers off 16 bytes: (3000, 2501, 3001) 56 (64x32 split 330), (777, 1111, 999) 17
-//     and 15, (389, 701, 253) 11 and 5.6.
-enum Kernel { SPLIT11, SPLIT21, SPLIT22, SPLIT42, ANY, RING_256x256, RING_128x256, RING_128x128_TWO, RING_128x128 };
+//   * k_linear_i8_split by the bytes a CU reads, 25 a ns, 16 on rows off 4 bytes: (1, 8960, 1536) 4.9 against 8.6 on
+//     128x128 tiles, (16, 1536, 8960) 9.8 and 27, (390, 256, 256) 2.5 and 4.0, (64, 5120, 5120) 17.3 and 17.3, (512, 1536,
+//     4096) 25 and 15.
+//   * k_linear_i8_any for the larger layers off 16 bytes: (3000, 2501, 3001) 52 (64x32 split 176), (777, 1111, 999) 16
+//     and 12, (389, 701, 253) 10 and 5.6, (5000, 333, 2222) 24 and 40.
+enum Kernel { SPLIT11, SPLIT21, SPLIT22, SPLIT42, ANY, RING_256x256, RING_128x256, RING_128x128_TWO, RING_128x128, MIX };
+struct Plan {
+  Kernel kernel;
+  int wta = 0, blocks = 0, tall = 0;   // MIX
+};
 constexpr const char *kNames[] = {"split:16x16", "split:32x16", "split:32x32", "split:64x32", "any", "256x256", "128x256",
                                   "128x128:two", "128x128"};
 
-// aligned: what the ring kernels take.
-Kernel pick(int M, int N, int K, bool aligned, int epi) {
+// A round of 32 w rows, of one of 256.
+constexpr double kHeight[9] = {0, 0, 0, 0, 0, 0.75, 0.82, 0.9, 1.0};
+// Whether rows start off 4 bytes.
+bool off_words(const I8Args &g, int K) { return ((uintptr_t)g.A | (uintptr_t)g.W | (uintptr_t)K) % 4; }
+
+// aligned: what the ring kernels take; words: rows on 4 bytes.
+Plan pick(int M, int N, int K, bool aligned, bool words, int epi) {
   // FLASHBON_I8_TILE (tests and tuning) forces a kernel by its name; one that does not take the layer is passed over
-  if (const char *force = getenv("FLASHBON_I8_TILE"))
+  // ("mix:<w>:<blocks>:<tall>": two heights of 32 w and 32 (w - 1) rows, w in 6..8, covering M)
+  if (const char *force = getenv("FLASHBON_I8_TILE")) {
     for (int k = 0; k < 9; ++k)
-      if (!strcmp(force, kNames[k]) && (k <= SPLIT42 || (k == ANY ? K >= 16 : aligned))) return (Kernel)k;
+      if (!strcmp(force, kNames[k]) && (k <= SPLIT42 || (k == ANY ? K >= 16 : aligned))) return {(Kernel)k};
+    Plan p = {MIX};
+    if (aligned && sscanf(force, "mix:%d:%d:%d", &p.wta, &p.blocks, &p.tall) == 3 && p.wta >= 6 && p.wta <= 8 && p.tall >= 0 &&
+        p.tall <= p.blocks && p.blocks <= M && 32 * ((int64_t)(p.wta - 1) * p.blocks + p.tall) >= M)
+      return p;
+  }
   const double cus = cu_count(), kt = (K + 127) / 128;
-  Kernel best = SPLIT11;
+  Plan best = {SPLIT11};
   double t_best = 1e30;
   // rounds of `slots` workgroups of bm x bn outputs, each `per_round`
   auto offer = [&](Kernel k, int bm, int bn, double slots, double once, double per_round) {
     const double tiles = (double)((M + bm - 1) / bm) * ((N + bn - 1) / bn), t = once + ceil(tiles / slots) * per_round;
     if (t < t_best) {
       t_best = t;
-      best = k;
+      best = {k};
     }
-    return tiles;
   };
-  const double rate = aligned ? 25e3 : 15e3;   // bytes a us and CU
+  const double rate = words ? 25e3 : 16e3;   // bytes a us and CU
   offer(SPLIT11, 16, 16, cus, 2.1, (16 + fmin(16, M)) * K / rate);
   offer(SPLIT21, 32, 16, cus, 2.1, (16 + fmin(32, M)) * K / rate);
   offer(SPLIT22, 32, 32, cus, 2.1, (32 + fmin(32, M)) * K / rate);
   offer(SPLIT42, 64, 32, cus, 2.1, (32 + fmin(64, M)) * K / rate);
   if (!aligned) {
-    if (K >= 16) offer(ANY, 128, 128, 2 * cus, 5.0, 1.6 * kt);
+    if (K >= 16) offer(ANY, 128, 128, 2 * cus, 5.0, 1.2 * kt);
     return best;
   }
   if ((double)((M + 127) / 128) * ((N + 127) / 128) <= cus) {
@@ -618,6 +676,20 @@ Kernel pick(int M, int N, int K, bool aligned, int epi) {
   offer(RING_256x256, 256, 256, cus, 0, 1.75 * kt + (res ? 27 : 9));
   offer(RING_128x256, 128, 256, cus, 0, 1.03 * kt + (res ? 15 : 6));
   offer(RING_128x128_TWO, 128, 128, 2 * cus, 0, 1.2 * kt + (res ? 12 : 5.5));
+  // as many blocks of two heights as fill whole rounds
+  const int NT = (N + 255) / 256;
+  for (int w = 8; w >= 6; --w) {
+    const int lo = 32 * (w - 1), least = (M + lo + 31) / (lo + 32), most = (M + lo - 1) / lo;
+    for (int r = (int)((least * NT + cus - 1) / cus); r * cus < (double)(most + 1) * NT; ++r) {
+      const int blocks = std::min(most, (int)(r * cus / NT)), tall = std::max(0, (M - lo * blocks + 31) / 32);
+      if (blocks < least || tall > blocks) continue;
+      const double t = r * ((1.75 * kt + (res ? 27 : 9)) * (kHeight[w - 1] + (kHeight[w] - kHeight[w - 1]) * tall / blocks));
+      if (t < 0.98 * t_best) {
+        t_best = t;
+        best = {MIX, w, blocks, tall};
+      }
+    }
+  }
   return best;
 }
 
@@ -630,32 +702,57 @@ hipError_t launch_any(int M, int N, int K, const I8Args &g, const EpiArgs &e, hi
 
 template <int EPI, typename TO, int MF, int NF, int U>
 hipError_t launch_split(int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s) {
-  hipLaunchKernelGGL((k_linear_i8_split<EPI, TO, MF, NF, 8, U>), dim3((N + 16 * NF - 1) / (16 * NF), (M + 16 * MF - 1) / (16 * MF)),
-                     dim3(512), 0, s, M, N, K, g, e);
+  const dim3 grid((N + 16 * NF - 1) / (16 * NF), (M + 16 * MF - 1) / (16 * MF));
+  if (off_words(g, K))
+    hipLaunchKernelGGL((k_linear_i8_split<EPI, TO, MF, NF, 8, U, true>), grid, dim3(512), 0, s, M, N, K, g, e);
+  else
+    hipLaunchKernelGGL((k_linear_i8_split<EPI, TO, MF, NF, 8, U, false>), grid, dim3(512), 0, s, M, N, K, g, e);
+  return hipGetLastError();
+}
+
+// Gives a kernel its LDS on the current device, once; ready: the devices that have it.
+template <typename F> hipError_t with_lds(F kern, int lds, std::atomic<uint64_t> &ready) {
+  int dev = 0;
+  hipError_t err = hipGetDevice(&dev);
+  if (err != hipSuccess) return err;
+  const uint64_t bit = (uint64_t)1 << (dev & 63);
+  if (dev <= 63 && (ready & bit)) return hipSuccess;
+  err = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (err == hipSuccess) ready |= bit;
+  return err;
+}
+
+template <int EPI, typename TO> bool stores_past_caches(int M, int N, const EpiArgs &e) {
+  return (size_t)M * N * (EPI == EPI_STORE || EPI == EPI_GELU ? sizeof(TO) : EPI == EPI_RESIDUAL && e.cache ? 8 : 4) >= kNTBytes;
+}
+
+// Row blocks of a tile group: (24960, 1536, 8960) 409 us at 1, 419 at 4, 432 at 8; (16384, 13824, 5120) 985 at 2, 1024 at
+// 1, 1037 at 4; (24960, 4608, 1536) 173 at 8, 183 at 4, 200 at 2; (24960, 8960, 1536) 394 at 4, 397 at 8, 429 at 1.
+int group_of(int N, int K) { return N <= 2048 ? 1 : K >= 4096 ? 2 : 8; }
+
+template <int EPI, typename TO, int WTA>
+hipError_t launch_mix(int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s, const Plan &p) {
+  constexpr int LDS = 2 * (32 * WTA + 256) * ring::BK;
+  const bool nt = stores_past_caches<EPI, TO>(M, N, e);
+  const auto kern = nt ? k_linear_i8_mix<EPI, TO, WTA, kStoreNT> : k_linear_i8_mix<EPI, TO, WTA, 0>;
+  static std::atomic<uint64_t> ready[2];
+  const hipError_t err = with_lds(kern, LDS, ready[nt]);
+  if (err != hipSuccess) return err;
+  const int NT = (N + 255) / 256;
+  hipLaunchKernelGGL(kern, dim3(p.blocks * NT), dim3(512), LDS, s, M, N, K, g, e, p.blocks, NT, group_of(N, K), p.tall);
   return hipGetLastError();
 }
 
 template <int EPI, typename TO, int WTA, int WT, int NST>
 hipError_t launch_ring(int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s) {
   constexpr int BM = 32 * WTA, BN = 64 * WT, LDS = NST * (BM + BN) * ring::BK;
-  const size_t written = (size_t)M * N * (EPI == EPI_STORE || EPI == EPI_GELU ? sizeof(TO) : EPI == EPI_RESIDUAL && e.cache ? 8 : 4);
-  const bool nt = written >= kNTBytes;
+  const bool nt = stores_past_caches<EPI, TO>(M, N, e);
   const auto kern = nt ? k_linear_i8_ring<EPI, TO, WTA, WT, NST, kStoreNT> : k_linear_i8_ring<EPI, TO, WTA, WT, NST, 0>;
-  static std::atomic<uint64_t> ready[2];   // devices on which the function has its LDS
-  int dev = 0;
-  hipError_t err = hipGetDevice(&dev);
+  static std::atomic<uint64_t> ready[2];
+  const hipError_t err = with_lds(kern, LDS, ready[nt]);
   if (err != hipSuccess) return err;
-  const uint64_t bit = (uint64_t)1 << (dev & 63);
-  if (dev > 63 || !(ready[nt] & bit)) {
-    err = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (err != hipSuccess) return err;
-    ready[nt] |= bit;
-  }
   const int MT = (M + BM - 1) / BM, NT = (N + BN - 1) / BN;
-  // row blocks of a tile group: (24960, 1536, 8960) 409 us at 1, 419 at 4, 432 at 8; (16384, 13824, 5120) 985 at 2, 1024 at
-  // 1, 1037 at 4; (24960, 4608, 1536) 173 at 8, 183 at 4, 200 at 2; (24960, 8960, 1536) 394 at 4, 397 at 8, 429 at 1
-  const int group = N <= 2048 ? 1 : K >= 4096 ? 2 : 8;
-  hipLaunchKernelGGL(kern, dim3(MT * NT), dim3(512), LDS, s, M, N, K, g, e, MT, NT, group);
+  hipLaunchKernelGGL(kern, dim3(MT * NT), dim3(512), LDS, s, M, N, K, g, e, MT, NT, group_of(N, K));
   return hipGetLastError();
 }
 
@@ -663,7 +760,8 @@ template <int EPI, typename TO>
 hipError_t launch_rows(int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s) {
   const uintptr_t at = (uintptr_t)g.A | (uintptr_t)g.W | (uintptr_t)g.w_scale | (uintptr_t)e.bias | (uintptr_t)e.out |
                        (uintptr_t)e.res_in | (uintptr_t)e.cache | (uintptr_t)e.gate;
-  switch (pick(M, N, K, K % 16 == 0 && N % 8 == 0 && at % 16 == 0, EPI)) {
+  const Plan p = pick(M, N, K, K % 16 == 0 && N % 8 == 0 && at % 16 == 0, !off_words(g, K), EPI);
+  switch (p.kernel) {
     case SPLIT11: return launch_split<EPI, TO, 1, 1, 2>(M, N, K, g, e, s);
     case SPLIT21: return launch_split<EPI, TO, 2, 1, 2>(M, N, K, g, e, s);
     case SPLIT22: return launch_split<EPI, TO, 2, 2, 2>(M, N, K, g, e, s);
@@ -673,6 +771,10 @@ hipError_t launch_rows(int M, int N, int K, const I8Args &g, const EpiArgs &e, h
     case RING_128x256: return launch_ring<EPI, TO, 4, 4, 3>(M, N, K, g, e, s);
     case RING_128x128: return launch_ring<EPI, TO, 4, 2, 3>(M, N, K, g, e, s);
     case RING_128x128_TWO: return launch_ring<EPI, TO, 4, 2, 2>(M, N, K, g, e, s);
+    case MIX:
+      return p.wta == 8   ? launch_mix<EPI, TO, 8>(M, N, K, g, e, s, p)
+             : p.wta == 7 ? launch_mix<EPI, TO, 7>(M, N, K, g, e, s, p)
+                          : launch_mix<EPI, TO, 6>(M, N, K, g, e, s, p);
   }
   return hipErrorInvalidValue;
 }

@@ -216,6 +216,13 @@ def test_every_kernel_gives_the_same_bits(M, N, K, epi, dtype, monkeypatch):
         got = _linear(M, N, K, dtype, epi)
         first = got if first is None else first
         assert torch.equal(got, first), tile
+    for w in (8, 7, 6):   # row blocks of two heights: all of the one or the other, mixed, and more than the rows need
+        lo = 32 * (w - 1)
+        for blocks in {-(-M // (lo + 32)), -(-M // lo), min(M, -(-M // lo) + 2)}:
+            for tall in {max(0, -(-(M - lo * blocks) // 32)), blocks // 2, blocks}:
+                if 0 <= tall <= blocks and lo * blocks + 32 * tall >= M:
+                    monkeypatch.setenv("FLASHBON_I8_TILE", f"mix:{w}:{blocks}:{tall}")
+                    assert torch.equal(_linear(M, N, K, dtype, epi), first), (w, blocks, tall)
 
 
 @pytest.mark.parametrize("M,N", [(2, 40), (40000, 16)])
