@@ -608,7 +608,9 @@ namespace {
 // 1000 -> 968, (24960, 4608, 1536) 169 -> 159.  Smaller ones stay where the next kernel finds them.
 constexpr int kStoreNT = 2;
 constexpr size_t kNTBytes = (size_t)64 << 20;
-constexpr int kRowsPerLaunch = 1 << 15;   // a grid within 2^32 threads at N <= 2^20
+// Rows of a launch: a grid of 512 threads for 256 outputs, the most a kernel takes, is within 2^32 threads and 2^16 rows
+// of workgroups.
+int rows_per_launch(int N) { return std::min(1 << 15, (1 << 30) / N); }
 
 // Choice of kernel: estimates of a launch's device time in us, whole rounds of workgroups at a time, which stay within
 // 10% of the fastest over the shapes they were fitted to (us below: 256x256, 128x256, 128x128 two a CU, 128x128 with three
@@ -781,7 +783,8 @@ hipError_t launch_rows(int M, int N, int K, const I8Args &g, const EpiArgs &e, h
 
 template <int EPI, typename TO>
 hipError_t launch_epi(int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s) {
-  for (int64_t m = 0; m < M; m += kRowsPerLaunch) {
+  const int most = rows_per_launch(N);
+  for (int64_t m = 0; m < M; m += most) {
     I8Args p = g;
     p.A += m * K;
     p.a_scale += m;
@@ -790,7 +793,7 @@ hipError_t launch_epi(int M, int N, int K, const I8Args &g, const EpiArgs &e, hi
     r.out = (char *)e.out + (size_t)m * e.ldo * es;
     if (r.res_in) r.res_in += m * e.ldo;
     if (r.cache) r.cache += m * e.ldo;
-    const hipError_t err = launch_rows<EPI, TO>((int)(M - m < kRowsPerLaunch ? M - m : kRowsPerLaunch), N, K, p, r, s);
+    const hipError_t err = launch_rows<EPI, TO>((int)std::min<int64_t>(M - m, most), N, K, p, r, s);
     if (err != hipSuccess) return err;
   }
   return hipSuccess;

@@ -22,34 +22,72 @@ typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 constexpr float kTinyScale = 1.17549435e-38f;   // 2^-126
 constexpr uint32_t kInf = 0x7f800000u;
 
-// Elements c .. c + 7 of a row of n, zero past its end (TAIL: n % 8 != 0, so that a piece may end early).
+// Elements c .. c + 7 of a row of n, zero past its end (TAIL: n % 8 != 0, so that a piece may end early).  A piece that
+// ends early comes from the row's last eight elements, moved down: one load in the place of up to seven, which a whole
+// wave would wait for.  Nothing outside the row is read (but the other half of a word that holds one of its elements).
 template <bool TAIL>
 __device__ __forceinline__ void load8(const float *p, int c, int n, float (&v)[8]) {
-  if (!TAIL || c + 8 <= n) {
-    const f32x4u a = *reinterpret_cast<const f32x4u *>(p + c), b = *reinterpret_cast<const f32x4u *>(p + c + 4);
+  if (TAIL && n < 8) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = a[i];
-      v[4 + i] = b[i];
-    }
-  } else {
+    for (int i = 0; i < 8; ++i) v[i] = p[min(c + i, n - 1)];   // all on their way at once
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < n ? p[c + i] : 0.f;
+    for (int i = 0; i < 8; ++i) v[i] = c + i < n ? v[i] : 0.f;
+    return;
   }
+  const float *at = p + (TAIL ? min(c, n - 8) : c);
+  const f32x4u a = *reinterpret_cast<const f32x4u *>(at), b = *reinterpret_cast<const f32x4u *>(at + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = a[i];
+    v[4 + i] = b[i];
+  }
+  if (TAIL && c + 8 > n) {
+    const int by = c + 8 - n;
+#pragma unroll
+    for (int s = 4; s > 0; s >>= 1)
+      if (by & s) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i + s < 8 ? v[i + s] : 0.f;
+      }
+  }
+}
+// The same of a row of bf16, as it is stored.  Rows of odd length start off 4 bytes, which a load of 16 bytes pays for several
+// times over: those come from the five words around them.
+template <bool TAIL>
+__device__ __forceinline__ u32x4 raw8(const bf16 *p, int c, int n) {
+  if constexpr (!TAIL) return *reinterpret_cast<const u32x4u *>(p + c);
+  if (n < 8) {
+    u32x4 v = {0, 0, 0, 0};
+    uint32_t e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = __builtin_bit_cast(uint16_t, p[min(c + j, n - 1)]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j >> 1] |= c + j < n ? e[j] << (16 * (j & 1)) : 0u;
+    return v;
+  }
+  typedef uint32_t words __attribute__((ext_vector_type(4), aligned(4)));
+  const uintptr_t at = (uintptr_t)(p + min(c, n - 8));
+  const u32x4 w = *reinterpret_cast<const words *>(at & ~(uintptr_t)3);
+  const uint32_t last = *reinterpret_cast<const uint32_t *>((at + 15) & ~(uintptr_t)3), by = (uint32_t)at & 3;
+  u32x4 v = {__builtin_amdgcn_alignbyte(w[1], w[0], by), __builtin_amdgcn_alignbyte(w[2], w[1], by),
+             __builtin_amdgcn_alignbyte(w[3], w[2], by), __builtin_amdgcn_alignbyte(last, w[3], by)};
+  if (c + 8 > n) {
+    const int s = 16 * (c + 8 - n);   // 16 .. 112
+    typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+    const u64x2 d = __builtin_bit_cast(u64x2, v);
+    const uint64_t far = d[1] >> (s & 63);
+    v = __builtin_bit_cast(u32x4, s >= 64 ? u64x2{far, 0} : u64x2{d[0] >> s | d[1] << (64 - s), far});
+  }
+  return v;
+}
+__device__ __forceinline__ float half_of(u32x4 v, int j) {
+  return __builtin_bit_cast(float, j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16);
 }
 template <bool TAIL>
 __device__ __forceinline__ void load8(const bf16 *p, int c, int n, float (&v)[8]) {
-  if (!TAIL || c + 8 <= n) {
-    const u32x4u a = *reinterpret_cast<const u32x4u *>(p + c);
+  const u32x4 a = raw8<TAIL>(p, c, n);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __builtin_bit_cast(float, a[i] << 16);
-      v[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < n ? (float)p[c + i] : 0.f;
-  }
+  for (int i = 0; i < 8; ++i) v[i] = half_of(a, i);
 }
 // Eight elements as they are stored.
 template <typename T> struct Piece;
@@ -60,19 +98,8 @@ template <> struct Piece<float> {
 };
 template <> struct Piece<bf16> {
   u32x4 v;
-  template <bool TAIL> __device__ __forceinline__ void load(const bf16 *p, int c, int n) {
-    if (!TAIL || c + 8 <= n) {
-      v = *reinterpret_cast<const u32x4u *>(p + c);
-    } else {
-      v = u32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c + j < n) v[j >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, p[c + j]) << (16 * (j & 1));
-    }
-  }
-  __device__ __forceinline__ float operator[](int j) const {
-    return __builtin_bit_cast(float, j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16);
-  }
+  template <bool TAIL> __device__ __forceinline__ void load(const bf16 *p, int c, int n) { v = raw8<TAIL>(p, c, n); }
+  __device__ __forceinline__ float operator[](int j) const { return half_of(v, j); }
 };
 template <bool TAIL, bool NT = false>
 __device__ __forceinline__ void store8(float *p, int c, int n, const float (&v)[8]) {
@@ -251,7 +278,7 @@ template <typename T>
 static hipError_t quant_rows_of(int M, int K, const T *x, int64_t xs, int8_t *q, float *scale, hipStream_t s) {
   const int pieces = (K + 7) / 8;
 #define FB_ROWS(TR, NV) if (pieces <= TR * NV) return quant_rows<T, TR, NV>(M, K, x, xs, q, scale, s);
-  FB_ROWS(16, 1) FB_ROWS(32, 1) FB_ROWS(64, 1) FB_ROWS(64, 2) FB_ROWS(64, 3) FB_ROWS(64, 4)
+  FB_ROWS(16, 1) FB_ROWS(32, 1) FB_ROWS(64, 1) FB_ROWS(32, 3) FB_ROWS(64, 2) FB_ROWS(64, 3) FB_ROWS(64, 4)
   FB_ROWS(256, 2) FB_ROWS(256, 3) FB_ROWS(256, 4) FB_ROWS(256, 5) FB_ROWS(256, 6) FB_ROWS(256, 8)
   FB_ROWS(1024, 3) FB_ROWS(1024, 4) FB_ROWS(1024, 6) FB_ROWS(1024, 8)
 #undef FB_ROWS
@@ -353,7 +380,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
   __shared__ double part[2 * R::WAVES][2], tops[R::WAVES];
   const int64_t row = R::index();
   if (row >= M) return;
-  const int D = a.D;
+  const int D = a.D;   // elements past it (TAIL) take no branches: they stand at the pivot in the sums, and at zero in the end
   const float *xr = a.x + row * D;
   const T *yr = (const T *)a.y + row * D;
   const V alpha = (V)a.alpha;
@@ -384,8 +411,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
       if (a.post == NORM_NONE) continue;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (TAIL && c + j >= D) break;
-        const double d = (double)y[i][j] - pivot;
+        const double d = (double)(TAIL && c + j >= D ? (float)pivot : y[i][j]) - pivot;
         sum += d;
         sq = fma(d, d, sq);
       }
@@ -402,7 +428,6 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (TAIL && c + j >= D) break;
         h[i][j] = (float)fma((V)gate[j] * (V)gain[j], norm(y[i][j]), alpha * (V)h[i][j]);
       }
     }
@@ -439,8 +464,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
       if (a.pre == NORM_NONE) continue;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (TAIL && c + j >= D) break;
-        const double d = (double)h[i][j] - pivot;
+        const double d = (double)(TAIL && c + j >= D ? (float)pivot : h[i][j]) - pivot;
         sum += d;
         sq = fma(d, d, sq);
       }
@@ -458,8 +482,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (TAIL && c + j >= D) break;
-        v[i][j] = fma(norm(h[i][j]), (V)1 + (V)scale[j], (V)shift[j]);
+        v[i][j] = TAIL && c + j >= D ? (V)0 : fma(norm(h[i][j]), (V)1 + (V)scale[j], (V)shift[j]);
         if constexpr (OUT == SEAM_I8) {
           top = fmax(top, fabs(v[i][j]));
           bad |= v[i][j] != v[i][j];   // the maximum leaves NaN out
@@ -488,7 +511,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
         for (int j = 0; j < 8; ++j) {   // the nearest integer is what the low bits hold
           const double r = fma(v[i][j], inv, 6755399441055744.0);   // 1.5 2^52
-          code[j] = bad || (TAIL && c + j >= D) ? 0u : (uint32_t)__builtin_bit_cast(uint64_t, r);
+          code[j] = bad ? 0u : (uint32_t)__builtin_bit_cast(uint64_t, r);
         }
         store_codes<TAIL>(a.q + row * D, c, D, code);
       }

@@ -230,6 +230,20 @@ def test_more_rows_than_a_launch_takes(M, N):
     _linear(M, N, 48, "bf16", "residual")
 
 
+def test_more_outputs_than_a_launch_takes():
+    """1030 x 2^20: the widest layer, its rows in two launches."""
+    M, N, K = 1030, 1 << 20, 5
+    g = torch.Generator(device="cuda").manual_seed(21)
+    a = torch.randint(-128, 128, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-128, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    sa, sw = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+    out = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    F.flashbon_op_linear_i8(F.BF16, M, N, K, a, sa, w, sw, None, F.EPI_STORE, out)
+    for m in (0, 1023, 1024, 1029):
+        acc = (a[m].float() * w.float()).sum(1)            # whole numbers below 2^17
+        assert torch.equal(out[m], ((acc * sw) * sa[m]).bfloat16())
+
+
 @pytest.mark.parametrize("offset", [1, 4, 8])
 @pytest.mark.parametrize("M,N,K", [(70, 72, 80), (5, 48, 512), (300, 264, 256)])
 @pytest.mark.parametrize("epi", ["store", "residual"])
