@@ -464,7 +464,7 @@ __device__ __forceinline__ void epilogue(const I8Args &g, const EpiArgs &e, cons
 
 template <int EPI, typename TO, int WTA, int WT, int NST, int POL>
 __device__ __forceinline__ void tile(int M, int N, int K, const I8Args &g, const EpiArgs &e, int m0, int n0, char *smem) {
-  static_assert(WTA >= 4 && WTA <= 8 && (WT == 2 || WT == 4), "tile");
+  static_assert(WTA >= 2 && WTA <= 8 && (WT == 2 || WT == 4), "tile");
   constexpr int BM = 32 * WTA, BN = 64 * WT, STAGE = (BM + BN) * BK;
   static_assert(NST >= 2 && NST <= 4 && NST * STAGE <= 160 * 1024, "LDS");
   constexpr int NA = WTA, NW = 2 * WT, NL = NA > NW ? NA : NW;   // loads a K tile of an A wave and of a W wave
@@ -576,6 +576,91 @@ __device__ __forceinline__ void tile(int M, int N, int K, const I8Args &g, const
 
 }  // namespace ring
 
+// ------------------------------------------------------------ few rows, aligned: K shared by the waves, each with a ring
+// (16 MF) x (16 NF) outputs a workgroup and K dealt to its waves in pieces of 128 bytes as in k_linear_i8_split, but each
+// wave brings its pieces through an LDS ring of its own by loads that write LDS, rows of 128 bytes whole, NST pieces
+// ahead: nobody waits for another wave until the sums are added, and a CU reads two to three times the bytes a ns.  For K
+// in whole pieces of 16 bytes and rows on 16 bytes.  (130, 1536, 8960) 9.5 us against 18.9 of k_linear_i8_split, (37, 1536,
+// 8960) 6.7 and 14.0, (1, 5120, 13824) 12.6 and 19.5 (5.6 TB/s, W from the cache behind L2): the bytes a CU has on its way
+// bound it, below some 5 us latency.  Four stages for four waves or for a 16x16 tile were no faster.
+template <int EPI, typename TO, int MF, int NF, int WAVES, int NST>
+__global__ __launch_bounds__(64 * WAVES) void k_linear_i8_few(int M, int N, int K, I8Args g, EpiArgs e) {
+  using namespace ring;
+  constexpr int T = 64 * WAVES, ROWS = 16 * (MF + NF), STAGE = ROWS * BK, LA = 2 * MF, LW = 2 * NF, PER = LA + LW;
+  static_assert(NST <= 3 && (NST - 1) * PER < 64 && NST * STAGE >= MF * NF * 1024, "a wave's ring holds its sums");
+  extern __shared__ __attribute__((aligned(16))) char smem_few[];
+  const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int m0 = blockIdx.y * (16 * MF), n0 = blockIdx.x * (16 * NF);
+  char *const mine = smem_few + wave * (NST * STAGE);
+  const __amdgpu_buffer_rsrc_t rsA = buffer(g.A + (int64_t)m0 * K, (uint32_t)min(M - m0, 16 * MF) * (uint32_t)K);
+  const __amdgpu_buffer_rsrc_t rsW = buffer(g.W + (int64_t)n0 * K, (uint32_t)min(N - n0, 16 * NF) * (uint32_t)K);
+  // load x: rows 8 x .. + 7 of A (x < LA), then of W; lane l the piece that belongs in slot l & 7 of row l >> 3
+  const int lr = lane >> 3, ls = lane & 7;
+  const int pieces = (K + BK - 1) / BK, count = wave < pieces ? (pieces - wave + WAVES - 1) / WAVES : 0;
+  auto load = [&](int i) {   // this wave's piece i
+    const int k0 = (wave + i * WAVES) * BK;
+    char *to = mine + (i % NST) * STAGE;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      const int r = 8 * (x < LA ? x : x - LA) + lr, slot = (ls ^ swz(8 * x + lr)) << 4;
+      // past K (the next row's bytes, or past the last row): zero
+      const uint32_t off = k0 + slot < K ? (uint32_t)(r * K + slot) : OUT_OF_RANGE;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(x < LA ? rsA : rsW, (__attribute__((address_space(3))) void *)(to + x * (8 * BK)), 16,
+                                               off, k0, 0, 0);
+    }
+  };
+  i32x4 acc[NF][MF] = {};
+#pragma unroll
+  for (int i = 0; i < NST; ++i)
+    if (i < count) load(i);
+  for (int i = 0; i < count; ++i) {
+    wait_tiles<PER>(min(NST - 1, count - 1 - i));   // all but the pieces after this one
+    asm volatile("" ::: "memory");
+    const char *from = mine + (i % NST) * STAGE;
+    i32x4 fw[2][NF], fa[2][MF];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < MF; ++j) fa[h][j] = *reinterpret_cast<const i32x4 *>(from + at(16 * j + fr, 4 * h + fq));
+#pragma unroll
+      for (int n = 0; n < NF; ++n) fw[h][n] = *reinterpret_cast<const i32x4 *>(from + at(16 * (MF + n) + fr, 4 * h + fq));
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the stage has been read
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + NST < count) load(i + NST);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int n = 0; n < NF; ++n)
+#pragma unroll
+        for (int j = 0; j < MF; ++j) acc[n][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[h][n], fa[h][j], acc[n][j], 0, 0, 0);
+  }
+  if (count) {
+#pragma unroll
+    for (int n = 0; n < NF; ++n)
+#pragma unroll
+      for (int j = 0; j < MF; ++j)   // lane: columns 4 fq .. + 3 of row fr
+        *reinterpret_cast<i32x4 *>(mine + ((j * NF + n) * 256 + fr * 16 + 4 * fq) * 4) = acc[n][j];
+  }
+  __syncthreads();
+  const int busy = min(WAVES, pieces);
+#pragma unroll
+  for (int x = 0; x < (MF * NF * 256 + T - 1) / T; ++x) {
+    const int o = tid + T * x, ml = o / (16 * NF), nl = o % (16 * NF), m = m0 + ml, n = n0 + nl;
+    if (o >= MF * NF * 256 || m >= M || n >= N) continue;
+    const int64_t to = (int64_t)m * e.ldo + n;
+    float h = 0.f;
+    if constexpr (EPI == EPI_RESIDUAL) h = (e.res_in ? e.res_in : (const float *)e.out)[to];
+    const char *from = smem_few + (((ml >> 4) * NF + (nl >> 4)) * 256 + (ml & 15) * 16 + (nl & 15)) * 4;
+    int sum = 0;
+    for (int w = 0; w < busy; ++w) sum += *reinterpret_cast<const int *>(from + w * (NST * STAGE));
+    put<EPI, TO>(e, to, scaled(sum, g.w_scale[n], g.a_scale[m], e.bias ? e.bias[n] : 0.f),
+                 EPI == EPI_RESIDUAL && e.gate ? e.gate[n] : 1.f, h);
+  }
+}
+
 template <int EPI, typename TO, int WTA, int WT, int NST, int POL>
 __global__ __launch_bounds__(512, 1) void k_linear_i8_ring(int M, int N, int K, I8Args g, EpiArgs e, int MT, int NT, int group) {
   extern __shared__ __attribute__((aligned(16))) char smem_ring[];
@@ -618,33 +703,40 @@ int rows_per_launch(int N) { return std::min(1 << 15, (1 << 30) / N); }
 //   * Ring tiles: a round costs its K tiles and a fixed part, the epilogue, larger where it reads and writes the
 //     residual stream.  (24960, 8960, 1536) GELU 377, 425, 406, 483; (16384, 5120, 13824) residual 968, 1158, 1315, 1443;
 //     (24960, 1536, 1536) residual 148, 140, 136, 149; (24960, 1536, 8960) residual 394, 381, 410, 480; (4680, 1536,
-//     8960) 117, 75, 81, 97; (1560, 4608, 1536) 22, 17, 16, 18.  What fits one round of 128x128 tiles waits on the latency
-//     of each K tile, which a third stage hides best: (1560, 1536, 8960) 84, 54, 50, 34; (1560, 1536, 1536) 26, 17, 15, 13.
-//   * k_linear_i8_split by the bytes a CU reads, 25 a ns, 16 on rows off 4 bytes: (1, 8960, 1536) 4.9 against 8.6 on
-//     128x128 tiles, (16, 1536, 8960) 9.8 and 27, (390, 256, 256) 2.5 and 4.0, (64, 5120, 5120) 17.3 and 17.3, (512, 1536,
-//     4096) 25 and 15.
+//     8960) 117, 75, 81, 97; (1560, 4608, 1536) 22, 17, 16, 18.
+//   * What fits one round of 128x128 tiles waits on the latency of each K tile, which a third stage hides best, and less on
+//     smaller tiles as long as those fit a round too.  (1560, 1536, 8960) residual 84, 54, 50, and with three stages 128x128
+//     35, 96x128 33, 64x128 45 (two rounds); (1560, 1536, 1536) 9.3, 8.6, 10.5; (512, 1536, 4096) 15.4, 14.1, 13.3; (851,
+//     1536, 8960) 29, 27, 25; (200, 5120, 5120) 18.7, 18.5, 16.5.
+//   * k_linear_i8_few by the bytes a CU reads, 85 a ns, and a part a round: (130, 1536, 8960) 32x32 9.5, 64x32 13.9, 64x128
+//     ring tiles 22.6; (64, 5120, 5120) 64x32 11.2, 32x32 12.4, ring 15.8; (37, 1536, 8960) 32x16 6.7, 16x16 7.6, ring 21;
+//     (200, 5120, 5120) 26 and 16.5; (325, 1536, 1536) 8.5 and 6.7.
+//   * k_linear_i8_split the same way, 25 a ns, 16 on rows off 4 bytes: it has what few does not take, and small layers, for
+//     which it needs no more LDS than its sums: (390, 704, 256) 3.4 against 3.9 of few and 3.8 of ring tiles.
 //   * k_linear_i8_any for the larger layers off 16 bytes: (3000, 2501, 3001) 52 (64x32 split 176), (777, 1111, 999) 16
-//     and 12, (389, 701, 253) 10 and 5.6, (5000, 333, 2222) 24 and 40.
-enum Kernel { SPLIT11, SPLIT21, SPLIT22, SPLIT42, ANY, RING_256x256, RING_128x256, RING_128x128_TWO, RING_128x128, MIX };
+//     and 12, (389, 701, 253) 10 and 4.8, (5000, 333, 2222) 24 and 40.
+enum Kernel { SPLIT11, SPLIT21, SPLIT22, SPLIT42, ANY, FEW11, FEW21, FEW22, FEW42,
+              RING_256x256, RING_128x256, RING_128x128_TWO, RING_128x128, RING_96x128, RING_64x128, MIX };
 struct Plan {
   Kernel kernel;
   int wta = 0, blocks = 0, tall = 0;   // MIX
 };
-constexpr const char *kNames[] = {"split:16x16", "split:32x16", "split:32x32", "split:64x32", "any", "256x256", "128x256",
-                                  "128x128:two", "128x128"};
+constexpr const char *kNames[] = {"split:16x16", "split:32x16", "split:32x32", "split:64x32", "any", "few:16x16",
+                                  "few:32x16", "few:32x32", "few:64x32", "256x256", "128x256", "128x128:two", "128x128",
+                                  "96x128", "64x128"};
 
 // A round of 32 w rows, of one of 256.
 constexpr double kHeight[9] = {0, 0, 0, 0, 0, 0.75, 0.82, 0.9, 1.0};
 // Whether rows start off 4 bytes.
 bool off_words(const I8Args &g, int K) { return ((uintptr_t)g.A | (uintptr_t)g.W | (uintptr_t)K) % 4; }
 
-// aligned: what the ring kernels take; words: rows on 4 bytes.
-Plan pick(int M, int N, int K, bool aligned, bool words, int epi) {
+// aligned: what the ring tiles take; pieces: rows of whole 16-byte pieces; words: rows on 4 bytes.
+Plan pick(int M, int N, int K, bool aligned, bool pieces, bool words, int epi) {
   // FLASHBON_I8_TILE (tests and tuning) forces a kernel by its name; one that does not take the layer is passed over
   // ("mix:<w>:<blocks>:<tall>": two heights of 32 w and 32 (w - 1) rows, w in 6..8, covering M)
   if (const char *force = getenv("FLASHBON_I8_TILE")) {
-    for (int k = 0; k < 9; ++k)
-      if (!strcmp(force, kNames[k]) && (k <= SPLIT42 || (k == ANY ? K >= 16 : aligned))) return {(Kernel)k};
+    for (int k = 0; k < MIX; ++k)
+      if (!strcmp(force, kNames[k]) && (k <= SPLIT42 || (k == ANY ? K >= 16 : k <= FEW42 ? pieces : aligned))) return {(Kernel)k};
     Plan p = {MIX};
     if (aligned && sscanf(force, "mix:%d:%d:%d", &p.wta, &p.blocks, &p.tall) == 3 && p.wta >= 6 && p.wta <= 8 && p.tall >= 0 &&
         p.tall <= p.blocks && p.blocks <= M && 32 * ((int64_t)(p.wta - 1) * p.blocks + p.tall) >= M)
@@ -665,13 +757,22 @@ Plan pick(int M, int N, int K, bool aligned, bool words, int epi) {
   offer(SPLIT11, 16, 16, cus, 2.1, (16 + fmin(16, M)) * K / rate);
   offer(SPLIT21, 32, 16, cus, 2.1, (16 + fmin(32, M)) * K / rate);
   offer(SPLIT22, 32, 32, cus, 2.1, (32 + fmin(32, M)) * K / rate);
-  offer(SPLIT42, 64, 32, cus, 2.1, (32 + fmin(64, M)) * K / rate);
+  offer(SPLIT42, 64, 32, cus, 2.8, (32 + fmin(64, M)) * K / rate);
+  if (pieces) {
+    const double ring = 85e3;
+    offer(FEW11, 16, 16, cus, 2.5, 0.5 + (16 + fmin(16, M)) * K / ring);
+    offer(FEW21, 32, 16, cus, 2.5, 0.7 + (16 + fmin(32, M)) * K / ring);
+    offer(FEW22, 32, 32, cus, 2.5, 1.0 + (32 + fmin(32, M)) * K / ring);
+    offer(FEW42, 64, 32, cus, 2.5, 2.3 + (32 + fmin(64, M)) * K / ring);
+  }
   if (!aligned) {
     if (K >= 16) offer(ANY, 128, 128, 2 * cus, 5.0, 1.2 * kt);
     return best;
   }
   if ((double)((M + 127) / 128) * ((N + 127) / 128) <= cus) {
-    offer(RING_128x128, 128, 128, cus, 3.3, 0.35 * kt);
+    offer(RING_64x128, 64, 128, cus, 3.3, 0.3 * kt);
+    offer(RING_96x128, 96, 128, cus, 3.3, 0.345 * kt);
+    offer(RING_128x128, 128, 128, cus, 3.3, 0.37 * kt);
     return best;
   }
   const bool res = epi == EPI_RESIDUAL;
@@ -732,6 +833,17 @@ template <int EPI, typename TO> bool stores_past_caches(int M, int N, const EpiA
 // 1, 1037 at 4; (24960, 4608, 1536) 173 at 8, 183 at 4, 200 at 2; (24960, 8960, 1536) 394 at 4, 397 at 8, 429 at 1.
 int group_of(int N, int K) { return N <= 2048 ? 1 : K >= 4096 ? 2 : 8; }
 
+template <int EPI, typename TO, int MF, int NF, int WAVES, int NST>
+hipError_t launch_few(int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s) {
+  constexpr int LDS = WAVES * NST * 16 * (MF + NF) * ring::BK;
+  const auto kern = k_linear_i8_few<EPI, TO, MF, NF, WAVES, NST>;
+  static std::atomic<uint64_t> ready;
+  const hipError_t err = with_lds(kern, LDS, ready);
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL(kern, dim3((N + 16 * NF - 1) / (16 * NF), (M + 16 * MF - 1) / (16 * MF)), dim3(64 * WAVES), LDS, s, M, N, K, g, e);
+  return hipGetLastError();
+}
+
 template <int EPI, typename TO, int WTA>
 hipError_t launch_mix(int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s, const Plan &p) {
   constexpr int LDS = 2 * (32 * WTA + 256) * ring::BK;
@@ -762,17 +874,24 @@ template <int EPI, typename TO>
 hipError_t launch_rows(int M, int N, int K, const I8Args &g, const EpiArgs &e, hipStream_t s) {
   const uintptr_t at = (uintptr_t)g.A | (uintptr_t)g.W | (uintptr_t)g.w_scale | (uintptr_t)e.bias | (uintptr_t)e.out |
                        (uintptr_t)e.res_in | (uintptr_t)e.cache | (uintptr_t)e.gate;
-  const Plan p = pick(M, N, K, K % 16 == 0 && N % 8 == 0 && at % 16 == 0, !off_words(g, K), EPI);
+  const bool pieces = K % 16 == 0 && ((uintptr_t)g.A | (uintptr_t)g.W) % 16 == 0;
+  const Plan p = pick(M, N, K, pieces && N % 8 == 0 && at % 16 == 0, pieces, !off_words(g, K), EPI);
   switch (p.kernel) {
     case SPLIT11: return launch_split<EPI, TO, 1, 1, 2>(M, N, K, g, e, s);
     case SPLIT21: return launch_split<EPI, TO, 2, 1, 2>(M, N, K, g, e, s);
     case SPLIT22: return launch_split<EPI, TO, 2, 2, 2>(M, N, K, g, e, s);
     case SPLIT42: return launch_split<EPI, TO, 4, 2, 1>(M, N, K, g, e, s);
     case ANY: return launch_any<EPI, TO>(M, N, K, g, e, s);
+    case FEW11: return launch_few<EPI, TO, 1, 1, 8, 2>(M, N, K, g, e, s);
+    case FEW21: return launch_few<EPI, TO, 2, 1, 8, 2>(M, N, K, g, e, s);
+    case FEW22: return launch_few<EPI, TO, 2, 2, 8, 2>(M, N, K, g, e, s);
+    case FEW42: return launch_few<EPI, TO, 4, 2, 6, 2>(M, N, K, g, e, s);
     case RING_256x256: return launch_ring<EPI, TO, 8, 4, 2>(M, N, K, g, e, s);
     case RING_128x256: return launch_ring<EPI, TO, 4, 4, 3>(M, N, K, g, e, s);
     case RING_128x128: return launch_ring<EPI, TO, 4, 2, 3>(M, N, K, g, e, s);
     case RING_128x128_TWO: return launch_ring<EPI, TO, 4, 2, 2>(M, N, K, g, e, s);
+    case RING_96x128: return launch_ring<EPI, TO, 3, 2, 3>(M, N, K, g, e, s);
+    case RING_64x128: return launch_ring<EPI, TO, 2, 2, 3>(M, N, K, g, e, s);
     case MIX:
       return p.wta == 8   ? launch_mix<EPI, TO, 8>(M, N, K, g, e, s, p)
              : p.wta == 7 ? launch_mix<EPI, TO, 7>(M, N, K, g, e, s, p)

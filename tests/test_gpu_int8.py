@@ -201,7 +201,9 @@ def test_linear_options(M, N, K, kw):
     _linear(M, N, K, "bf16", "residual", **kw)
 
 
-TILES = ["split:16x16", "split:32x16", "split:32x32", "split:64x32", "any", "256x256", "128x256", "128x128:two", "128x128"]
+FEW = ["few:16x16", "few:32x16", "few:32x32", "few:64x32"]
+TILES = ["split:16x16", "split:32x16", "split:32x32", "split:64x32", "any", "256x256", "128x256", "128x128:two", "128x128",
+         "96x128", "64x128", *FEW]
 
 
 # a K of one, two, three and more of the ring's K tiles, K tails of 16 to 112, rows and columns on and beside the tiles' edges
@@ -223,6 +225,19 @@ def test_every_kernel_gives_the_same_bits(M, N, K, epi, dtype, monkeypatch):
                 if 0 <= tall <= blocks and lo * blocks + 32 * tall >= M:
                     monkeypatch.setenv("FLASHBON_I8_TILE", f"mix:{w}:{blocks}:{tall}")
                     assert torch.equal(_linear(M, N, K, dtype, epi), first), (w, blocks, tall)
+
+
+# waves with none, one, two, three and more of the pieces of K, a last piece of 16 to 128 bytes; columns that the tiles take
+# and no ring tile does
+@pytest.mark.parametrize("M,N,K", [(1, 1, 16), (65, 33, 1008), (31, 15, 1040), (17, 47, 2064), (130, 129, 2688), (3, 70, 8976)])
+@pytest.mark.parametrize("epi", ["store", "gelu", "residual"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_few_rows_any_columns(M, N, K, epi, dtype, monkeypatch):
+    monkeypatch.setenv("FLASHBON_I8_TILE", "split:16x16")
+    first = _linear(M, N, K, dtype, epi)
+    for tile in FEW:
+        monkeypatch.setenv("FLASHBON_I8_TILE", tile)
+        assert torch.equal(_linear(M, N, K, dtype, epi), first), tile
 
 
 @pytest.mark.parametrize("M,N", [(2, 40), (40000, 16)])
