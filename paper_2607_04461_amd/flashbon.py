@@ -557,6 +557,12 @@ def _raw_stream(stream, device: int) -> int:
     return int(stream) if stream is not None else _torch._C._cuda_getCurrentRawStream(device)
 
 
+def _int32(*sizes) -> None:
+    """Refuses sizes that the ABI's 32-bit integers would wrap."""
+    if max(sizes) > 0x7FFFFFFF:
+        raise ValueError(f"sizes must be below 2^31, got {sizes}")
+
+
 def _pointers(device: Optional[int], *wanted) -> list:
     """Addresses of the tensors in ``wanted``, (name, tensor or None, dtype, elements, required) each: of that dtype,
     contiguous, of at least so many elements, on the GPU ``device`` (None: anywhere)."""
@@ -583,6 +589,7 @@ def validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale, *, require_devic
     """Raise ValueError unless the tensors are what flashbon_op_quant_rows reads and writes; their addresses.  ``x`` may
     be a view of wider rows: 2-D with a unit column stride."""
     act, device = _act(dtype), _current_device(require_device)
+    _int32(M, K)
     if M < 1 or K < 1 or x_row_stride < K:
         raise ValueError(f"need M, K >= 1 and a row stride of at least K, got {M}, {K}, {x_row_stride}")
     if x.dtype is not act:
@@ -612,6 +619,7 @@ def validate_linear_i8(dtype, M, N, K, A, a_scale, W, w_scale, bias, epilogue, o
     """Raise ValueError unless the tensors are what flashbon_op_linear_i8 reads and writes; their addresses."""
     act, device = _act(dtype), _current_device(require_device)
     i8, f32 = _torch.int8, _torch.float32
+    _int32(M, N, K)
     found = _pointers(device, ("A", A, i8, M * K, True), ("a_scale", a_scale, f32, M, True), ("W", W, i8, N * K, True),
                       ("w_scale", w_scale, f32, N, True), ("bias", bias, f32, N, False),
                       ("out", out, act if epilogue == EPI_STORE or epilogue == EPI_GELU else f32, M * N, True))
@@ -635,6 +643,7 @@ def validate_norm_residual(dtype, M, D, x, y=None, out=None, q=None, q_scale=Non
     """Raise ValueError unless the tensors are what flashbon_op_norm_residual reads and writes; their addresses."""
     act, device = _act(dtype), _current_device(require_device)
     f32 = _torch.float32
+    _int32(M, D)
     return _pointers(device, ("x", x, f32, M * D, True), ("y", y, act, M * D, False), ("post_gain", post_gain, f32, D, False),
                      ("gate", gate, f32, D, False), ("x_out", x_out, f32, M * D, False), ("shift", shift, f32, D, False),
                      ("scale", scale, f32, D, False), ("out", out, act, M * D, False), ("q", q, _torch.int8, M * D, False),

@@ -107,6 +107,19 @@ def test_binding_refuses_norm(kw):
         fb.validate_norm_residual(**a, require_device=False)
 
 
+@pytest.mark.parametrize("M", [1 << 31, (1 << 32) + 1])
+def test_binding_refuses_sizes_that_would_wrap(M):
+    def m(shape, dtype):
+        return torch.empty(shape, dtype=dtype, device="meta")
+    with pytest.raises(ValueError, match="2\\^31"):
+        fb.validate_quant_rows(BF, M, 1, m((M, 1), B), 1, m((M, 1), I8), m(M, F), require_device=False)
+    with pytest.raises(ValueError, match="2\\^31"):
+        fb.validate_linear_i8(BF, M, 1, 1, m((M, 1), I8), m(M, F), m((1, 1), I8), m(1, F), None, fb.EPI_STORE, m((M, 1), B),
+                              require_device=False)
+    with pytest.raises(ValueError, match="2\\^31"):
+        fb.validate_norm_residual(BF, M, 1, m((M, 1), F), out=m((M, 1), B), require_device=False)
+
+
 def test_binding_wants_the_current_device():
     with pytest.raises(ValueError):
         fb._pointers(0, ("x", _t(4, F), F, 4, True))
