@@ -77,9 +77,11 @@ __device__ __forceinline__ i32x4 piece(const int8_t *p, int k, int K) {
 
 // ------------------------------------------------------------------------- few rows: K shared by the waves
 // (16 MF) x (16 NF) outputs a workgroup, K dealt to its eight waves in pieces of 128 bytes, operands from memory straight
-// into the products' registers: for layers whose larger tiles would leave most CUs idle, of any size and alignment.  A
-// piece of U of a wave's K, all loaded before their products, is on its way at once.  The waves' sums are added in LDS.
-// Bound by reading W once, below a few us by latency.
+// into the products' registers: for layers whose larger tiles would leave most CUs idle, of any size and alignment.  U
+// pieces of a wave's K, all loaded before their products, are on their way at once.  The waves' sums are added in LDS.
+// Bound by the loads, 16 rows of 64 bytes each (25 bytes a ns and CU, 16 where rows start off words), below a few us by
+// latency: (20, 24, 11076) 8.8 us, (20, 24, 11073) 15.3, (389, 701, 253) fp32 4.8.  Sixteen waves were no faster, and four
+// pieces at once slower where K is short.
 template <int EPI, typename TO, int MF, int NF, int WAVES, int U, bool BYTES>
 __global__ __launch_bounds__(64 * WAVES) void k_linear_i8_split(int M, int N, int K, I8Args g, EpiArgs e) {
   constexpr int T = 64 * WAVES;
@@ -166,7 +168,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_linear_i8_split(int M, int N, in
 
 // ------------------------------------------------------------------------------ any size and alignment
 // 128x128 tiles, four waves of 64x64, two workgroups a CU.  K tiles of 128 bytes go through registers into two LDS
-// stages, loaded two K tiles ahead: rows that start on any byte are not loaded into LDS directly.  K >= 16.
+// stages, loaded two K tiles ahead: rows that start on any byte are not loaded into LDS directly.  K >= 16.  Bound by those
+// loads and stores: (3000, 2504, 3004) 43 us, on bytes that start off words 52, on ring tiles with K = 3008 28.
 namespace any8 {
 constexpr int BM = 128, BN = 128, BK = 128, STAGE = (BM + BN) * BK, PER = (BM + BN) / 32;
 // 16-byte piece c of row r at c ^ swz(r): the 16 lanes that read one piece of 16 rows at once meet 16 places
@@ -298,6 +301,15 @@ __global__ __launch_bounds__(256, 2) void k_linear_i8_any(int M, int N, int K, I
 // tile's loads issued NST - 1 tiles ahead or more; the fragments of a 64-byte substep are read between the
 // products of the one before, and one barrier a K tile keeps the waves together.  The weights are the products' row
 // operand, their rows permuted within groups of 32 so that a lane ends with eight consecutive columns of one row.
+// On 256x256 tiles (16384, 5120, 13824) residual takes 975 us, 2.38 POP/s (an 8192^3 library product reaches 2.1), at 1.5
+// GHz with the matrix cores busy 63% of the cycles: power bounds it.  With the loads, the LDS reads or the epilogue left
+// out it takes 0.81, 0.96 and 0.83 of its time, the products alone 0.61.  (24960, 8960, 1536) GELU takes 375, 1.83 POP/s,
+// at 2.0 GHz and 42%: 0.89, 0.92, 0.67 and 0.51, so there the epilogue costs most, 12 K tiles and 447 MB of output a launch.
+// Two workgroups of four waves a CU on smaller tiles, so that one's epilogue runs under the other's products, took 388 at
+// best where these took 398, and 1219 where these took 1033.
+// The tiles for one round of workgroups are bound by the bytes a CU brings into LDS, 70 to 85 a ns: (1560, 1536, 8960) 31
+// us, 204 tiles of 96x128.  With half of each K tile for four waves in place of eight, three quarters of the LDS reads
+// and half the steps, they were slower (33, and 20 for 17 of (1560, 4608, 1536) on 128x128).
 namespace ring {
 
 constexpr int BK = 128;
@@ -466,7 +478,7 @@ template <int EPI, typename TO, int WTA, int WT, int NST, int POL>
 __device__ __forceinline__ void tile(int M, int N, int K, const I8Args &g, const EpiArgs &e, int m0, int n0, char *smem) {
   static_assert(WTA >= 2 && WTA <= 8 && (WT == 2 || WT == 4), "tile");
   constexpr int BM = 32 * WTA, BN = 64 * WT, STAGE = (BM + BN) * BK;
-  static_assert(NST >= 2 && NST <= 4 && NST * STAGE <= 160 * 1024, "LDS");
+  static_assert(NST >= 2 && NST <= 3 && NST * STAGE <= 160 * 1024, "wait_tiles counts two tiles ahead; LDS");
   constexpr int NA = WTA, NW = 2 * WT, NL = NA > NW ? NA : NW;   // loads a K tile of an A wave and of a W wave
   constexpr int NR = WT + WTA;                                   // fragments a substep
   const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4;
@@ -537,7 +549,6 @@ __device__ __forceinline__ void tile(int M, int N, int K, const I8Args &g, const
     if (loads_a) wait_tiles<NA>(ahead);
     else wait_tiles<NW>(ahead);
   };
-  static_assert(NST <= 3, "wait_tiles counts two tiles ahead");
   landed(min(NST, KT) - 1);
   barrier();
 #pragma unroll
