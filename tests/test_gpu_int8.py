@@ -566,3 +566,101 @@ def test_the_branch_captured_and_replayed():
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(p, q) for p, q in zip(ref, b.results()))
+
+
+# ------------------------------------------------------------------------- tensors past 2^31 elements and 2^32 bytes
+def _spread(M):
+    """Rows on both sides of a launch's part of the rows, and the last."""
+    return [0, (1 << 20) - 1, 1 << 20, M - 1]
+
+
+def test_rows_past_32_bits():
+    M, K = (1 << 20) + 77, 2100
+    g = torch.Generator(device="cuda").manual_seed(31)
+    x = torch.empty(M, K, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    q, s = torch.empty(M, K, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    F.flashbon_op_quant_rows(F.BF16, M, K, x, q, s)
+    for m in _spread(M):
+        rq, rs = o8.quant_rows(_f64(x[m:m + 1]))
+        assert np.array_equal(_f64(q[m:m + 1]), rq) and s[m].item() == rs[0]
+
+
+def test_a_row_stride_past_32_bits():
+    stride, K = (1 << 31) + 24, 1000
+    x = torch.zeros(2 * stride, dtype=torch.bfloat16, device="cuda").view(2, stride)[:, :K]
+    x.copy_(torch.randn(2, K, generator=torch.Generator(device="cuda").manual_seed(32), device="cuda"))
+    q, s = _quant(x, F.BF16, 2, K)
+    rq, rs = o8.quant_rows(_f64(x))
+    assert np.array_equal(q, rq) and np.array_equal(s, rs)
+
+
+@pytest.mark.parametrize("out", ["i8", "act"])
+def test_a_stream_past_32_bits(out):
+    M, D = (1 << 20) + 77, 2100
+    g = torch.Generator(device="cuda").manual_seed(33)
+    x = torch.empty(M, D, device="cuda").normal_(generator=g)
+    y = torch.empty(M, D, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+
+    def run(x, y):
+        n = x.shape[0]
+        h = torch.empty(n, D, device="cuda")
+        a = torch.empty(n, D, dtype=torch.int8 if out == "i8" else torch.bfloat16, device="cuda")
+        s = torch.empty(n, device="cuda")
+        F.flashbon_op_norm_residual(F.BF16, n, D, EPS, x, y, post_norm=F.NORM_RMS, x_out=h,
+                                    **(dict(q=a, q_scale=s) if out == "i8" else dict(out=a)))
+        return (h, a, s) if out == "i8" else (h, a)
+
+    whole, rows = run(x, y), _spread(M)
+    few = run(x[rows].contiguous(), y[rows].contiguous())   # held to the oracle by the tests above
+    assert all(torch.equal(p[rows], r) for p, r in zip(whole, few))
+
+
+@pytest.mark.parametrize("K", [65536, 65533])
+def test_layers_past_32_bits(K):
+    """Rows that begin past 2^31 bytes of A, and weights that do."""
+    for M, N in ((34000, 8), (5, 34000)):
+        g = torch.Generator(device="cuda").manual_seed(34)
+        a = torch.randint(-128, 128, (M, K), generator=g, device="cuda", dtype=torch.int8)
+        w = torch.randint(-128, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
+        sa, sw = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+        out = torch.empty(M, N, device="cuda")
+        F.flashbon_op_linear_i8(F.FP32, M, N, K, a, sa, w, sw, None, F.EPI_STORE, out)
+        for m in (0, 32767, 32768, M - 1) if M > N else range(M):
+            for n in range(N) if M > N else (0, 32767, 32768, N - 1):
+                acc = int((_f64(a[m]) * _f64(w[n])).sum())   # whole numbers below 2^30
+                assert out[m, n].item() == np.float32(np.float32(acc) * np.float32(sw[n].item())) * np.float32(sa[m].item())
+
+
+# ------------------------------------------------------------------------------------------- two threads at once
+def test_two_threads_at_once():
+    """Two branches, each on a thread and a stream of its own."""
+    import threading
+
+    branches = [Branch(130, 256, 704, 41), Branch(390, 136, 520, 42)]
+    refs, failed = [], []
+    for b in branches:
+        b.x.normal_()
+        b.run()
+        torch.cuda.synchronize()
+        refs.append(b.results())
+        for t in (b.a, b.u, b.qu, b.y, b.out, b.next):
+            t.zero_()
+    torch.cuda.synchronize()
+
+    def work(b):
+        try:
+            stream = torch.cuda.Stream()
+            for _ in range(20):
+                b.run(stream=stream.cuda_stream)
+            stream.synchronize()
+        except Exception as e:   # noqa: BLE001 - reported by the test's own thread
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(b,)) for b in branches]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    for b, ref in zip(branches, refs):
+        assert all(torch.equal(p, q) for p, q in zip(ref, b.results()))
