@@ -400,14 +400,19 @@ __device__ __forceinline__ void epilogue(const I8Args &g, const EpiArgs &e, cons
       for (int cg = 0; cg < CG; ++cg)
 #pragma unroll
         for (int j = 0; j < WP; ++j) {
-          bf16x8 w;
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
+          auto value = [&](int q) {
             const float v = scaled(acc[2 * cg + (q >> 2)][WP * p + j][q & 3], ws[cg][q >> 2][q & 3], as[WP * p + j],
                                    bias[cg][q >> 2][q & 3]);
-            w[q] = (bf16)(EPI == EPI_GELU ? gelu_tanh(v) : v);
+            return EPI == EPI_GELU ? gelu_tanh(v) : v;
+          };
+          typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+          u32x4 w;   // by pairs: one conversion each, and no moves between them
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float lo = value(2 * q), hi = value(2 * q + 1);
+            w[q] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)lo, (bf16)hi});
           }
-          *reinterpret_cast<bf16x8 *>(wl + place(16 * j + fr, 4 * cg + fq)) = w;
+          *reinterpret_cast<u32x4 *>(wl + place(16 * j + fr, 4 * cg + fq)) = w;
         }
 #pragma unroll
       for (int t = 0; t < R / RI; ++t) {
