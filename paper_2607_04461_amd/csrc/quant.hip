@@ -306,10 +306,11 @@ hipError_t launch_quant_rows(ActType t, int M, int K, const void *x, int64_t x_r
 // come from one pass of sums in 64 bits over the row less its first element (the pivot), so that a large common offset
 // costs no digits: the variance is off by about 2^-53 (1 + (mean - pivot)^2 / variance) of itself.  Codes are decided on
 // values in 64 bits as well.
-// Bound by HBM: (4 + e) M D bytes read, 4 M D + (e or 1) M D written: 24960 x 1536 bf16 to codes 99 us (4.2 TB/s) and to
-// activations 98 (4.7), 16384 x 5120 to activations 212 (4.7), one token of 1536 3.9 us.  The 64-bit arithmetic, some 30
-// instructions an element at the rate of 32-bit ones, hides behind that, as long as registers leave five waves a SIMD:
-// y stays as it is stored and values are formed anew from h (held in 64 bits instead, 105 us).
+// Bound by HBM: (4 + e) M D bytes read, 4 M D + (e or 1) M D written: 24960 x 1536 bf16 to codes 97 us (4.3 TB/s) and to
+// activations 96 (4.8), 16384 x 5120 to activations 212 (4.7), one token of 1536 3.9 us.  The 64-bit arithmetic, some 30
+// instructions an element at the rate of 32-bit ones, hides behind that, as long as registers leave four waves a SIMD: y
+// stays as it is stored.  Pieces of four elements, which make a wave's accesses to fp32 whole ranges, bring the vectors in
+// twice as many waits: (16384, 5120) to activations 191, but (24960, 1536) 102 and (8192, 6144) 152 in place of 131.
 namespace {
 
 // The row's two sums, for all its threads.  part: LDS that this call alone uses, so that one barrier does.
@@ -373,7 +374,9 @@ __device__ __forceinline__ void load8_or(const float *p, float otherwise, int c,
 
 enum { SEAM_NONE = 0, SEAM_ACT = 1, SEAM_I8 = 2 };
 
-template <typename T, int TR, int NV, bool TAIL, int OUT, bool NT>
+// FULL: the row fills its threads' pieces, so that no load waits behind a branch: (1560, 1536) to codes 10.2 us against 11.5,
+// (24960, 1536) 96 and 98.
+template <typename T, int TR, int NV, bool TAIL, int OUT, bool NT, bool FULL>
 __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArgs a) {
   using R = Row<TR>;
   using V = std::conditional_t<OUT == SEAM_I8, double, float>;   // of the elements
@@ -388,7 +391,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = 8 * (R::lane() + TR * i);
-    if (c < D) load8<TAIL>(xr, c, D, h[i]);
+    if (FULL || c < D) load8<TAIL>(xr, c, D, h[i]);
   }
   // one piece a thread: what it needs of the vectors is on its way before the sums
   constexpr bool EARLY = NV == 1;
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
-      if (c >= D) break;
+      if (!FULL && c >= D) break;
       y[i].template load<TAIL>(yr, c, D);
       if (a.post == NORM_NONE) continue;
 #pragma unroll
@@ -421,7 +424,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
-      if (c >= D) break;
+      if (!FULL && c >= D) break;
       if constexpr (!EARLY) {
         load8_or<TAIL>(a.gain, 1.f, c, D, gain);
         load8_or<TAIL>(a.gate, 1.f, c, D, gate);
@@ -441,7 +444,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
-      if (c < D) store8<TAIL, NT>(a.x_out + row * D, c, D, h[i]);
+      if (FULL || c < D) store8<TAIL, NT>(a.x_out + row * D, c, D, h[i]);
     }
   }
   if constexpr (OUT != SEAM_NONE) {
@@ -460,7 +463,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
-      if (c >= D) break;
+      if (!FULL && c >= D) break;
       if (a.pre == NORM_NONE) continue;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -475,7 +478,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
-      if (c >= D) break;
+      if (!FULL && c >= D) break;
       if constexpr (!EARLY) {
         load8_or<TAIL>(a.scale, 0.f, c, D, scale);
         load8_or<TAIL>(a.shift, 0.f, c, D, shift);
@@ -506,7 +509,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = 8 * (R::lane() + TR * i);
-        if (c >= D) break;
+        if (!FULL && c >= D) break;
         uint32_t code[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {   // the nearest integer is what the low bits hold
@@ -525,9 +528,13 @@ static hipError_t norm_rows(int M, const SeamArgs &a, hipStream_t s) {
   // a stream of 64 MiB and more is stored non-temporally: nothing reads it soon ((24960, 1536) to codes 105 -> 101 us,
   // (16384, 5120) to activations 224 -> 219); a smaller one the next kernel may still find in the caches
   const bool nt = a.x_out && (size_t)M * a.D * 4 >= (size_t)64 << 20;
-  if (a.D % 8) hipLaunchKernelGGL((k_norm_residual<T, TR, NV, true, OUT, false>), grid, block, 0, s, M, a);
-  else if (nt) hipLaunchKernelGGL((k_norm_residual<T, TR, NV, false, OUT, true>), grid, block, 0, s, M, a);
-  else hipLaunchKernelGGL((k_norm_residual<T, TR, NV, false, OUT, false>), grid, block, 0, s, M, a);
+  // on more threads it gained nothing: (1560, 4096) to codes 20.6 us and 21.3, but to activations 18.8 and 18.2
+  constexpr bool FULL = NV > 1 && TR < 256;
+  const bool full = FULL && a.D == 8 * TR * NV;
+  const auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, s, M, a); };
+  if (a.D % 8) go(k_norm_residual<T, TR, NV, true, OUT, false, false>);
+  else if (nt) full ? go(k_norm_residual<T, TR, NV, false, OUT, true, FULL>) : go(k_norm_residual<T, TR, NV, false, OUT, true, false>);
+  else full ? go(k_norm_residual<T, TR, NV, false, OUT, false, FULL>) : go(k_norm_residual<T, TR, NV, false, OUT, false, false>);
   return hipGetLastError();
 }
 
@@ -536,7 +543,7 @@ static hipError_t norm_rows_of(int M, const SeamArgs &a, hipStream_t s) {
   const int pieces = (a.D + 7) / 8;
 #define FB_ROWS(TR, NV) if (pieces <= TR * NV) return norm_rows<T, TR, NV, OUT>(M, a, s);
   FB_ROWS(16, 1) FB_ROWS(32, 1) FB_ROWS(64, 1)   // several rows a wave: 24960 x 64 10 us, on whole waves 34
-  // few rows wait on a row's own chain, which more threads shorten: 390 x 1536 5.4 us and 7.3, but 24960 x 1536 105 and 99
+  // few rows wait on a row's own chain, which more threads shorten: 390 x 1536 5.5 us and 7.3, but 24960 x 1536 105 and 99
   if (M <= 2 * cu_count()) { FB_ROWS(256, 1) }
   FB_ROWS(64, 2) FB_ROWS(64, 3) FB_ROWS(128, 2) FB_ROWS(192, 2) FB_ROWS(256, 2) FB_ROWS(256, 3)
 #undef FB_ROWS
