@@ -303,7 +303,7 @@ __global__ __launch_bounds__(256, 2) void k_linear_i8_any(int M, int N, int K, I
 // operand, their rows permuted within groups of 32 so that a lane ends with eight consecutive columns of one row.
 // On 256x256 tiles (16384, 5120, 13824) residual takes 975 us, 2.38 POP/s (an 8192^3 library product reaches 2.1), at 1.5
 // GHz with the matrix cores busy 63% of the cycles: power bounds it.  With the loads, the LDS reads or the epilogue left
-// out it takes 0.81, 0.96 and 0.83 of its time, the products alone 0.61.  (24960, 8960, 1536) GELU takes 375, 1.83 POP/s,
+// out it takes 0.81, 0.96 and 0.83 of its time, the products alone 0.61.  (24960, 8960, 1536) GELU takes 370, 1.86 POP/s,
 // at 2.0 GHz and 42%: 0.89, 0.92, 0.67 and 0.51, so there the epilogue costs most, 12 K tiles and 447 MB of output a launch.
 // Two workgroups of four waves a CU on smaller tiles, so that one's epilogue runs under the other's products, took 388 at
 // best where these took 398, and 1219 where these took 1033.
