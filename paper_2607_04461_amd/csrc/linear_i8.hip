@@ -719,7 +719,8 @@ int rows_per_launch(int N) { return std::min(1 << 15, (1 << 30) / N); }
 //   * Ring tiles: a round costs its K tiles and a fixed part, the epilogue, larger where it reads and writes the
 //     residual stream.  (24960, 8960, 1536) GELU 377, 425, 406, 483; (16384, 5120, 13824) residual 968, 1158, 1315, 1443;
 //     (24960, 1536, 1536) residual 148, 140, 136, 149; (24960, 1536, 8960) residual 394, 381, 410, 480; (4680, 1536,
-//     8960) 117, 75, 81, 97; (1560, 4608, 1536) 22, 17, 16, 18.
+//     8960) 117, 75, 81, 97; (1560, 4608, 1536) 22, 16.4, 15.4, 18; (900, 7168, 512) 128x256 9.1, 128x128 8.3; (3120, 2304,
+//     768) GELU 12.8 and 11.5; (1560, 4608, 2048) 18.4 and 17.8, (3000, 2504, 3008) 27.6 and 30.3.
 //   * What fits one round of 128x128 tiles waits on the latency of each K tile, which a third stage hides best, and less on
 //     smaller tiles as long as those fit a round too.  (1560, 1536, 8960) residual 84, 54, 50, and with three stages 128x128
 //     35, 96x128 33, 64x128 45 (two rounds); (1560, 1536, 1536) 9.3, 8.6, 10.5; (512, 1536, 4096) 15.4, 14.1, 13.3; (851,
@@ -794,7 +795,8 @@ Plan pick(int M, int N, int K, bool aligned, bool pieces, bool words, int epi) {
   const bool res = epi == EPI_RESIDUAL;
   offer(RING_256x256, 256, 256, cus, 0, 1.75 * kt + (res ? 27 : 9));
   offer(RING_128x256, 128, 256, cus, 0, 1.03 * kt + (res ? 15 : 6));
-  offer(RING_128x128_TWO, 128, 128, 2 * cus, 0, 1.2 * kt + (res ? 12 : 5.5));
+  const bool alone = (double)((M + 127) / 128) * ((N + 127) / 128) <= 2 * cus;   // one round, nothing stored before it
+  offer(RING_128x128_TWO, 128, 128, 2 * cus, 0, 1.2 * kt + (res ? 12 : alone ? 2.9 : 5.5));
   // as many blocks of two heights as fill whole rounds
   const int NT = (N + 255) / 256;
   for (int w = 8; w >= 6; --w) {
