@@ -129,21 +129,22 @@ __device__ __forceinline__ void store8(bf16 *p, int c, int n, const float (&v)[8
       if (c + i < n) p[c + i] = (bf16)v[i];
   }
 }
-// Eight codes, each in the low byte of a word.
-template <bool TAIL>
-__device__ __forceinline__ void store_codes(int8_t *p, int c, int n, const uint32_t (&q)[8]) {
+// Eight codes, each in byte AT of a word; zeros for a row without a scale.
+template <bool TAIL, int AT>
+__device__ __forceinline__ void store_codes(int8_t *p, int c, int n, const uint32_t (&q)[8], bool bad) {
   if (!TAIL || c + 8 <= n) {
     u32x2u w;
+    constexpr uint32_t two = 0x0c0c0400 + 0x0101 * AT;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {   // bytes 0 and 4 of a pair, then the two halves
-      const uint32_t lo = __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0c0c0400), hi = __builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x0c0c0400);
-      w[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100);
+    for (int i = 0; i < 2; ++i) {   // the bytes of a pair, then the two halves
+      const uint32_t lo = __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], two), hi = __builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], two);
+      w[i] = bad ? 0u : __builtin_amdgcn_perm(hi, lo, 0x05040100);
     }
     *reinterpret_cast<u32x2u *>(p + c) = w;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c + i < n) p[c + i] = (int8_t)q[i];
+      if (c + i < n) p[c + i] = bad ? (int8_t)0 : (int8_t)(q[i] >> (8 * AT));
   }
 }
 
@@ -258,11 +259,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_quant_rows(int M, int K, con
 #pragma unroll
       for (int j = 0; j < 8; ++j) code[j] = (uint32_t)(int)__builtin_rint((double)v[i][j] / (double)s);
     }
-    if (bad) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) code[j] = 0;
-    }
-    store_codes<TAIL>(qr, c, K, code);
+    store_codes<TAIL, 0>(qr, c, K, code, bad);
   }
 }
 
@@ -510,13 +507,24 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
       for (int i = 0; i < NV; ++i) {
         const int c = 8 * (R::lane() + TR * i);
         if (!FULL && c >= D) break;
-        uint32_t code[8];
+        // v / s + 1/2 to 24 bits behind the point, the integer in the low word's last byte: off by less than a step of those
+        // it decides, but where it comes out as a whole number
+        uint32_t code[8], least = ~0u;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {   // the nearest integer is what the low bits hold
-          const double r = fma(v[i][j], inv, 6755399441055744.0);   // 1.5 2^52
-          code[j] = bad ? 0u : (uint32_t)__builtin_bit_cast(uint64_t, r);
+        for (int j = 0; j < 8; ++j) {
+          code[j] = (uint32_t)__builtin_bit_cast(uint64_t, fma(v[i][j], inv, 402653184.5));   // 1.5 2^28 + 1/2
+          least = min(least, code[j] << 8);
         }
-        store_codes<TAIL>(a.q + row * D, c, D, code);
+        if (least == 0) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            // the border, a number of 8 bits times s, is exact, and so is the sign of its distance
+            const int up = (int)code[j] >> 24;
+            const double over = fma(up - 0.5, (double)s, -v[i][j]);
+            if (code[j] << 8 == 0 && (over > 0 || (over == 0 && up % 2))) code[j] -= 1;
+          }
+        }
+        store_codes<TAIL, 3>(a.q + row * D, c, D, code, bad);
       }
     }
   }

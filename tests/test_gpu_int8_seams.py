@@ -1,0 +1,79 @@
+"""The seam between two blocks where its rounding decides: ties between two codes, rows that a norm leaves nothing of,
+vectors whose product no fp32 holds, rows at the end of the range, and the same rows among many and among few."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import int8 as o8
+from paper_2607_04461_amd import flashbon as F
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24                                     # half a step of fp32, relative
+ACT = {F.BF16: torch.bfloat16, F.FP32: torch.float32}
+EPS = 1e-6
+# fewer rows than two a CU and more: widths of 513 to 2048 are laid out otherwise
+FEW, MANY = 6, 530
+WIDTHS = [(FEW, 40), (FEW, 41), (FEW, 500), (FEW, 1000), (MANY, 1000), (MANY, 1536), (MANY, 1601), (FEW, 2100), (FEW, 5003)]
+
+
+def _dev(a, dtype=torch.float32):
+    return torch.from_numpy(np.ascontiguousarray(a)).to("cuda").to(dtype)
+
+
+def _f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def _to_codes(x, y=None, dtype=F.FP32, **kw):
+    M, D = x.shape
+    q, s = torch.empty(M, D, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    h = torch.empty(M, D, device="cuda")
+    F.flashbon_op_norm_residual(dtype, M, D, EPS, x, y, x_out=h, q=q, q_scale=s, **kw)
+    return h, q.cpu().numpy(), s.cpu().numpy()
+
+
+def _to_act(x, y=None, dtype=F.FP32, **kw):
+    a, h = torch.empty_like(x, dtype=ACT[dtype]), torch.empty_like(x)
+    F.flashbon_op_norm_residual(dtype, *x.shape, EPS, x, y, x_out=h, out=a, **kw)
+    return h, a
+
+
+# ------------------------------------------------------------------------------------------------- ties
+def _ties(M, D):
+    """Rows whose elements are (k + 1/2) s, s whole numbers and thirds of powers of two that fp32 holds; every third one
+    step below, every third one above.  The largest is 127 s."""
+    r = np.random.default_rng(3)
+    scales = np.array([3, 5, 7, 11, 49, 99, 197, 3 * 2.0 ** -70, 5 * 2.0 ** 40])[np.arange(M) % 9]
+    v = ((r.integers(-127, 127, (M, D)) + 0.5) * scales[:, None]).astype(np.float32)
+    v[:, 1::3] = np.nextafter(v[:, 1::3], np.float32(0))
+    v[:, 2::3] = np.nextafter(v[:, 2::3], np.float32(np.inf))
+    v[:, D // 2] = 127 * scales
+    return v
+
+
+@pytest.mark.parametrize("M,D", WIDTHS)
+def test_ties_go_to_the_even_code(M, D):
+    v = _ties(M, D)
+    rq, rs = o8.quant_rows(v)
+    _, q, s = _to_codes(_dev(v), pre_norm=F.NORM_NONE)
+    assert np.array_equal(s, rs) and np.array_equal(q, rq)
+
+
+@pytest.mark.parametrize("M,D", WIDTHS)
+def test_ties_made_of_a_branch_and_a_shift(M, D):
+    """Whole halves: the stream, the branch, its gate and the shift add to (k + 1/2) s without a rounding."""
+    r = np.random.default_rng(4)
+    scales = np.array([3, 5, 7, 11, 49, 99])[np.arange(M) % 6]
+    k = r.integers(-120, 120, (M, D))
+    k[:, 0], half = 127, np.full((M, D), 0.5)
+    half[:, 0] = 0.0
+    a = (k + half) * scales[:, None]
+    shift, gate = r.integers(-9, 10, D).astype(np.float64), r.choice([-2.0, 0.5, 1.0], D)
+    y = r.integers(-50, 50, (M, D)).astype(np.float64)
+    x = (a - shift - gate * y) * 2                                    # alpha 1/2
+    h, q, s = _to_codes(_dev(x), _dev(y, torch.bfloat16), F.BF16, alpha=0.5, gate=_dev(gate), shift=_dev(shift),
+                        pre_norm=F.NORM_NONE)
+    rq, rs = o8.quant_rows(a)
+    assert np.array_equal(_f64(h), a - shift)
+    assert np.array_equal(s, rs) and np.array_equal(q, rq)
