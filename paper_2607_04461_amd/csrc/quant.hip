@@ -334,15 +334,16 @@ template <int TR> __device__ __forceinline__ void row_sums(double &a, double &b,
 // A row's norm, (v - mean) by, in type V; from the sums of v - pivot and of its square over D elements (pivot 0 but for
 // LayerNorm's, whose mean is pivot + sum / D).
 template <typename V> struct Norm;
-template <> struct Norm<double> {
-  double by = 1.0, plus = 0.0;
-  __device__ __forceinline__ Norm(int kind, double pivot, double sum, double sq, int D, double eps) {
+template <> struct Norm<double> {   // the pivot comes off first: what equals it in a row of one value leaves no digits
+  double by = 1.0, pivot = 0.0, plus = 0.0;
+  __device__ __forceinline__ Norm(int kind, double first, double sum, double sq, int D, double eps) {
     if (kind == NORM_NONE) return;
     const double n = D, m = kind == NORM_LAYER ? sum / n : 0.0, var = sq / n - m * m;
     by = 1.0 / sqrt((var < 0 ? 0 : var) + eps);   // NaN stays
-    plus = -(pivot + m) * by;
+    pivot = first;
+    plus = -m * by;
   }
-  __device__ __forceinline__ double operator()(float v) const { return fma((double)v, by, plus); }
+  __device__ __forceinline__ double operator()(float v) const { return fma((double)v - pivot, by, plus); }
 };
 template <> struct Norm<float> {   // the mean in two parts, so that it costs no digits of v - mean
   float by, mean, rest;

@@ -77,3 +77,26 @@ def test_ties_made_of_a_branch_and_a_shift(M, D):
     rq, rs = o8.quant_rows(a)
     assert np.array_equal(_f64(h), a - shift)
     assert np.array_equal(s, rs) and np.array_equal(q, rq)
+
+
+# ------------------------------------------------------------------------------------------ constant rows
+CONSTANTS = [0.3, -7.7, 1e-3, 33333.3, 1e30, -1e-30]
+
+
+@pytest.mark.parametrize("M,D", WIDTHS)
+def test_layer_norm_leaves_nothing_of_a_constant_row(M, D):
+    c = np.array(CONSTANTS, np.float32)[np.arange(M) % len(CONSTANTS)]
+    x = _dev(np.repeat(c[:, None], D, 1))
+    h, q, s = _to_codes(x, pre_norm=F.NORM_LAYER)
+    assert torch.equal(h, x)
+    assert (s == np.float32(2.0 ** -126)).all() and (q == 0).all()
+    _, a = _to_act(x, pre_norm=F.NORM_LAYER)
+    assert (a == 0).all()
+
+
+@pytest.mark.parametrize("M,D", WIDTHS)
+def test_a_constant_branch_adds_nothing(M, D):
+    c = np.array(CONSTANTS, np.float32)[np.arange(M) % len(CONSTANTS)]
+    x, y = torch.zeros(M, D, device="cuda"), _dev(np.repeat(c[:, None], D, 1))
+    for run in (_to_codes, _to_act):
+        assert (run(x, y, post_norm=F.NORM_LAYER, pre_norm=F.NORM_NONE)[0] == 0).all()
