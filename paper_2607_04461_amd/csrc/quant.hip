@@ -377,14 +377,13 @@ enum { SEAM_NONE = 0, SEAM_ACT = 1, SEAM_I8 = 2 };
 template <typename T, int TR, int NV, bool TAIL, int OUT, bool NT, bool FULL>
 __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArgs a) {
   using R = Row<TR>;
-  using V = std::conditional_t<OUT == SEAM_I8, double, float>;   // of the elements
+  using V = std::conditional_t<OUT == SEAM_I8, double, float>;   // of the outputs
   __shared__ double part[2 * R::WAVES][2], tops[R::WAVES];
   const int64_t row = R::index();
   if (row >= M) return;
   const int D = a.D;   // elements past it (TAIL) take no branches: they stand at the pivot in the sums, and at zero in the end
   const float *xr = a.x + row * D;
   const T *yr = (const T *)a.y + row * D;
-  const V alpha = (V)a.alpha;
   float h[NV][8];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -418,7 +417,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
       }
     }
     if (a.post != NORM_NONE) row_sums<TR>(sum, sq, part);
-    const Norm<V> norm(a.post, pivot, sum, sq, D, a.eps);
+    const Norm<double> norm(a.post, pivot, sum, sq, D, a.eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
@@ -429,7 +428,8 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        h[i][j] = (float)fma((V)gate[j] * (V)gain[j], norm(y[i][j]), alpha * (V)h[i][j]);
+        // in 64 bits whatever comes of h, so that the stream does not depend on that: the first and the last product are exact
+        h[i][j] = (float)fma((double)gate[j] * (double)gain[j], norm(y[i][j]), (double)a.alpha * (double)h[i][j]);
       }
     }
   } else {

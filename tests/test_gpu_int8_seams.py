@@ -100,3 +100,34 @@ def test_a_constant_branch_adds_nothing(M, D):
     x, y = torch.zeros(M, D, device="cuda"), _dev(np.repeat(c[:, None], D, 1))
     for run in (_to_codes, _to_act):
         assert (run(x, y, post_norm=F.NORM_LAYER, pre_norm=F.NORM_NONE)[0] == 0).all()
+
+
+# ------------------------------------------------------------------------------------- the stream's rounding
+@pytest.mark.parametrize("y,gain,gate", [(1e-30, 1e30, 1e30), (1e30, 1e-30, 1e-30), (1e30, 1e30, 1e-30), (1e-30, 1e-30, 1e30),
+                                         (1e-20, 1e30, -1e20)])
+def test_a_gate_and_a_gain_whose_product_no_fp32_holds(y, gain, gate):
+    D = 77
+    v = lambda c: _dev(np.full(D, c))  # noqa: E731
+    x = _dev(np.full((3, D), 1e-31))
+    rh, _ = o8.seam(_f64(x), np.full((3, D), np.float32(y)), 1.0, o8.NONE, _f64(v(gain)), _f64(v(gate)), o8.NONE, None, None, EPS)
+    for run in (_to_codes, _to_act):
+        h = run(x, _dev(np.full((3, D), y)), post_gain=v(gain), gate=v(gate), pre_norm=F.NORM_NONE)[0]
+        np.testing.assert_allclose(_f64(h), rh, rtol=1.001 * U)      # rounded once
+
+
+@pytest.mark.parametrize("post", [F.NORM_NONE, F.NORM_LAYER, F.NORM_RMS])
+@pytest.mark.parametrize("M,D", WIDTHS)
+@pytest.mark.parametrize("dtype", [F.BF16, F.FP32])
+def test_the_stored_stream_does_not_depend_on_the_output(M, D, dtype, post):
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, y = torch.randn(M, D, generator=g, device="cuda"), torch.randn(M, D, generator=g, device="cuda").to(ACT[dtype])
+    kw = dict(alpha=0.7, post_norm=post, post_gain=torch.randn(D, generator=g, device="cuda"),
+              gate=torch.randn(D, generator=g, device="cuda"))
+    alone = torch.empty_like(x)
+    F.flashbon_op_norm_residual(dtype, M, D, EPS, x, y, x_out=alone, **kw)
+    assert torch.equal(alone, _to_codes(x, y, dtype, **kw)[0])
+    assert torch.equal(alone, _to_act(x, y, dtype, **kw)[0])
+    kw = dict(alpha=0.7)
+    F.flashbon_op_norm_residual(dtype, M, D, EPS, x, x_out=alone, **kw)
+    assert torch.equal(alone, _to_codes(x, dtype=dtype, **kw)[0])
+    assert torch.equal(alone, _to_act(x, dtype=dtype, **kw)[0])
