@@ -345,16 +345,20 @@ template <> struct Norm<double> {   // the pivot comes off first: what equals it
   }
   __device__ __forceinline__ double operator()(float v) const { return fma((double)v - pivot, by, plus); }
 };
-template <> struct Norm<float> {   // the mean in two parts, so that it costs no digits of v - mean
-  float by, mean, rest;
+template <> struct Norm<float> {
+  // The mean in two parts, so that it costs no digits of v - mean.  Where the deviation is past 2^64, all in units of 2^64:
+  // v - mean may be past fp32's range there, and the reciprocal below it.
+  float by, unit = 1.f, mean, rest;
   __device__ __forceinline__ Norm(int kind, double pivot, double sum, double sq, int D, double eps) {
     const Norm<double> n(kind, pivot, sum, sq, D, eps);
-    const double m = kind == NORM_LAYER ? pivot + sum / (double)D : 0.0;
-    by = (float)n.by;
+    const bool wide = n.by < 0x1p-64;
+    const double m = (kind == NORM_LAYER ? pivot + sum / (double)D : 0.0) * (wide ? 0x1p-64 : 1.0);
+    if (wide) unit = 0x1p-64f;
+    by = (float)(wide ? n.by * 0x1p64 : n.by);
     mean = (float)m;
     rest = (float)(m - (double)mean);
   }
-  __device__ __forceinline__ float operator()(float v) const { return ((v - mean) - rest) * by; }
+  __device__ __forceinline__ float operator()(float v) const { return (fmaf(v, unit, -mean) - rest) * by; }
 };
 
 // Elements c .. c + 7 of a vector, or eight times `otherwise` for none.

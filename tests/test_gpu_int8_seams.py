@@ -131,3 +131,29 @@ def test_the_stored_stream_does_not_depend_on_the_output(M, D, dtype, post):
     F.flashbon_op_norm_residual(dtype, M, D, EPS, x, x_out=alone, **kw)
     assert torch.equal(alone, _to_codes(x, dtype=dtype, **kw)[0])
     assert torch.equal(alone, _to_act(x, dtype=dtype, **kw)[0])
+
+
+# --------------------------------------------------------------------------------- rows at the end of the range
+@pytest.mark.parametrize("D", [40, 1000, 2100])
+@pytest.mark.parametrize("dtype", [F.BF16, F.FP32])
+def test_norms_of_rows_at_the_end_of_the_range(D, dtype):
+    """Rows whose differences from their mean, or whose reciprocal standard deviation, no fp32 holds."""
+    r = np.random.default_rng(6)
+    x = np.empty((4, D), np.float32)
+    x[0] = np.where(np.arange(D) % 8 == 1, 3e38, -3e38)
+    x[1] = np.where(np.arange(D) % 2, 3e38, -3e38)
+    x[2] = 3e38 * r.uniform(0.5, 1, D)
+    x[3] = 1e-38 * r.standard_normal(D)
+    for pre, kind in ((F.NORM_LAYER, o8.LAYER), (F.NORM_RMS, o8.RMS)):
+        h, a = _to_act(_dev(x), dtype=dtype, pre_norm=pre)
+        assert torch.equal(h, _dev(x))
+        ref = o8.norm(x, kind, EPS)
+        # the output's rounding; of fp32 at most five more (the difference, the reciprocal, their product) and the mean's
+        v = x.astype(np.float64)
+        mean = v.mean(1, keepdims=True) if pre == F.NORM_LAYER else 0.0
+        rstd = 1 / np.sqrt(((v - mean) ** 2).mean(1, keepdims=True) + EPS)
+        # Below 2^-126 a type holds multiples of its smallest value alone, 2^-133 in bf16 and 2^-149 in fp32, and rounds by half
+        # of that at most: the outputs next to zero in the last row, and that row's mean, whose rounding rstd multiplies.
+        half, least = (2.0 ** -8, 2.0 ** -134) if dtype == F.BF16 else (U, 2.0 ** -150)
+        off = U * np.abs(mean) + 2.0 ** -150
+        assert (np.abs(_f64(a) - ref) <= (half + 5.1 * U) * 1.01 * np.abs(ref) + off * rstd + least).all()
