@@ -148,8 +148,9 @@ enum {
  * the modulated norm before the next block:
  *   h[m][d] = alpha x[m][d] + gate[d] (post_norm(y[m])[d] post_gain[d])         -> x_out (fp32)
  *   a[m][d] = pre_norm(h[m])[d] (1 + scale[d]) + shift[d]                        -> out (act), or q and q_scale
- * pre_norm reads h as it is rounded to fp32.  q and q_scale are what flashbon_op_quant_rows would make of a's exact
- * rows: statistics are held in 64 bits, and with q the values too, so the codes do not depend on the kernel's order.
+ * pre_norm reads h as it is rounded to fp32: once, from 64 bits, whatever else is asked for.  q and q_scale are what
+ * flashbon_op_quant_rows would make of a's rows, ties included: statistics are held in 64 bits, and with q the values too
+ * (a scale that fp32 does not hold counts as one that is not finite).  A row's bits do not depend on the other rows.
  * x: device fp32 [M][D]; y: device act [M][D], or NULL (no branch: h = alpha x; post_norm, post_gain and gate are
  * ignored); post_gain, gate, scale, shift: device fp32 [D], each may be NULL (gain and gate 1, scale and shift 0).
  * x_out: device fp32 [M][D], may be x itself, or NULL.  Of out (device act [M][D]) and q (device int8 [M][D], with

@@ -3,9 +3,8 @@
 //
 // A row v becomes q = nearest-even(v / s) with one scale s = max(max |v| / 127, 2^-126), rounded once to fp32.  The
 // nearest integer is decided exactly: for rows that come as numbers (k_quant_rows) on the quotient itself, for rows
-// that are computed (k_norm_residual) on values held in 64 bits.  So a code depends neither on the order in which a
-// row's sums were added nor on how many threads shared the row, and two launches that form the same row agree to the
-// bit.
+// that are computed (k_norm_residual) on values held in 64 bits.  A row's sums are added in one order, however many rows
+// a launch has, so that a row's bits do not depend on the other rows.
 #include <type_traits>
 
 #include "common.h"
@@ -310,13 +309,46 @@ hipError_t launch_quant_rows(ActType t, int M, int K, const void *x, int64_t x_r
 // twice as many waits: (16384, 5120) to activations 191, but (24960, 1536) 102 and (8192, 6144) 152 in place of 131.
 namespace {
 
-// The row's two sums, for all its threads.  part: LDS that this call alone uses, so that one barrier does.
-template <int TR> __device__ __forceinline__ void row_sums(double &a, double &b, double (*part)[2]) {
+// Rows of 513 to 2048 elements are on one wave, two or four, by the number of rows.  So that a row's bits are those it has among
+// few rows and among many, their sums are added in one order: chunks of 64 pieces one after another in each lane, then lanes.
+template <int TR, int NV> struct Sums {
+  static constexpr int CHUNKS = Row<TR>::WAVES * NV;
+  static constexpr bool BY_LANE = Row<TR>::WAVES > 1 && CHUNKS <= 4;
+  static constexpr int PARTS = BY_LANE ? 64 * CHUNKS : Row<TR>::WAVES;
+};
+// The row's two sums, for all its threads, from its pieces'.  part: LDS that this call alone uses, so that one barrier does.
+template <int TR, int NV>
+__device__ __forceinline__ void row_sums(const double (&sum)[NV], const double (&sq)[NV], double &a, double &b, double (*part)[2]) {
   using R = Row<TR>;
-  const auto sum = [](double p, double q) { return p + q; };
-  a = reduced<R::LANES>(a, sum);
-  b = reduced<R::LANES>(b, sum);
-  if constexpr (R::WAVES > 1) {
+  using S = Sums<TR, NV>;
+  const auto add = [](double p, double q) { return p + q; };
+  a = sum[0];
+  b = sq[0];
+  if constexpr (S::BY_LANE) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      part[64 * (R::WAVES * i + wave) + lane][0] = sum[i];
+      part[64 * (R::WAVES * i + wave) + lane][1] = sq[i];
+    }
+    __syncthreads();
+    a = part[lane][0];
+    b = part[lane][1];
+#pragma unroll
+    for (int c = 1; c < S::CHUNKS; ++c) {
+      a += part[64 * c + lane][0];
+      b += part[64 * c + lane][1];
+    }
+  } else {
+#pragma unroll
+    for (int i = 1; i < NV; ++i) {
+      a += sum[i];
+      b += sq[i];
+    }
+  }
+  a = reduced<R::LANES>(a, add);
+  b = reduced<R::LANES>(b, add);
+  if constexpr (R::WAVES > 1 && !S::BY_LANE) {
     if ((threadIdx.x & 63) == 0) {
       part[threadIdx.x >> 6][0] = a;
       part[threadIdx.x >> 6][1] = b;
@@ -382,7 +414,8 @@ template <typename T, int TR, int NV, bool TAIL, int OUT, bool NT, bool FULL>
 __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArgs a) {
   using R = Row<TR>;
   using V = std::conditional_t<OUT == SEAM_I8, double, float>;   // of the outputs
-  __shared__ double part[2 * R::WAVES][2], tops[R::WAVES];
+  constexpr int PARTS = Sums<TR, NV>::PARTS;
+  __shared__ __attribute__((aligned(16))) double part[2 * PARTS][2], tops[R::WAVES];
   const int64_t row = R::index();
   if (row >= M) return;
   const int D = a.D;   // elements past it (TAIL) take no branches: they stand at the pivot in the sums, and at zero in the end
@@ -406,7 +439,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
   if (a.y) {
     Piece<T> y[NV];
     const double pivot = a.post == NORM_LAYER ? (double)to_f32(yr[0]) : 0.0;
-    double sum = 0, sq = 0;
+    double sums[NV] = {}, sqs[NV] = {}, sum = 0, sq = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 8 * (R::lane() + TR * i);
@@ -416,11 +449,11 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const double d = (double)(TAIL && c + j >= D ? (float)pivot : y[i][j]) - pivot;
-        sum += d;
-        sq = fma(d, d, sq);
+        sums[i] += d;
+        sqs[i] = fma(d, d, sqs[i]);
       }
     }
-    if (a.post != NORM_NONE) row_sums<TR>(sum, sq, part);
+    if (a.post != NORM_NONE) row_sums<TR, NV>(sums, sqs, sum, sq, part);
     const Norm<double> norm(a.post, pivot, sum, sq, D, a.eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -450,7 +483,7 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
     }
   }
   if constexpr (OUT != SEAM_NONE) {
-    double pivot = 0, sum = 0, sq = 0;
+    double pivot = 0, sums[NV] = {}, sqs[NV] = {}, sum = 0, sq = 0;
     V v[NV][8], top = 0;
     if (a.pre == NORM_LAYER) {
       // the row's first element: of its first lane, for rows of several waves through LDS (read by all at the sums' barrier)
@@ -470,11 +503,11 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const double d = (double)(TAIL && c + j >= D ? (float)pivot : h[i][j]) - pivot;
-        sum += d;
-        sq = fma(d, d, sq);
+        sums[i] += d;
+        sqs[i] = fma(d, d, sqs[i]);
       }
     }
-    if (a.pre != NORM_NONE) row_sums<TR>(sum, sq, part + R::WAVES);
+    if (a.pre != NORM_NONE) row_sums<TR, NV>(sums, sqs, sum, sq, part + PARTS);
     const Norm<V> norm(a.pre, pivot, sum, sq, D, a.eps);
     bool bad = false;
 #pragma unroll

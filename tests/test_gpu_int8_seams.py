@@ -157,3 +157,25 @@ def test_norms_of_rows_at_the_end_of_the_range(D, dtype):
         half, least = (2.0 ** -8, 2.0 ** -134) if dtype == F.BF16 else (U, 2.0 ** -150)
         off = U * np.abs(mean) + 2.0 ** -150
         assert (np.abs(_f64(a) - ref) <= (half + 5.1 * U) * 1.01 * np.abs(ref) + off * rstd + least).all()
+
+
+# --------------------------------------------------------------------------------------- many rows and few
+@pytest.mark.parametrize("D", [520, 1000, 1024, 1025, 1536, 1537, 1999, 2048])
+@pytest.mark.parametrize("norm", [F.NORM_LAYER, F.NORM_RMS])
+def test_a_rows_bits_are_the_same_among_many_rows_and_few(D, norm):
+    """The stream is what a rounding to fp32 leaves of the branch's norm, so that it shows the last bits of the norm's 64."""
+    r = np.random.default_rng(7)
+    y = r.standard_normal((700, D)).astype(np.float32)
+    x = o8.norm(y, {F.NORM_LAYER: o8.LAYER, F.NORM_RMS: o8.RMS}[norm], EPS)
+    tx, ty = _dev(x), _dev(y)
+
+    def run(m0, m1):
+        return _to_codes(tx[m0:m1], ty[m0:m1], alpha=-1.0, post_norm=norm, pre_norm=F.NORM_LAYER)
+
+    many = run(0, 700)
+    for m0, m1 in ((0, 500), (500, 700), (333, 334)):
+        for whole, part in zip(many, run(m0, m1)):
+            assert torch.equal(whole[m0:m1], part) if torch.is_tensor(part) else np.array_equal(whole[m0:m1], part)
+    a = _to_act(tx, ty, alpha=-1.0, post_norm=norm, pre_norm=F.NORM_LAYER)
+    b = _to_act(tx[:500], ty[:500], alpha=-1.0, post_norm=norm, pre_norm=F.NORM_LAYER)
+    assert all(torch.equal(p[:500], q) for p, q in zip(a, b))
