@@ -558,9 +558,9 @@ def _raw_stream(stream, device: int) -> int:
 
 
 def _int32(*sizes) -> None:
-    """Refuses sizes that the ABI's 32-bit integers would wrap."""
-    if max(sizes) > 0x7FFFFFFF:
-        raise ValueError(f"sizes must be below 2^31, got {sizes}")
+    """Refuses integers that the ABI's 32 bits would wrap."""
+    if max(sizes) > 0x7FFFFFFF or min(sizes) < -0x80000000:
+        raise ValueError(f"integers must be below 2^31 in magnitude, got {sizes}")
 
 
 def _pointers(device: Optional[int], *wanted) -> list:
@@ -619,7 +619,7 @@ def validate_linear_i8(dtype, M, N, K, A, a_scale, W, w_scale, bias, epilogue, o
     """Raise ValueError unless the tensors are what flashbon_op_linear_i8 reads and writes; their addresses."""
     act, device = _act(dtype), _current_device(require_device)
     i8, f32 = _torch.int8, _torch.float32
-    _int32(M, N, K)
+    _int32(M, N, K, epilogue)
     found = _pointers(device, ("A", A, i8, M * K, True), ("a_scale", a_scale, f32, M, True), ("W", W, i8, N * K, True),
                       ("w_scale", w_scale, f32, N, True), ("bias", bias, f32, N, False),
                       ("out", out, act if epilogue == EPI_STORE or epilogue == EPI_GELU else f32, M * N, True))
