@@ -592,6 +592,8 @@ def validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale, *, require_devic
     _int32(M, K)
     if M < 1 or K < 1 or x_row_stride < K:
         raise ValueError(f"need M, K >= 1 and a row stride of at least K, got {M}, {K}, {x_row_stride}")
+    if x is None:
+        raise ValueError("x is required")
     if x.dtype is not act:
         raise ValueError(f"x must be {act}, got {x.dtype}")
     if x.is_contiguous():
@@ -608,7 +610,7 @@ def validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale, *, require_devic
 def flashbon_op_quant_rows(dtype, M, K, x, q, scale, x_row_stride=None, stream=None):
     """Rows x [M][K] to int8 codes q and one scale a row; ``x_row_stride`` in elements (None: a matrix's own, else K)."""
     if x_row_stride is None:
-        x_row_stride = int(x.stride(0)) if x.dim() == 2 and x.shape[0] > 1 else K
+        x_row_stride = int(x.stride(0)) if x is not None and x.dim() == 2 and x.shape[0] > 1 else K
     px, pq, ps = validate_quant_rows(dtype, M, K, x, x_row_stride, q, scale)
     _check(load().flashbon_op_quant_rows(dtype, M, K, px, x_row_stride, pq, ps, _raw_stream(stream, x.get_device())),
            "flashbon_op_quant_rows")

@@ -35,3 +35,18 @@ def test_an_epilogue_that_would_wrap_is_refused(epilogue):
     with pytest.raises(ValueError, match="2\\^31"):
         fb.validate_linear_i8(BF, 3, 4, 8, _t((3, 8), I8), _t(3, F), _t((4, 8), I8), _t(4, F), None, epilogue, _t((3, 4), F),
                               require_device=False)
+
+
+@pytest.mark.parametrize("missing", ["x", "q", "scale"])
+def test_rows_need_their_tensors(missing):
+    a = dict(x=_t((3, 8), B), q=_t((3, 8), I8), scale=_t(3, F))
+    a[missing] = None
+    with pytest.raises(ValueError, match=f"{missing} is required"):
+        fb.validate_quant_rows(BF, 3, 8, a["x"], 8, a["q"], a["scale"], require_device=False)
+
+
+@pytest.mark.parametrize("stride", [None, 8])
+def test_a_call_without_rows_is_refused(stride, monkeypatch):
+    monkeypatch.setattr(fb, "_current_device", lambda require_device: None)
+    with pytest.raises(ValueError, match="x is required"):
+        fb.flashbon_op_quant_rows(BF, 3, 8, None, _t((3, 8), I8), _t(3, F), x_row_stride=stride)
