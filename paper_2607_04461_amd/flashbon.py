@@ -553,8 +553,10 @@ def _current_device(require_device: bool) -> Optional[int]:
 
 
 def _raw_stream(stream, device: int) -> int:
-    """``stream``, or torch's current one on ``device`` (its address alone: a tenth of the time of a Stream object)."""
-    return int(stream) if stream is not None else _torch._C._cuda_getCurrentRawStream(device)
+    """``_stream`` on ``device``, the current one: torch's call for the address alone, which is no public one, takes a tenth
+    of the time of a Stream object; without it the public one."""
+    raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None) if stream is None else None
+    return raw(device) if raw is not None else _stream(stream)
 
 
 def _int32(*sizes) -> None:

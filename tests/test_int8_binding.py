@@ -50,3 +50,11 @@ def test_a_call_without_rows_is_refused(stride, monkeypatch):
     monkeypatch.setattr(fb, "_current_device", lambda require_device: None)
     with pytest.raises(ValueError, match="x is required"):
         fb.flashbon_op_quant_rows(BF, 3, 8, None, _t((3, 8), I8), _t(3, F), x_row_stride=stride)
+
+
+def test_the_stream_where_torch_lacks_the_short_way_to_it(monkeypatch):
+    fb._with_torch()
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(fb, "_stream", lambda stream: 4321 if stream is None else int(stream))
+    assert fb._raw_stream(None, 0) == 4321
+    assert fb._raw_stream(77, 0) == 77
