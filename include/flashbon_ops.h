@@ -120,7 +120,7 @@ flashbon_status flashbon_op_unpatch_sde(int32_t n, int32_t C, int32_t H, int32_t
  * whose maximum is not finite gets scale NaN and codes 0, so that every output made of it is NaN.
  * x: device, act of `dtype`, row m at x + m * x_row_stride (elements, >= K): activations [M][K], a slice of fused rows,
  * or the weights [N][K] of a layer (then the scale is one of an output channel).  q: device [M][K] dense, scale: device
- * fp32 [M]; neither may overlap x.  M >= 1, 1 <= K <= 65536. */
+ * fp32 [M]; neither may overlap x's rows or the other (FLASHBON_EINVAL).  M >= 1, 1 <= K <= 65536. */
 flashbon_status flashbon_op_quant_rows(int32_t dtype, int32_t M, int32_t K, const void *x, int64_t x_row_stride,
                                        int8_t *q, float *scale, void *stream);
 
@@ -131,7 +131,8 @@ flashbon_status flashbon_op_quant_rows(int32_t dtype, int32_t M, int32_t K, cons
  * A: device int8 [M][K], W: device int8 [N][K], dense (every value from -128 to 127 is taken); a_scale: device fp32 [M];
  * w_scale: device fp32 [N]; bias, gate, cache_out, out as in flashbon_op_linear, act of `dtype` where the epilogue
  * stores act; residual_in: device fp32 [M][N], read only, out itself or disjoint from it.  gate, residual_in and
- * cache_out are for FLASHBON_EPI_RESIDUAL and ignored by the others; cache_out must not overlap anything else.
+ * cache_out are for FLASHBON_EPI_RESIDUAL and ignored by the others; out and cache_out must not otherwise overlap an input
+ * or each other (FLASHBON_EINVAL).
  * M >= 1, 1 <= N <= 2^20, 1 <= K <= 65536. */
 flashbon_status flashbon_op_linear_i8(int32_t dtype, int32_t M, int32_t N, int32_t K, const int8_t *A,
                                       const float *a_scale, const int8_t *W, const float *w_scale, const float *bias,
@@ -154,8 +155,8 @@ enum {
  * x: device fp32 [M][D]; y: device act [M][D], or NULL (no branch: h = alpha x; post_norm, post_gain and gate are
  * ignored); post_gain, gate, scale, shift: device fp32 [D], each may be NULL (gain and gate 1, scale and shift 0).
  * x_out: device fp32 [M][D], may be x itself, or NULL.  Of out (device act [M][D]) and q (device int8 [M][D], with
- * q_scale device fp32 [M]) at most one is given; at least one of x_out, out and q.  Outputs must not overlap inputs
- * otherwise.  alpha finite, eps positive and finite.  M >= 1, 1 <= D <= 6144. */
+ * q_scale device fp32 [M]) at most one is given; at least one of x_out, out and q.  Outputs must not otherwise overlap
+ * inputs or each other (FLASHBON_EINVAL).  alpha finite, eps positive and finite.  M >= 1, 1 <= D <= 6144. */
 flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, float eps, const float *x, float alpha,
                                           const void *y, int32_t post_norm, const float *post_gain, const float *gate,
                                           float *x_out, int32_t pre_norm, const float *shift, const float *scale,

@@ -3,6 +3,7 @@
 
 #include <climits>
 #include <cmath>
+#include <initializer_list>
 #include <string>
 
 #include "../../include/flashbon_ops.h"
@@ -16,6 +17,36 @@ static flashbon_status launched(hipError_t e, const char *what) {
   if (e != hipSuccess) return fail(FLASHBON_EHIP, std::string(what) + ": " + hipGetErrorString(e));
   return FLASHBON_OK;
 }
+
+namespace {
+
+// A buffer of a call: rows of `bytes` each, `pitch` apart (one row: any).  A null address is none.
+struct Span {
+  const void *at;
+  size_t bytes;
+  size_t rows = 1, pitch = 0;
+};
+// Whether one row of a and the one row of b share a byte.
+bool overlap(const Span &a, const Span &b) {
+  if (!a.at || !b.at) return false;
+  // rows m with m pitch < hi and m pitch + bytes > lo
+  const __int128 lo = (__int128)(uintptr_t)b.at - (uintptr_t)a.at, hi = lo + b.bytes, pitch = a.rows > 1 ? a.pitch : 1;
+  if (hi <= 0) return false;
+  const __int128 past = lo - (__int128)a.bytes, first = past < 0 ? 0 : past / pitch + 1, last = (hi - 1) / pitch;
+  return first <= last && first < (__int128)a.rows;
+}
+// Whether an output shares a byte with an input or with another output.
+bool overlaps(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
+  for (const Span *o = outputs.begin(); o != outputs.end(); ++o) {
+    for (const Span *p = o + 1; p != outputs.end(); ++p)
+      if (overlap(*p, *o)) return true;
+    for (const Span &i : inputs)
+      if (overlap(i, *o)) return true;
+  }
+  return false;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -159,6 +190,9 @@ flashbon_status flashbon_op_quant_rows(int32_t dtype, int32_t M, int32_t K, cons
   if (M < 1 || K < 1 || K > 65536) return fail(FLASHBON_ESHAPE, "need M, K >= 1 and K <= 65536");
   if (x_row_stride < K) return fail(FLASHBON_ESHAPE, "x_row_stride must be at least K");
   if (!x || !q || !scale) return fail(FLASHBON_EINVAL, "x, q and scale are required");
+  const size_t rows = M, es = dtype == FLASHBON_BF16 ? 2 : 4;
+  if (overlaps({{q, rows * K}, {scale, 4 * rows}}, {{x, K * es, rows, (size_t)x_row_stride * es}}))
+    return fail(FLASHBON_EINVAL, "q and scale must not overlap x or each other");
   ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
   return launched(launch_quant_rows(t, M, K, x, x_row_stride, q, scale, (hipStream_t)stream), "quant_rows");
 }
@@ -172,11 +206,17 @@ flashbon_status flashbon_op_linear_i8(int32_t dtype, int32_t M, int32_t N, int32
     return fail(FLASHBON_ESHAPE, "need M, N, K >= 1, N <= 2^20 and K <= 65536");
   if (!A || !a_scale || !W || !w_scale || !out) return fail(FLASHBON_EINVAL, "A, a_scale, W, w_scale and out are required");
   if (epilogue < FLASHBON_EPI_STORE || epilogue > FLASHBON_EPI_RESIDUAL) return fail(FLASHBON_EINVAL, "bad epilogue");
+  const bool residual = epilogue == FLASHBON_EPI_RESIDUAL;
+  const size_t m = M, n = N, outs = m * n * (dtype == FLASHBON_BF16 && epilogue <= FLASHBON_EPI_GELU ? 2 : 4);
+  if (overlaps({{out, outs}, {residual ? cache_out : nullptr, outs}},
+               {{A, m * K}, {a_scale, 4 * m}, {W, n * K}, {w_scale, 4 * n}, {bias, 4 * n}, {residual ? gate : nullptr, 4 * n},
+                {residual && residual_in != out ? residual_in : nullptr, outs}}))
+    return fail(FLASHBON_EINVAL, "out and cache_out must not overlap an input (but out residual_in, which it may be) or each other");
   I8Args g;
   g.A = A; g.W = W; g.a_scale = a_scale; g.w_scale = w_scale;
   EpiArgs e;
   e.out = out; e.ldo = N; e.bias = bias;
-  if (epilogue == FLASHBON_EPI_RESIDUAL) {
+  if (residual) {
     e.gate = gate; e.cache = cache_out;
     if (residual_in != out) e.res_in = residual_in;
   }
@@ -199,6 +239,11 @@ flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, f
     return fail(FLASHBON_EINVAL, "bad norm");
   if (!(eps > 0.f) || !std::isfinite(eps)) return fail(FLASHBON_EINVAL, "eps must be positive and finite");
   if (!std::isfinite(alpha)) return fail(FLASHBON_EINVAL, "alpha must be finite");
+  const size_t m = M, d = D, es = dtype == FLASHBON_BF16 ? 2 : 4;
+  if (overlaps({{x_out, 4 * m * d}, {out, m * d * es}, {q, m * d}, {q_scale, 4 * m}},
+               {{x == x_out ? nullptr : x, 4 * m * d}, {y, m * d * es}, {y ? post_gain : nullptr, 4 * d}, {y ? gate : nullptr, 4 * d},
+                {shift, 4 * d}, {scale, 4 * d}}))
+    return fail(FLASHBON_EINVAL, "outputs must not overlap an input (but x_out x, which it may be) or each other");
   SeamArgs a;
   a.D = D; a.post = post_norm; a.pre = pre_norm; a.alpha = alpha; a.eps = eps;
   a.x = x; a.y = y; a.gain = post_gain; a.gate = gate; a.scale = scale; a.shift = shift;
