@@ -574,8 +574,8 @@ static hipError_t norm_rows(int M, const SeamArgs &a, hipStream_t s) {
   // a stream of 64 MiB and more is stored non-temporally: nothing reads it soon ((24960, 1536) to codes 105 -> 101 us,
   // (16384, 5120) to activations 224 -> 219); a smaller one the next kernel may still find in the caches
   const bool nt = a.x_out && (size_t)M * a.D * 4 >= (size_t)64 << 20;
-  // on more threads it gained nothing: (1560, 4096) to codes 20.6 us and 21.3, but to activations 18.8 and 18.2
-  constexpr bool FULL = NV > 1 && TR < 256;
+  // on 256 threads it gained nothing: (1560, 4096) to codes 20.6 us and 21.3, but to activations 18.8 and 18.2
+  constexpr bool FULL = NV > 1 && TR <= 128;
   const bool full = FULL && a.D == 8 * TR * NV;
   const auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, s, M, a); };
   if (a.D % 8) go(k_norm_residual<T, TR, NV, true, OUT, false, false>);
