@@ -357,13 +357,12 @@ __device__ __forceinline__ void tile_of(int bid, int MT, int NT, int group, int 
 
 // A wave's accumulators acc[i][j] hold row mbase + 16 j + fr and columns nbase + 32 (i / 2) + 8 fq + 4 (i % 2) .. + 3.
 // They leave through the freed ring, so that every global access covers whole rows of the wave's tile: bf16 outputs as
-// bf16 rows of 16 WT columns, fp32 ones as rows of 32 columns, one column group after another; in P parts of the rows,
-// where `lds` holds no more.  A wave has a region of its own there, in which its accesses are in order.
-template <int EPI, typename TO, int WTA, int WT, int P, int POL>
+// bf16 rows of 16 WT columns, fp32 ones as rows of 32 columns, one column group after another.  A wave has a region of its
+// own there, in which its accesses are in order.
+template <int EPI, typename TO, int WTA, int WT, int POL>
 __device__ __forceinline__ void epilogue(const I8Args &g, const EpiArgs &e, const i32x4 (&acc)[WT][WTA], int M, int N,
                                          int mbase, int nbase, int fr, int fq, int lane, int wave, char *lds) {
-  constexpr int WP = WTA / P, R = 16 * WP, CG = WT / 2;
-  static_assert(WTA % P == 0, "parts");
+  constexpr int R = 16 * WTA, CG = WT / 2;
   constexpr bool NARROW = (EPI == EPI_STORE || EPI == EPI_GELU) && sizeof(TO) == 2;
   constexpr uint32_t ES = NARROW ? 2u : 4u;
   char *wl = lds + wave * (NARROW ? R * 32 * WT : R * 128);
@@ -395,30 +394,26 @@ __device__ __forceinline__ void epilogue(const I8Args &g, const EpiArgs &e, cons
     // a buffer is below 2^30 bytes: an offset out of range stays there with a row's offset added
     const uint32_t o0 = n < N ? (uint32_t)rr * (uint32_t)e.ldo * 2u + (uint32_t)n * 2u : OUT_OF_RANGE;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
+    for (int cg = 0; cg < CG; ++cg)
 #pragma unroll
-      for (int cg = 0; cg < CG; ++cg)
+      for (int j = 0; j < WTA; ++j) {
+        auto value = [&](int q) {
+          const float v = scaled(acc[2 * cg + (q >> 2)][j][q & 3], ws[cg][q >> 2][q & 3], as[j], bias[cg][q >> 2][q & 3]);
+          return EPI == EPI_GELU ? gelu_tanh(v) : v;
+        };
+        typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        u32x4 w;   // by pairs: one conversion each, and no moves between them
 #pragma unroll
-        for (int j = 0; j < WP; ++j) {
-          auto value = [&](int q) {
-            const float v = scaled(acc[2 * cg + (q >> 2)][WP * p + j][q & 3], ws[cg][q >> 2][q & 3], as[WP * p + j],
-                                   bias[cg][q >> 2][q & 3]);
-            return EPI == EPI_GELU ? gelu_tanh(v) : v;
-          };
-          typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
-          u32x4 w;   // by pairs: one conversion each, and no moves between them
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float lo = value(2 * q), hi = value(2 * q + 1);
-            w[q] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)lo, (bf16)hi});
-          }
-          *reinterpret_cast<u32x4 *>(wl + place(16 * j + fr, 4 * cg + fq)) = w;
+        for (int q = 0; q < 4; ++q) {
+          const float lo = value(2 * q), hi = value(2 * q + 1);
+          w[q] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)lo, (bf16)hi});
         }
-#pragma unroll
-      for (int t = 0; t < R / RI; ++t) {
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(wl + place(RI * t + rr, k));
-        __builtin_amdgcn_raw_buffer_store_b128(v, rsO, o0 + (uint32_t)(R * p + RI * t) * (uint32_t)e.ldo * 2u, 0, POL);
+        *reinterpret_cast<u32x4 *>(wl + place(16 * j + fr, 4 * cg + fq)) = w;
       }
+#pragma unroll
+    for (int t = 0; t < R / RI; ++t) {
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(wl + place(RI * t + rr, k));
+      __builtin_amdgcn_raw_buffer_store_b128(v, rsO, o0 + (uint32_t)(RI * t) * (uint32_t)e.ldo * 2u, 0, POL);
     }
   } else {
     constexpr int NTR = R / 8, B = NTR % 4 == 0 ? 4 : 2, NB = NTR / B;   // read-back instructions a column group, in batches of B
@@ -436,43 +431,39 @@ __device__ __forceinline__ void epilogue(const I8Args &g, const EpiArgs &e, cons
       const uint32_t o0 = n < N ? (uint32_t)rr * (uint32_t)e.ldo * 4u + (uint32_t)n * 4u : OUT_OF_RANGE;
       f32x4 gate = {1.f, 1.f, 1.f, 1.f}, h[2][B];
       if (EPI == EPI_RESIDUAL && e.gate) gate = ld4(rsG, n < N ? (uint32_t)n * 4u : OUT_OF_RANGE);
+      auto fetch = [&](int bt) {
+        if constexpr (EPI == EPI_RESIDUAL) {
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const uint32_t op = o0 + (uint32_t)(R * p) * (uint32_t)e.ldo * 4u;
-        auto fetch = [&](int bt) {
+          for (int i = 0; i < B; ++i) h[bt & 1][i] = ld4(rsI, o0 + (uint32_t)(B * bt + i) * step);
+        }
+      };
+      fetch(0);
+#pragma unroll
+      for (int j = 0; j < WTA; ++j)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          f32x4 v;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            v[q] = scaled(acc[2 * cg + hf][j][q], ws[hf][q], as[j], bias[hf][q]);
+            if constexpr (EPI == EPI_GELU) v[q] = gelu_tanh(v[q]);
+          }
+          const int r = 16 * j + fr, kk = 2 * fq + hf;
+          *reinterpret_cast<f32x4 *>(wl + r * 128 + ((kk ^ ((r >> 1) & 7)) << 4)) = v;
+        }
+#pragma unroll
+      for (int bt = 0; bt < NB; ++bt) {
+        if (bt + 1 < NB) fetch(bt + 1);
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+          const int t = B * bt + i, r = 8 * t + rr;
+          f32x4 v = *reinterpret_cast<const f32x4 *>(wl + r * 128 + ((k ^ ((r >> 1) & 7)) << 4));
           if constexpr (EPI == EPI_RESIDUAL) {
 #pragma unroll
-            for (int i = 0; i < B; ++i) h[bt & 1][i] = ld4(rsI, op + (uint32_t)(B * bt + i) * step);
+            for (int q = 0; q < 4; ++q) v[q] = fmaf(gate[q], v[q], h[bt & 1][i][q]);
           }
-        };
-        fetch(0);
-#pragma unroll
-        for (int j = 0; j < WP; ++j)
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            f32x4 v;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              v[q] = scaled(acc[2 * cg + hf][WP * p + j][q], ws[hf][q], as[WP * p + j], bias[hf][q]);
-              if constexpr (EPI == EPI_GELU) v[q] = gelu_tanh(v[q]);
-            }
-            const int r = 16 * j + fr, kk = 2 * fq + hf;
-            *reinterpret_cast<f32x4 *>(wl + r * 128 + ((kk ^ ((r >> 1) & 7)) << 4)) = v;
-          }
-#pragma unroll
-        for (int bt = 0; bt < NB; ++bt) {
-          if (bt + 1 < NB) fetch(bt + 1);
-#pragma unroll
-          for (int i = 0; i < B; ++i) {
-            const int t = B * bt + i, r = 8 * t + rr;
-            f32x4 v = *reinterpret_cast<const f32x4 *>(wl + r * 128 + ((k ^ ((r >> 1) & 7)) << 4));
-            if constexpr (EPI == EPI_RESIDUAL) {
-#pragma unroll
-              for (int q = 0; q < 4; ++q) v[q] = fmaf(gate[q], v[q], h[bt & 1][i][q]);
-            }
-            st4<POL>(rsO, op + (uint32_t)t * step, v);
-            if (EPI == EPI_RESIDUAL && e.cache) st4<POL>(rsC, op + (uint32_t)t * step, v);
-          }
+          st4<POL>(rsO, o0 + (uint32_t)t * step, v);
+          if (EPI == EPI_RESIDUAL && e.cache) st4<POL>(rsC, o0 + (uint32_t)t * step, v);
         }
       }
     }
@@ -587,7 +578,7 @@ __device__ __forceinline__ void tile(int M, int N, int K, const I8Args &g, const
   substep(T_{}, F_{}, F_{}, fw0, fa0, st, 1, fw1, fa1, 0, 0);
   substep(F_{}, F_{}, F_{}, fw1, fa1, 0, 0, fw0, fa0, 0, 0);
   static_assert(8 * 16 * WTA * 128 <= NST * STAGE, "the ring holds the waves' rows");
-  epilogue<EPI, TO, WTA, WT, 1, POL>(g, e, acc, M, N, m0 + 16 * WTA * wm, n0 + 16 * WT * wn, fr, fq, lane, wave, smem);
+  epilogue<EPI, TO, WTA, WT, POL>(g, e, acc, M, N, m0 + 16 * WTA * wm, n0 + 16 * WT * wn, fr, fq, lane, wave, smem);
 }
 
 }  // namespace ring
