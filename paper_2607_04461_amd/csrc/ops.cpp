@@ -246,7 +246,8 @@ flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, f
     return fail(FLASHBON_EINVAL, "outputs must not overlap an input (but x_out x, which it may be) or each other");
   SeamArgs a;
   a.D = D; a.post = post_norm; a.pre = pre_norm; a.alpha = alpha; a.eps = eps;
-  a.x = x; a.y = y; a.gain = post_gain; a.gate = gate; a.scale = scale; a.shift = shift;
+  a.x = x; a.y = y; a.scale = scale; a.shift = shift;
+  a.gain = y ? post_gain : nullptr; a.gate = y ? gate : nullptr;   // ignored without a branch: kernels may read what is not null
   a.x_out = x_out; a.out = out; a.q = q; a.q_scale = q_scale;
   ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
   return launched(launch_norm_residual(t, M, a, (hipStream_t)stream), "norm_residual");

@@ -179,3 +179,20 @@ def test_a_rows_bits_are_the_same_among_many_rows_and_few(D, norm):
     a = _to_act(tx, ty, alpha=-1.0, post_norm=norm, pre_norm=F.NORM_LAYER)
     b = _to_act(tx[:500], ty[:500], alpha=-1.0, post_norm=norm, pre_norm=F.NORM_LAYER)
     assert all(torch.equal(p[:500], q) for p, q in zip(a, b))
+
+
+# ------------------------------------------------------------------------------------ vectors of no branch
+@pytest.mark.parametrize("M,D", [(FEW, 40), (FEW, 500), (FEW, 1536), (MANY, 1536), (FEW, 5003)])
+def test_a_branchs_vectors_are_ignored_without_one(M, D):
+    """The library's call with the addresses of one element each: nothing of them is to be read, where y is null."""
+    import ctypes
+
+    p = lambda t: ctypes.c_void_p(t.data_ptr())  # noqa: E731
+    x, one = torch.randn(M, D, device="cuda"), torch.full((1,), float("nan"), device="cuda")
+    h, a, ref = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    F.flashbon_op_norm_residual(F.FP32, M, D, EPS, x, alpha=0.5, out=ref)
+    status = F.load().flashbon_op_norm_residual(F.FP32, M, D, EPS, p(x), 0.5, None, F.NORM_LAYER, p(one), p(one), p(h),
+                                                F.NORM_LAYER, None, None, p(a), None, None,
+                                                ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    assert status == F.OK and torch.equal(h, 0.5 * x) and torch.equal(a, ref)
