@@ -29,11 +29,13 @@ struct Span {
 // Whether one row of a and the one row of b share a byte.
 bool overlap(const Span &a, const Span &b) {
   if (!a.at || !b.at) return false;
+  const uintptr_t p = (uintptr_t)a.at, q = (uintptr_t)b.at;
+  if (q + b.bytes <= p || p + (a.rows - 1) * a.pitch + a.bytes <= q) return false;
+  if (a.rows == 1) return true;
   // rows m with m pitch < hi and m pitch + bytes > lo
-  const __int128 lo = (__int128)(uintptr_t)b.at - (uintptr_t)a.at, hi = lo + b.bytes, pitch = a.rows > 1 ? a.pitch : 1;
-  if (hi <= 0) return false;
-  const __int128 past = lo - (__int128)a.bytes, first = past < 0 ? 0 : past / pitch + 1, last = (hi - 1) / pitch;
-  return first <= last && first < (__int128)a.rows;
+  const int64_t lo = (int64_t)(q - p), hi = lo + (int64_t)b.bytes, past = lo - (int64_t)a.bytes, pitch = (int64_t)a.pitch;
+  const int64_t first = past < 0 ? 0 : past / pitch + 1, last = (hi - 1) / pitch;
+  return first <= last && first < (int64_t)a.rows;
 }
 // Whether an output shares a byte with an input or with another output.
 bool overlaps(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
