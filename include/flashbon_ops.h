@@ -108,7 +108,8 @@ flashbon_status flashbon_op_unpatch_sde(int32_t n, int32_t C, int32_t H, int32_t
                                         const float *v, float *z, float t_cur, float t_next, float a,
                                         uint64_t seed, int32_t step, int32_t row0, void *stream);
 
-/* ---- 8-bit layers: drafts are only ranked, and may take their linear layers in 8-bit integers.  A DiT branch runs as
+/* ---- 8-bit layers, for drafts: they are only ranked, and a caller who finds that the ranking bears it may take their
+ * linear layers in 8-bit integers (flashbon_draft_step itself does not).  A DiT branch runs as
  *   flashbon_op_norm_residual (int8 rows of the modulated norm) -> flashbon_op_linear_i8 (GELU) ->
  *   flashbon_op_quant_rows -> flashbon_op_linear_i8 -> flashbon_op_norm_residual (the next branch's rows),
  * on weights that flashbon_op_quant_rows made once.  There is no training path, as in the rest of the library.

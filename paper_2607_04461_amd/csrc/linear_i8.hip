@@ -701,7 +701,7 @@ namespace {
 constexpr int kStoreNT = 2;
 constexpr size_t kNTBytes = (size_t)64 << 20;
 // Rows of a launch: a grid of 512 threads for 256 outputs, the most a kernel takes, is within 2^32 threads and 2^16 rows
-// of workgroups.
+// of workgroups.  Larger tiles would take more; past 32768 rows they run as several launches all the same.
 int rows_per_launch(int N) { return std::min(1 << 15, (1 << 30) / N); }
 
 // Choice of kernel: estimates of a launch's device time in us, whole rounds of workgroups at a time, which stay within
@@ -712,6 +712,10 @@ int rows_per_launch(int N) { return std::min(1 << 15, (1 << 30) / N); }
 //     (24960, 1536, 1536) residual 148, 140, 136, 149; (24960, 1536, 8960) residual 394, 381, 410, 480; (4680, 1536,
 //     8960) 117, 75, 81, 97; (1560, 4608, 1536) 22, 16.4, 15.4, 18; (900, 7168, 512) 128x256 9.1, 128x128 8.3; (3120, 2304,
 //     768) GELU 12.8 and 11.5; (1560, 4608, 2048) 18.4 and 17.8, (3000, 2504, 3008) 27.6 and 30.3.
+//   * Row blocks of two heights, where they save a round: beside 256x256, 128x256 and two 128x128, (24960, 8960, 1536) GELU
+//     370, 374, 422, 401; (6240, 8960, 1536) GELU 97, 105, 112, 105; (3120, 8960, 1536) GELU 52, 54, 66, 58; (24960, 1536,
+//     8960) residual 364, 395, 382, 411; (12480, 1536, 8960) residual 212, 225, 211, 230; (24960, 1536, 1536) residual 138,
+//     149, 140, 136, where the estimate misses the fastest by 2%.
 //   * What fits one round of 128x128 tiles waits on the latency of each K tile, which a third stage hides best, and less on
 //     smaller tiles as long as those fit a round too.  (1560, 1536, 8960) residual 84, 54, 50, and with three stages 128x128
 //     35, 96x128 33, 64x128 45 (two rounds); (1560, 1536, 1536) 9.3, 8.6, 10.5; (512, 1536, 4096) 15.4, 14.1, 13.3; (851,
@@ -838,8 +842,9 @@ template <int EPI, typename TO> bool stores_past_caches(int M, int N, const EpiA
   return (size_t)M * N * (EPI == EPI_STORE || EPI == EPI_GELU ? sizeof(TO) : EPI == EPI_RESIDUAL && e.cache ? 8 : 4) >= kNTBytes;
 }
 
-// Row blocks of a tile group: (24960, 1536, 8960) 409 us at 1, 419 at 4, 432 at 8; (16384, 13824, 5120) 985 at 2, 1024 at
-// 1, 1037 at 4; (24960, 4608, 1536) 173 at 8, 183 at 4, 200 at 2; (24960, 8960, 1536) 394 at 4, 397 at 8, 429 at 1.
+// Row blocks of a tile group, a compromise over what was measured at 1, 2, 4 and 8: (24960, 8960, 1536) 403, 370, 364, 362 us;
+// (24960, 4608, 1536) 164, 164, 166, 168; (16384, 13824, 5120) 967, 931, 915, 958; (16384, 5120, 13824) 992, 974, 988, 1011;
+// (16384, 5120, 5120) 486, 476, 482, 491; (24960, 1536, 8960) 357, 356, 351, 363; (24960, 1536, 1536) 135, 134, 133, 133.
 int group_of(int N, int K) { return N <= 2048 ? 1 : K >= 4096 ? 2 : 8; }
 
 template <int EPI, typename TO, int MF, int NF, int WAVES, int NST>

@@ -203,8 +203,8 @@ template <int TR> struct Row {
 // TR threads a row, NV pieces of eight elements each, held in registers between the maximum and the codes, so that
 // a row is read once.  Bound by HBM (M K (2 or 4 + 1) bytes): 24960 x 8960 bf16 130 us, 5.2 TB/s (what a large copy reaches);
 // 13824 x 5120 fp32 65 us, 5.5 TB/s; 1 x 1536 3.0 us, a launch's latency.  With five operations an element the codes hide
-// behind the loads; the threads of a row are the fewest that hold it with eight pieces or less, so that little of the
-// last pass is idle (8960 on 256 x 8 pieces 155 us, on 256 x 5 136).
+// behind the loads; the threads of a row are one wave's or less up to four pieces each, four waves' up to eight, then sixteen's, in steps that
+// leave little of the last pass idle (8960 on 256 x 8 pieces 150 us, on 256 x 5 129).
 template <typename T, int TR, int NV, bool TAIL>
 __global__ __launch_bounds__(Row<TR>::BLOCK) void k_quant_rows(int M, int K, const T *__restrict__ x, int64_t xs,
                                                                int8_t *__restrict__ q, float *__restrict__ scale) {
@@ -302,11 +302,14 @@ hipError_t launch_quant_rows(ActType t, int M, int K, const void *x, int64_t x_r
 // come from one pass of sums in 64 bits over the row less its first element (the pivot), so that a large common offset
 // costs no digits: the variance is off by about 2^-53 (1 + (mean - pivot)^2 / variance) of itself.  Codes are decided on
 // values in 64 bits as well.
-// Bound by HBM: (4 + e) M D bytes read, 4 M D + (e or 1) M D written: 24960 x 1536 bf16 to codes 97 us (4.3 TB/s) and to
-// activations 96 (4.8), 16384 x 5120 to activations 212 (4.7), one token of 1536 3.9 us.  The 64-bit arithmetic, some 30
-// instructions an element at the rate of 32-bit ones, hides behind that, as long as registers leave four waves a SIMD: y
-// stays as it is stored.  Pieces of four elements, which make a wave's accesses to fp32 whole ranges, bring the vectors in
-// twice as many waits: (16384, 5120) to activations 191, but (24960, 1536) 102 and (8192, 6144) 152 in place of 131.
+// Bound by HBM: (4 + e) M D bytes read, 4 M D + (e or 1) M D written: 24960 x 1536 bf16 to codes 98 us (4.3 TB/s) and to
+// activations 98 (4.7), 16384 x 5120 to activations 215 (4.7), one token of 1536 4.0 us; without a branch 24960 x 1536 45 us.
+// The 64-bit arithmetic, some 35 instructions an element at the rate of 32-bit ones, hides behind that for the most part, as
+// long as registers leave four waves a SIMD: y stays as it is stored.  The stream in fp32 where activations follow would save
+// 1 to 6% (1560 x 1536 9.8 us against 10.4), and sums without the pivot for RMS norm nothing.  Pieces of four
+// elements, which make a wave's accesses to fp32 whole ranges, bring the vectors in twice as many waits: measured on the fp32
+// stream, (16384, 5120) to activations 191 in place of 212, but (24960, 1536) 102 in place of 96 and (8192, 6144) 152 in
+// place of 131.
 namespace {
 
 // Rows of 513 to 2048 elements are on one wave, two or four, by the number of rows.  So that a row's bits are those it has among
@@ -408,8 +411,8 @@ __device__ __forceinline__ void load8_or(const float *p, float otherwise, int c,
 
 enum { SEAM_NONE = 0, SEAM_ACT = 1, SEAM_I8 = 2 };
 
-// FULL: the row fills its threads' pieces, so that no load waits behind a branch: (1560, 1536) to codes 10.2 us against 11.5,
-// (24960, 1536) 96 and 98.
+// FULL: the row fills its threads' pieces, so that no load waits behind a branch: (1560, 1536) to codes 10.4 us against 11.9,
+// (24960, 1536) 98 and 100, (1560, 2048) to activations 12.3 and 13.2.
 template <typename T, int TR, int NV, bool TAIL, int OUT, bool NT, bool FULL>
 __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArgs a) {
   using R = Row<TR>;
@@ -571,8 +574,8 @@ __global__ __launch_bounds__(Row<TR>::BLOCK) void k_norm_residual(int M, SeamArg
 template <typename T, int TR, int NV, int OUT>
 static hipError_t norm_rows(int M, const SeamArgs &a, hipStream_t s) {
   const dim3 grid(Row<TR>::blocks(M)), block(Row<TR>::BLOCK);
-  // a stream of 64 MiB and more is stored non-temporally: nothing reads it soon ((24960, 1536) to codes 105 -> 101 us,
-  // (16384, 5120) to activations 224 -> 219); a smaller one the next kernel may still find in the caches
+  // a stream of 64 MiB and more is stored non-temporally: nothing reads it soon ((24960, 1536) to codes 102 -> 98 us,
+  // (16384, 5120) to activations 219 -> 215); a smaller one the next kernel may still find in the caches
   const bool nt = a.x_out && (size_t)M * a.D * 4 >= (size_t)64 << 20;
   // on 256 threads it gained nothing: (1560, 4096) to codes 20.6 us and 21.3, but to activations 18.8 and 18.2
   constexpr bool FULL = NV > 1 && TR <= 128;
@@ -589,7 +592,9 @@ static hipError_t norm_rows_of(int M, const SeamArgs &a, hipStream_t s) {
   const int pieces = (a.D + 7) / 8;
 #define FB_ROWS(TR, NV) if (pieces <= TR * NV) return norm_rows<T, TR, NV, OUT>(M, a, s);
   FB_ROWS(16, 1) FB_ROWS(32, 1) FB_ROWS(64, 1)   // several rows a wave: 24960 x 64 10 us, on whole waves 34
-  // few rows wait on a row's own chain, which more threads shorten: 390 x 1536 5.5 us and 7.3, but 24960 x 1536 105 and 99
+  // few rows wait on a row's own chain, which more threads shorten, many on the waves' arithmetic: on 256 threads and on one
+  // wave 1 x 1536 to codes 4.0 us and 4.6, 512 rows 5.8 and 6.1, 650 rows 7.2 and 6.4, 1560 rows 12.3 and 10.4; to activations
+  // 512 rows 5.4 and 6.2, 780 rows 7.2 and 6.7
   if (M <= 2 * cu_count()) { FB_ROWS(256, 1) }
   FB_ROWS(64, 2) FB_ROWS(64, 3) FB_ROWS(128, 2) FB_ROWS(192, 2) FB_ROWS(256, 2) FB_ROWS(256, 3)
 #undef FB_ROWS
