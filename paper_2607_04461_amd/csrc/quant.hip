@@ -577,7 +577,8 @@ static hipError_t norm_rows(int M, const SeamArgs &a, hipStream_t s) {
   // a stream of 64 MiB and more is stored non-temporally: nothing reads it soon ((24960, 1536) to codes 102 -> 98 us,
   // (16384, 5120) to activations 219 -> 215); a smaller one the next kernel may still find in the caches
   const bool nt = a.x_out && (size_t)M * a.D * 4 >= (size_t)64 << 20;
-  // on 256 threads it gained nothing: (1560, 4096) to codes 20.6 us and 21.3, but to activations 18.8 and 18.2
+  // on 256 threads it lost as often as it gained: (1560, 4096) to codes 21.3 us in place of 22.3, to activations 19.5 of 19.2,
+  // (9000, 4096) 99 of 98 and 97 of 98, (16384, 4096) fp32 192 of 188 and 215 of 218
   constexpr bool FULL = NV > 1 && TR <= 128;
   const bool full = FULL && a.D == 8 * TR * NV;
   const auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, s, M, a); };
