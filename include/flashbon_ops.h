@@ -163,6 +163,116 @@ flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, f
                                           float *x_out, int32_t pre_norm, const float *shift, const float *scale,
                                           void *out, int8_t *q, float *q_scale, void *stream);
 
+/* ---- The cross-attention branch with a prompt and an adapter per candidate, and its gradients.  A pool may hold
+ * candidates of several requests: prompts of different lengths, timesteps of their own, and fine-tuned low-rank adapters.
+ * The same calls train such adapters on drafts (Sec. 5): the base weights stay frozen, and the gradient of a frozen linear
+ * layer's input is flashbon_op_linear on its transposed weights.  A branch h + gate W_o attention(W_q LN(h)) runs as
+ *   flashbon_op_layer_norm -> flashbon_op_linear + flashbon_op_adapters -> flashbon_op_cross_attention ->
+ *   flashbon_op_linear (FLASHBON_EPI_RESIDUAL) + flashbon_op_adapters,
+ * and backwards through the _grad calls.  A workspace is the caller's (device, on 16 bytes); a _workspace function returns
+ * the bytes a call needs, 0 also for sizes that the call refuses.  Calls that share a workspace must be ordered.  No call
+ * uses atomics on results: the same call gives the same bits.  All of them may be captured into a graph. */
+
+/* LayerNorm with saved statistics: out[m][d] (act) = (x[m][d] - mean[m]) rstd[m] f[g][d] + bias[g][d], mean and rstd =
+ * 1 / sqrt(biased variance + eps) of the row, g = m / rows_per_group; f = weight, or 1 + weight where `modulated` (adaLN).
+ * x: device fp32 [M][D]; weight, bias: device fp32 [ceil(M / rows_per_group)][D], each may be NULL (f = 1, bias = 0); out:
+ * device act [M][D]; mean, rstd: device fp32 [M] or NULL (the mean is taken off in more bits than the saved one has).
+ * rows_per_group >= 1; M shares one weight at rows_per_group >= M.  A row's bits do not depend on the other rows.  Outputs
+ * must not overlap an input or each other (FLASHBON_EINVAL).  eps positive and finite.  M >= 1, 1 <= D <= 6144.  Addresses
+ * need no more alignment than their elements; 16 bytes and D % 4 == 0 are fastest. */
+flashbon_status flashbon_op_layer_norm(int32_t dtype, int32_t M, int32_t D, float eps, const float *x, int32_t rows_per_group,
+                                       const float *weight, int32_t modulated, const float *bias, void *out, float *mean,
+                                       float *rstd, void *stream);
+
+/* Gradient of flashbon_op_layer_norm from dy, device act [M][D].  With xhat = (x - mean) rstd and g = dy f:
+ *   dx[m][d] = residual[m][d] + rstd[m] (g - mean_d(g) - xhat mean_d(g xhat));   dweight[g][d] = sum_m dy xhat, dbias[g][d] =
+ *   sum_m dy over the group's rows.
+ * mean, rstd: device fp32 [M], as the forward call left them.  residual: device fp32 [M][D] (the gradient that reaches x
+ * past the norm) or NULL (0).  dx: device fp32 [M][D], may be residual itself; dweight, dbias: device fp32, as weight; each
+ * output may be NULL, one at least is given.  Outputs must not otherwise overlap an input or each other (FLASHBON_EINVAL).
+ * Sizes as above; a workspace of flashbon_op_layer_norm_grad_workspace bytes wherever dweight or dbias is given
+ * (FLASHBON_ESHAPE if it is smaller). */
+flashbon_status flashbon_op_layer_norm_grad(int32_t dtype, int32_t M, int32_t D, const float *x, int32_t rows_per_group,
+                                            const float *weight, int32_t modulated, const float *mean, const float *rstd,
+                                            const void *dy, const float *residual, float *dx, float *dweight, float *dbias,
+                                            void *workspace, size_t workspace_bytes, void *stream);
+size_t flashbon_op_layer_norm_grad_workspace(int32_t M, int32_t D, int32_t rows_per_group);
+
+/* Cross-attention to encoder states of their own lengths: as flashbon_op_attention, but the queries of batch row b see only
+ * the first kv_len[c] of the tk key rows of c = kv_index[b], and query head h reads key head h / (heads / kv_heads).
+ * Key rows at or past kv_len[c] are never read.  A prompt of length 0 gives rows of zeros.  lse (device fp32
+ * [batch][heads][tq], or NULL): log sum_j exp(q k_j / sqrt(head_dim)), -infinity for an empty prompt.
+ * kv_index: device int32 [batch] or NULL (b; then n_kv = batch), kv_len: device int32 [n_kv] or NULL (tk); their values are
+ * clamped into [0, n_kv) and [0, tk].  heads % kv_heads == 0; head_dim one of 8, 16, 32, 64, 128; 1 <= tq, tk <= 2^24;
+ * batch heads ceil(tq / 64) < 2^24, n_kv kv_heads <= 65535.  Row i of batch row b is at q + b q_batch_stride + i
+ * q_row_stride + h head_dim, keys, values and out as in flashbon_op_attention.  Every address, and every stride in bytes, is
+ * a multiple of 16, strides lie in [0, 2^36), and out's keep its rows apart (FLASHBON_EINVAL).  out and lse must not
+ * overlap the extent of an input or each other (FLASHBON_EINVAL).
+ * Few queries (tq heads) to long states run over several ranges of keys at once where a workspace of
+ * flashbon_op_cross_attention_workspace bytes is given; without one, or with a smaller one, in one range.  A candidate's
+ * bits do not depend on the other candidates. */
+flashbon_status flashbon_op_cross_attention(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                            int32_t tq, int32_t tk, const void *q, int64_t q_batch_stride,
+                                            int64_t q_row_stride, const void *k, const void *v, int64_t kv_batch_stride,
+                                            int64_t kv_row_stride, const int32_t *kv_index, int32_t n_kv,
+                                            const int32_t *kv_len, void *out, int64_t out_batch_stride,
+                                            int64_t out_row_stride, float *lse, void *workspace, size_t workspace_bytes,
+                                            void *stream);
+size_t flashbon_op_cross_attention_workspace(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                             int32_t tq, int32_t tk);
+
+/* Gradient of flashbon_op_cross_attention from dout (act, out's strides), with out and lse as the forward call left them:
+ *   P = exp(S - lse), S = q k^T / sqrt(head_dim);   dS = P (dout v^T - sum_d dout out) / sqrt(head_dim);
+ *   dq = dS k;   dk = dS^T q, dv = P^T dout, summed over the batch rows and the query heads that read the key head.
+ * dq (act) has q's strides, dk and dv those of k and v; q's and k's strides must keep their rows apart.  Every row of dk and
+ * dv up to tk is written, zeros at or past kv_len[c] and for prompts that no row reads.  dq may be NULL, and so may dk
+ * and dv together.  The outputs must not overlap the extent of an input or each other, but rows of dk and dv may alternate
+ * as those of fused keys and values do (FLASHBON_EINVAL).  batch <= 4096; sizes and alignment otherwise as above; a
+ * workspace of flashbon_op_cross_attention_grad_workspace bytes (FLASHBON_ESHAPE if it is smaller). */
+flashbon_status flashbon_op_cross_attention_grad(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads,
+                                                 int32_t head_dim, int32_t tq, int32_t tk, const void *q,
+                                                 int64_t q_batch_stride, int64_t q_row_stride, const void *k, const void *v,
+                                                 int64_t kv_batch_stride, int64_t kv_row_stride, const int32_t *kv_index,
+                                                 int32_t n_kv, const int32_t *kv_len, const void *out,
+                                                 int64_t out_batch_stride, int64_t out_row_stride, const float *lse,
+                                                 const void *dout, void *dq, void *dk, void *dv, void *workspace,
+                                                 size_t workspace_bytes, void *stream);
+size_t flashbon_op_cross_attention_grad_workspace(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads,
+                                                  int32_t head_dim, int32_t tq, int32_t tk, int32_t n_kv);
+
+/* Low-rank adapters beside a shared projection: for each group of rows_per_group rows with the adapter a = index[m /
+ * rows_per_group],
+ *   u[m][r] = sum_k x[m][k] down[a][r][k];   out[m][n] = base[m][n] + gate[n] scales[a] sum_r u[m][r] up[a][n][r].
+ * Rows whose index lies outside [0, n_adapters) have none: u = 0, out = base.
+ * x: device act [M][K]; down: device act [n_adapters][rank][K]; up: device act [n_adapters][N][rank]; scales: device fp32
+ * [n_adapters] or NULL (1); index: device int32 [ceil(M / rows_per_group)] or NULL (adapter 0).  `epilogue` is that of the
+ * projection: FLASHBON_EPI_STORE: base and out are act; FLASHBON_EPI_STORE_F32: fp32; FLASHBON_EPI_RESIDUAL: fp32, with gate
+ * (device fp32 [N] or NULL: 1; ignored by the others).  base: device [M][N], the projection's output, may be out itself,
+ * or NULL (0).  u: device fp32 [M][rank], kept for the gradient; it is not rounded before the second product.  Outputs
+ * must not otherwise overlap an input or each other (FLASHBON_EINVAL).  A row's bits do not depend on the other rows.
+ * 1 <= M <= 2^22; N, K multiples of 8 up to 65536; rank a multiple of 8 up to 128; 1 <= n_adapters <= 1024; rows_per_group
+ * >= 1; addresses on 16 bytes but index, on 4 (FLASHBON_EINVAL). */
+flashbon_status flashbon_op_adapters(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t rank, int32_t n_adapters,
+                                     const void *x, const void *down, const void *up, const float *scales,
+                                     const int32_t *index, int32_t rows_per_group, int32_t epilogue, const float *gate,
+                                     const void *base, void *out, float *u, void *stream);
+
+/* Gradient of flashbon_op_adapters from dy, device act [M][N] (the gradient of out, times the gate where there is one), and u
+ * as the forward call left it.  With du[m][r] = scales[a] sum_n dy[m][n] up[a][n][r]:
+ *   dx[m][k] = base[m][k] + sum_r du[m][r] down[a][r][k];   d_down[a][r][k] = sum_m du[m][r] x[m][k];
+ *   d_up[a][n][r] = scales[a] sum_m dy[m][n] u[m][r], the sums over a's rows (0 without any).
+ * dx and base (the gradient through the projection, may be dx itself, or NULL: 0): device [M][K], act with
+ * FLASHBON_EPI_STORE, fp32 with FLASHBON_EPI_STORE_F32.  d_down, d_up: device fp32, as down and up.  dx, d_down and d_up may
+ * be NULL, one at least is given.  Outputs must not otherwise overlap an input or each other (FLASHBON_EINVAL).  Sizes and
+ * alignment as above; a workspace of flashbon_op_adapters_grad_workspace bytes (FLASHBON_ESHAPE if it is smaller). */
+flashbon_status flashbon_op_adapters_grad(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t rank, int32_t n_adapters,
+                                          const void *x, const void *down, const void *up, const float *scales,
+                                          const int32_t *index, int32_t rows_per_group, const float *u, const void *dy,
+                                          int32_t epilogue, const void *base, void *dx, float *d_down, float *d_up,
+                                          void *workspace, size_t workspace_bytes, void *stream);
+size_t flashbon_op_adapters_grad_workspace(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t rank, int32_t n_adapters,
+                                           int32_t rows_per_group);
+
 #ifdef __cplusplus
 }
 #endif

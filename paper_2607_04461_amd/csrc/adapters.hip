@@ -1,0 +1,571 @@
+// Low-rank adapters of many requests beside a shared projection, and their gradient.  Rows come in groups (a request's
+// tokens, `per` of them), each group with an adapter a of its own or none:
+//   u = x down_a^T,   out = base + gate s_a u up_a^T
+//   du = s_a dy up_a,   dx = base + du down_a,   d_down_a = sum_m du^T x,   d_up_a = s_a sum_m dy^T u
+// A projection adds 2 r flops to each element it reads and writes, so with r <= 128 all of it is bound by memory: by HBM
+// for many rows, by the latency of two or three launches for few.  Four kernels carry both directions:
+//   * k_down: [rows][K] . [r][K]^T.  A workgroup takes 16 to 64 rows of one group and all ranks, its eight waves every
+//     eighth 32 columns each, straight from memory to the matrix cores; their sums meet in LDS.  x is read once.
+//   * k_up: [rows][r] . [N][r]^T onto the base rows.  The weights feed the left operand with the rows of two tiles
+//     interleaved, so that a lane holds eight consecutive outputs of one row.
+//   * k_outer: the sum over rows of an outer product, both operands through LDS, the activations' columns by transposing
+//     reads.  Rows reach it through lists sorted by adapter (k_rows), in chunks; k_outer_sum adds the chunks' sums in order.
+//   * k_transpose: up and down the other way round for the gradient's two products, a few MB at most.
+// u and du are fp32 and stay so: next to bf16 weights each is split into bf16 parts that are multiplied one by one, three
+// where the result is fp32 (24 bits) and two where it is bf16 (16 bits of it, against the 8 that are kept).
+#include <algorithm>
+
+#include "fragments.h"
+#include "kernels.h"
+
+namespace fb {
+namespace {
+
+__device__ __forceinline__ int adapter_of(const int32_t *index, int64_t group, int count) {
+  const int a = index ? index[group] : 0;
+  return a >= 0 && a < count ? a : -1;
+}
+
+// what rounding v to `part` left; nothing where v was not finite or rounded to infinity
+__device__ __forceinline__ float rest(float v, float part) {
+  const float r = v - part;
+  return fabsf(r) <= fabsf(v) ? r : 0.f;
+}
+
+// parts of v: v ~ p[0] + p[1] + ...
+template <typename T, int P>
+__device__ __forceinline__ void split(f32x8 v, Frag<T> (&p)[P]) {
+#pragma unroll
+  for (int k = 0; k < P; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[k][i] = from_f32<T>(v[i]);
+      v[i] = rest(v[i], to_f32(p[k][i]));
+    }
+}
+
+struct Tile {     // rows [row0, row0 + rows) of one group
+  int64_t group, row0;
+  int rows;
+};
+__device__ __forceinline__ Tile tile_at(int64_t id, int size, int64_t M, int per) {
+  const int tiles = (per + size - 1) / size;
+  Tile t;
+  t.group = id / tiles;
+  const int64_t from = (id % tiles) * size;
+  t.row0 = t.group * per + from;
+  t.rows = (int)max((int64_t)0, min(min((int64_t)size, per - from), M - t.row0));
+  return t;
+}
+
+struct DownArgs {
+  int64_t M;
+  int per, K, rank, count;
+  const void *x, *w;            // [M][K], [count][rank][K]
+  const int32_t *index;
+  const float *scales;          // [count] or null
+  float *u;                     // [M][rank]
+};
+
+constexpr int DOWN_WAVES = 8;
+
+template <typename T, int MT, int RT>
+__global__ __launch_bounds__(64 * DOWN_WAVES) void k_down(DownArgs a) {
+  extern __shared__ float s_part[];     // [waves][MT RT][256]
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Tile t = tile_at(blockIdx.x, 16 * MT, a.M, a.per);
+  if (t.rows <= 0) return;
+  const int ad = adapter_of(a.index, t.group, a.count);
+  if (ad < 0) {
+    for (int i = tid; i < t.rows * a.rank; i += 64 * DOWN_WAVES) a.u[t.row0 * a.rank + i] = 0.f;
+    return;
+  }
+  f32x4 acc[MT][RT];
+  const T *xr[MT], *wr[RT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) xr[i] = (const T *)a.x + (t.row0 + min(16 * i + li, t.rows - 1)) * a.K;
+#pragma unroll
+  for (int j = 0; j < RT; ++j) wr[j] = (const T *)a.w + ((int64_t)ad * a.rank + min(16 * j + li, a.rank - 1)) * a.K;
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  Frag<T> xf[2][MT], wf[2][RT];
+  auto load = [&](int b, int step) __attribute__((always_inline)) {
+    const int k = 32 * step + 8 * g;
+    const bool in = k < a.K;      // K % 8 == 0
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xf[b][i] = in ? load_frag(xr[i] + k) : zero_frag<T>();
+#pragma unroll
+    for (int j = 0; j < RT; ++j) wf[b][j] = in ? load_frag(wr[j] + k) : zero_frag<T>();
+  };
+  auto multiply = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < RT; ++j) acc[i][j] = mma(xf[b][i], wf[b][j], acc[i][j]);
+  };
+  const int steps = (a.K + 31) / 32;
+  int s = w;
+  if (s < steps) load(0, s);
+  while (s < steps) {       // the next step's loads in flight under this one's products
+    if (s + DOWN_WAVES < steps) load(1, s + DOWN_WAVES);
+    multiply(0);
+    s += DOWN_WAVES;
+    if (s >= steps) break;
+    if (s + DOWN_WAVES < steps) load(0, s + DOWN_WAVES);
+    multiply(1);
+    s += DOWN_WAVES;
+  }
+  // element (row 4 g + e, rank li) of tile (i, j)
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < RT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s_part[(w * MT * RT + i * RT + j) * 256 + (4 * g + e) * 16 + li] = acc[i][j][e];
+  __syncthreads();
+  const float scale = a.scales ? a.scales[ad] : 1.f;
+  for (int p = tid; p < MT * RT * 256; p += 64 * DOWN_WAVES) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < DOWN_WAVES; ++k) v += s_part[k * MT * RT * 256 + p];
+    const int row = p / (RT * 256) * 16 + (p & 255) / 16, r = p / 256 % RT * 16 + (p & 15);
+    if (row < t.rows && r < a.rank) a.u[(t.row0 + row) * a.rank + r] = v * scale;
+  }
+}
+
+struct UpArgs {
+  int64_t M;
+  int per, N, rank, count, cols;      // cols: columns of a workgroup, a multiple of 128
+  const float *u;                     // [M][rank]
+  const void *w;                      // [count][N][rank]
+  const int32_t *index;
+  const float *scales, *gate;         // [count], [N] or null
+  const void *base;                   // [M][N] of the output's type, or null: zeros
+  void *out;
+};
+
+template <typename T, typename O, int MT, int RK>
+__global__ __launch_bounds__(256) void k_up(UpArgs a) {
+  constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(O) == 4 ? 3 : 2;
+  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tile t = tile_at(blockIdx.x, 16 * MT, a.M, a.per);
+  if (t.rows <= 0) return;
+  const int ad = adapter_of(a.index, t.group, a.count);
+  if (ad < 0 && a.base == a.out) return;
+  const int from = blockIdx.y * a.cols, to = min(from + a.cols, a.N);
+  int64_t row[MT];
+  bool in[MT];
+  Frag<T> uf[MT][RK][PARTS];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    in[i] = 16 * i + li < t.rows;
+    row[i] = t.row0 + min(16 * i + li, t.rows - 1);
+#pragma unroll
+    for (int c = 0; c < RK; ++c) {
+      const int r = 32 * c + 8 * g;
+      split<T, PARTS>(r < a.rank ? load_frag(a.u + row[i] * a.rank + r) : zero_frag<float>(), uf[i][c]);
+    }
+  }
+  const float scale = ad < 0 ? 0.f : a.scales ? a.scales[ad] : 1.f;
+  const T *W = (const T *)a.w + (int64_t)max(ad, 0) * a.N * a.rank;
+  // column of row li of tile h: four of each eight
+  const int col = 8 * (li >> 2) + (li & 3);
+  for (int n0 = from + 32 * w; n0 < to; n0 += 128) {
+    const int n = n0 + 8 * g;                  // this lane's eight columns; N % 8 == 0
+    const bool ok = n < to;
+    Frag<T> wf[2][RK];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c = 0; c < RK; ++c) {
+        const int r = 32 * c + 8 * g;
+        wf[h][c] = r < a.rank && ad >= 0 ? load_frag(W + (int64_t)min(n0 + col + 4 * h, a.N - 1) * a.rank + r) : zero_frag<T>();
+      }
+    Frag<O> b[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) b[i] = a.base && ok && in[i] ? load_frag((const O *)a.base + row[i] * a.N + n) : zero_frag<O>();
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = a.gate && ok ? scale * a.gate[n + e] : scale;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int p = PARTS - 1; p >= 0; --p)     // the small parts first
+#pragma unroll
+        for (int c = 0; c < RK; ++c)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) acc[h] = mma(wf[h][c], uf[i][c][p], acc[h]);
+      Frag<O> o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = to_f32(b[i][e]);
+        o[e] = from_f32<O>(ad < 0 ? v : fmaf(f[e], acc[e >> 2][e & 3], v));
+      }
+      if (ok && in[i]) store_frag((O *)a.out + row[i] * a.N + n, o);
+    }
+  }
+}
+
+// out[z][c][r] = in[z][r][c] for `count` matrices of each of two shapes
+struct TransposeArgs {
+  const void *in[2];
+  void *out[2];
+  int rows[2], cols[2], count;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_transpose(TransposeArgs a) {
+  __shared__ T s[32][33];
+  const int job = blockIdx.z >= a.count, z = blockIdx.z - job * a.count;
+  const int rows = a.rows[job], cols = a.cols[job], tc = (cols + 31) / 32;
+  if ((int64_t)blockIdx.x >= (int64_t)tc * ((rows + 31) / 32)) return;
+  const int r0 = blockIdx.x / tc * 32, c0 = blockIdx.x % tc * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const T *in = (const T *)a.in[job] + (int64_t)z * rows * cols;
+  T *out = (T *)a.out[job] + (int64_t)z * rows * cols;
+  for (int i = y; i < 32; i += 8)
+    if (r0 + i < rows && c0 + x < cols) s[i][x] = in[(int64_t)(r0 + i) * cols + c0 + x];
+  __syncthreads();
+  for (int i = y; i < 32; i += 8)
+    if (c0 + i < cols && r0 + x < rows) out[(int64_t)(c0 + i) * rows + r0 + x] = s[x][i];
+}
+
+// The rows of each adapter, in order, as a list that starts at a multiple of `chunk` and is filled up with -1:
+// `list`; chunk_adapter[c]: the adapter of a chunk, -1 past the last; first[a], first[count + a]: an adapter's chunks.
+// One workgroup an adapter; the counts are integers, so the order of their additions changes nothing.
+__global__ __launch_bounds__(1024) void k_rows(int64_t M, int per, int count, const int32_t *index, int chunk, int chunks,
+                                               int32_t *list, int32_t *chunk_adapter, int32_t *first) {
+  __shared__ int s_rows[1024], s_group[1024], s_wave[16], s_sum[2];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, me = blockIdx.x;
+  const int64_t groups = (M + per - 1) / per;
+  s_rows[tid] = 0;
+  if (tid < 2) s_sum[tid] = 0;
+  __syncthreads();
+  for (int64_t i = tid; i < groups; i += 1024) {
+    const int a = adapter_of(index, i, count);
+    if (a >= 0) atomicAdd(&s_rows[a], (int)min((int64_t)per, M - i * per));
+  }
+  __syncthreads();
+  if (tid < count) {
+    const int n = (s_rows[tid] + chunk - 1) / chunk;
+    if (n && tid < me) atomicAdd(&s_sum[0], n);
+    if (n) atomicAdd(&s_sum[1], n);
+  }
+  __syncthreads();
+  const int before = s_sum[0], total = s_sum[1], mine = s_rows[me], own = (mine + chunk - 1) / chunk;
+  if (tid == 0) {
+    first[me] = before;
+    first[count + me] = own;
+  }
+  for (int i = tid; i < own; i += 1024) chunk_adapter[before + i] = me;
+  if (me == 0)
+    for (int i = total + tid; i < chunks; i += 1024) chunk_adapter[i] = -1;
+  int32_t *at = list + (int64_t)before * chunk;
+  for (int64_t g0 = 0; g0 < groups; g0 += 1024) {
+    const bool match = g0 + tid < groups && adapter_of(index, g0 + tid, count) == me;
+    const uint64_t votes = __ballot(match);
+    if (lane == 0) s_wave[w] = __popcll(votes);
+    __syncthreads();
+    int slot = __popcll(votes & ((1ull << lane) - 1)), all = 0;
+    for (int i = 0; i < 16; ++i) {
+      if (i < w) slot += s_wave[i];
+      all += s_wave[i];
+    }
+    if (match) s_group[slot] = (int)(g0 + tid);
+    __syncthreads();
+    // every group but the last of all is whole, so an adapter's rows are dense
+    for (int64_t i = tid; i < (int64_t)all * per; i += 1024) {
+      const int64_t row = (int64_t)s_group[i / per] * per + i % per;
+      if (row < M) at[i] = (int32_t)row;
+    }
+    at += (int64_t)all * per;
+    __syncthreads();
+  }
+  at = list + (int64_t)before * chunk;
+  for (int i = mine + tid; i < own * chunk; i += 1024) at[i] = -1;
+}
+
+struct OuterArgs {
+  int rank, chunk;
+  int cols[2];                        // K and N
+  const void *x[2];                   // x [M][K] and dy [M][N]
+  const float *u[2];                  // du and u [M][rank]
+  const int32_t *list, *chunk_adapter;
+  float *partial;                     // [chunks][rank K + N rank]: d_down as [rank][K], then d_up as [N][rank]
+};
+
+constexpr int OUTER_COLS = 256, OUTER_CHUNK = 1024;   // columns of a workgroup; most rows of a chunk
+
+template <typename T, int RT>
+__global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
+  constexpr int PARTS = sizeof(T) == 4 ? 1 : 3;
+  constexpr int XP = OUTER_COLS + 16 / sizeof(T), UP = 32 + 16 / sizeof(T);   // pitches, elements
+  constexpr int PIECE = 16 / sizeof(T);                                       // elements of a 16-byte load
+  constexpr int XN = 32 * OUTER_COLS / PIECE / 256, UN = (32 * 4 * RT + 255) / 256;
+  extern __shared__ __attribute__((aligned(16))) char s_mem[];
+  T *sx = reinterpret_cast<T *>(s_mem), *su = sx + 32 * XP;                   // [32][XP], [PARTS][16 RT][UP]
+  int32_t *rows = reinterpret_cast<int32_t *>(su + PARTS * 16 * RT * UP);     // [chunk]
+  const int chunk = blockIdx.y;
+  if (a.chunk_adapter[chunk] < 0) return;
+  const int blocks0 = (a.cols[0] + OUTER_COLS - 1) / OUTER_COLS;
+  const int job = (int)blockIdx.x >= blocks0, c0 = ((int)blockIdx.x - job * blocks0) * OUTER_COLS, C = a.cols[job];
+  const T *X = (const T *)a.x[job];
+  const float *U = a.u[job];
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, g = lane >> 4, w = tid >> 6;
+  for (int i = tid; i < a.chunk; i += 256) rows[i] = a.list[(int64_t)chunk * a.chunk + i];
+  __syncthreads();
+  int steps = a.chunk / 32;
+  while (steps > 1 && rows[32 * (steps - 1)] < 0) --steps;     // lists end within a chunk
+  u32x4 xv[XN];
+  f32x4 uv[UN];
+  auto load = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < XN; ++i) {
+      const int p = tid + 256 * i, m = rows[32 * s + p / (OUTER_COLS / PIECE)], c = c0 + p % (OUTER_COLS / PIECE) * PIECE;
+      xv[i] = m >= 0 && c < C ? *reinterpret_cast<const u32x4 *>(X + (int64_t)m * C + c) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      const int p = tid + 256 * i, r = 4 * (p % (4 * RT)), m = p < 128 * RT ? rows[32 * s + p / (4 * RT)] : -1;
+      uv[i] = m >= 0 && r < a.rank ? *reinterpret_cast<const f32x4 *>(U + (int64_t)m * a.rank + r) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  auto land = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < XN; ++i) {
+      const int p = tid + 256 * i;
+      *reinterpret_cast<u32x4 *>(sx + p / (OUTER_COLS / PIECE) * XP + p % (OUTER_COLS / PIECE) * PIECE) = xv[i];
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      const int p = tid + 256 * i, m = p / (4 * RT), r = 4 * (p % (4 * RT));
+      if (p >= 128 * RT) break;
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const T v = from_f32<T>(uv[i][e]);
+          su[(k * 16 * RT + r + e) * UP + m] = v;
+          uv[i][e] = rest(uv[i][e], to_f32(v));
+        }
+    }
+  };
+  f32x4 acc[4][RT];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  load(0);
+  for (int s = 0; s < steps; ++s) {
+    __syncthreads();          // the last step's tiles have been read
+    land();
+    __syncthreads();
+    if (s + 1 < steps) load(s + 1);
+    Frag<T> xf[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) xf[i] = load_column_frag(sx, XP, 64 * w + 16 * i, 8 * g, 8 * g + 4);
+#pragma unroll
+    for (int k = PARTS - 1; k >= 0; --k)
+#pragma unroll
+      for (int j = 0; j < RT; ++j) {
+        const Frag<T> uf = load_frag(su + (k * 16 * RT + 16 * j + li) * UP + 8 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i][j] = mma(xf[i], uf, acc[i][j]);
+      }
+  }
+  float *out = a.partial + (int64_t)chunk * a.rank * ((int64_t)a.cols[0] + a.cols[1]) + (job ? (int64_t)a.rank * a.cols[0] : 0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = c0 + 64 * w + 16 * i + 4 * g;      // C % 8 == 0: all four or none
+#pragma unroll
+    for (int j = 0; j < RT; ++j) {
+      const int r = 16 * j + li;
+      if (c >= C || r >= a.rank) continue;
+      if (job) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[(int64_t)(c + e) * a.rank + r] = acc[i][j][e];
+      } else {
+        *reinterpret_cast<f32x4 *>(out + (int64_t)r * C + c) = acc[i][j];
+      }
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void k_outer_sum(int count, int64_t down, int64_t up, const int32_t *first, const float *scales,
+                                                   const float *partial, float *d_down, float *d_up) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= down + up) return;
+  for (int a = blockIdx.y; a < count; a += gridDim.y) {
+    const int c0 = first[a], n = first[count + a];
+    const float *p = partial + c0 * (down + up) + e;
+    double s = 0;
+#pragma unroll 4
+    for (int c = 0; c < n; ++c) s += (double)p[c * (down + up)];
+    if (e < down) {
+      if (d_down) d_down[a * down + e] = (float)s;
+    } else if (d_up) {
+      d_up[a * up + e - down] = (float)(s * (double)(scales ? scales[a] : 1.f));
+    }
+  }
+}
+
+// Rows of a tile: as many as leave a tile a CU at least, and no more than a group has (measured at the launches below).
+int tile_rows(int64_t M, int per, int most) {
+  int mt = most;
+  while (mt > 1 && (16 * (mt / 2) >= per || (M + 16 * mt - 1) / (16 * mt) < 256)) mt /= 2;
+  return mt;
+}
+int64_t tiles_of(int64_t M, int per, int rows) { return (M + per - 1) / per * ((per + rows - 1) / rows); }
+
+template <typename T, int MT, int RT>
+hipError_t down_tile(const DownArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL((k_down<T, MT, RT>), dim3((unsigned)tiles_of(a.M, a.per, 16 * MT)), dim3(64 * DOWN_WAVES),
+                     DOWN_WAVES * MT * RT * 1024, s, a);
+  return hipGetLastError();
+}
+// the waves' sums take MT RT 8 KB of LDS: 64 KB at most, two workgroups a CU
+template <typename T>
+hipError_t launch_down(const DownArgs &a, hipStream_t s) {
+  if (a.rank <= 16) {
+    const int mt = tile_rows(a.M, a.per, 4);
+    return mt == 4 ? down_tile<T, 4, 1>(a, s) : mt == 2 ? down_tile<T, 2, 1>(a, s) : down_tile<T, 1, 1>(a, s);
+  }
+  if (a.rank <= 32) {
+    const int mt = tile_rows(a.M, a.per, 4);
+    return mt == 4 ? down_tile<T, 4, 2>(a, s) : mt == 2 ? down_tile<T, 2, 2>(a, s) : down_tile<T, 1, 2>(a, s);
+  }
+  if (a.rank <= 64) return tile_rows(a.M, a.per, 2) == 2 ? down_tile<T, 2, 4>(a, s) : down_tile<T, 1, 4>(a, s);
+  return down_tile<T, 1, 8>(a, s);
+}
+
+template <typename T, typename O, int MT, int RK>
+hipError_t up_tile(UpArgs a, hipStream_t s) {
+  const int64_t tiles = tiles_of(a.M, a.per, 16 * MT);
+  // columns of a workgroup: enough workgroups for eight a CU, 128 columns at least
+  const int64_t parts = std::min<int64_t>((a.N + 127) / 128, std::max<int64_t>(1, 2048 / tiles));
+  a.cols = (int)((((a.N + 127) / 128 + parts - 1) / parts) * 128);
+  hipLaunchKernelGGL((k_up<T, O, MT, RK>), dim3((unsigned)tiles, (unsigned)((a.N + a.cols - 1) / a.cols)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T, typename O>
+hipError_t launch_up(const UpArgs &a, hipStream_t s) {
+  if (a.rank <= 32) {
+    const int mt = tile_rows(a.M, a.per, 4);
+    return mt == 4 ? up_tile<T, O, 4, 1>(a, s) : mt == 2 ? up_tile<T, O, 2, 1>(a, s) : up_tile<T, O, 1, 1>(a, s);
+  }
+  const int mt = tile_rows(a.M, a.per, 2);
+  if (a.rank <= 64) return mt == 2 ? up_tile<T, O, 2, 2>(a, s) : up_tile<T, O, 1, 2>(a, s);
+  return mt == 2 ? up_tile<T, O, 2, 4>(a, s) : up_tile<T, O, 1, 4>(a, s);
+}
+
+template <typename T, int RT>
+hipError_t outer_rank(const OuterArgs &a, dim3 grid, hipStream_t s) {
+  const size_t lds = (32 * (OUTER_COLS + 16 / sizeof(T)) + (sizeof(T) == 4 ? 1 : 3) * 16 * RT * (32 + 16 / sizeof(T))) * sizeof(T) +
+                     a.chunk * 4;
+  hipLaunchKernelGGL((k_outer<T, RT>), grid, dim3(256), lds, s, a);
+  return hipGetLastError();
+}
+
+// Rows of a chunk: what gives the outer products about a thousand workgroups, in steps of 32
+int outer_chunk(int64_t M, int N, int K) {
+  const int64_t blocks = (N + OUTER_COLS - 1) / OUTER_COLS + (K + OUTER_COLS - 1) / OUTER_COLS;
+  const int64_t rows = (M * blocks / 1024 + 31) / 32 * 32;
+  return (int)std::min<int64_t>(OUTER_CHUNK, std::max<int64_t>(64, rows));
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// the gradient's workspace: parts in order, each on 256 bytes
+struct GradSpace {
+  int chunk;
+  int64_t chunks;
+  size_t up_t, down_t, du, list, chunk_adapter, first, partial, bytes;
+  GradSpace(ActType t, const AdapterArgs &a) {
+    const size_t es = t == ACT_BF16 ? 2 : 4;
+    chunk = outer_chunk(a.M, a.N, a.K);
+    const int64_t groups = (a.M + a.per - 1) / a.per;
+    chunks = (a.M + chunk - 1) / chunk + std::min<int64_t>(a.count, groups);
+    size_t at = 0;
+    auto take = [&](size_t n) { const size_t p = at; at += up256(n); return p; };
+    up_t = take((size_t)a.count * a.N * a.rank * es);
+    down_t = take((size_t)a.count * a.K * a.rank * es);
+    du = take((size_t)a.M * a.rank * 4);
+    list = take((size_t)chunks * chunk * 4);
+    chunk_adapter = take((size_t)chunks * 4);
+    first = take((size_t)a.count * 8);
+    partial = take((size_t)chunks * a.rank * ((size_t)a.N + a.K) * 4);
+    bytes = at;
+  }
+};
+
+template <typename T>
+hipError_t adapters(const AdapterArgs &a, bool out_f32, hipStream_t s) {
+  DownArgs d;
+  d.M = a.M; d.per = a.per; d.K = a.K; d.rank = a.rank; d.count = a.count;
+  d.x = a.x; d.w = a.down; d.index = a.index; d.scales = nullptr; d.u = a.u;
+  const hipError_t e = launch_down<T>(d, s);
+  if (e != hipSuccess) return e;
+  UpArgs p;
+  p.M = a.M; p.per = a.per; p.N = a.N; p.rank = a.rank; p.count = a.count; p.cols = 0;
+  p.u = a.u; p.w = a.up; p.index = a.index; p.scales = a.scales; p.gate = a.gate; p.base = a.base; p.out = a.out;
+  return out_f32 ? launch_up<T, float>(p, s) : launch_up<T, T>(p, s);
+}
+
+template <typename T>
+hipError_t adapters_grad(const AdapterArgs &a, const AdapterGradArgs &b, bool dx_f32, hipStream_t s) {
+  const GradSpace g(sizeof(T) == 2 ? ACT_BF16 : ACT_F32, a);
+  char *ws = (char *)b.workspace;
+  float *du = (float *)(ws + g.du);
+  TransposeArgs t;
+  t.in[0] = a.up; t.out[0] = ws + g.up_t; t.rows[0] = a.N; t.cols[0] = a.rank;
+  t.in[1] = a.down; t.out[1] = ws + g.down_t; t.rows[1] = a.rank; t.cols[1] = a.K;
+  t.count = a.count;
+  const int across = std::max(a.N, a.K);
+  hipLaunchKernelGGL((k_transpose<T>), dim3((across + 31) / 32 * ((a.rank + 31) / 32), 1, 2 * a.count), dim3(256), 0, s, t);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  DownArgs d;
+  d.M = a.M; d.per = a.per; d.K = a.N; d.rank = a.rank; d.count = a.count;
+  d.x = b.dy; d.w = ws + g.up_t; d.index = a.index; d.scales = a.scales; d.u = du;
+  if ((e = launch_down<T>(d, s)) != hipSuccess) return e;
+  if (b.dx) {
+    UpArgs p;
+    p.M = a.M; p.per = a.per; p.N = a.K; p.rank = a.rank; p.count = a.count; p.cols = 0;
+    p.u = du; p.w = ws + g.down_t; p.index = a.index; p.scales = nullptr; p.gate = nullptr; p.base = b.base; p.out = b.dx;
+    if ((e = dx_f32 ? launch_up<T, float>(p, s) : launch_up<T, T>(p, s)) != hipSuccess) return e;
+  }
+  if (!b.d_down && !b.d_up) return hipSuccess;
+  int32_t *list = (int32_t *)(ws + g.list), *chunk_adapter = (int32_t *)(ws + g.chunk_adapter), *first = (int32_t *)(ws + g.first);
+  hipLaunchKernelGGL(k_rows, dim3(a.count), dim3(1024), 0, s, a.M, a.per, a.count, a.index, g.chunk, (int)g.chunks, list,
+                     chunk_adapter, first);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  OuterArgs o;
+  o.rank = a.rank; o.chunk = g.chunk;
+  o.cols[0] = a.K; o.cols[1] = a.N; o.x[0] = a.x; o.x[1] = b.dy; o.u[0] = du; o.u[1] = a.u;
+  o.list = list; o.chunk_adapter = chunk_adapter; o.partial = (float *)(ws + g.partial);
+  const dim3 grid((a.K + OUTER_COLS - 1) / OUTER_COLS + (a.N + OUTER_COLS - 1) / OUTER_COLS, (unsigned)g.chunks);
+  e = a.rank <= 16 ? outer_rank<T, 1>(o, grid, s) : a.rank <= 32 ? outer_rank<T, 2>(o, grid, s)
+      : a.rank <= 64 ? outer_rank<T, 4>(o, grid, s) : outer_rank<T, 8>(o, grid, s);
+  if (e != hipSuccess) return e;
+  const int64_t down = (int64_t)a.rank * a.K, up = (int64_t)a.rank * a.N;
+  hipLaunchKernelGGL(k_outer_sum, dim3((unsigned)((down + up + 255) / 256), a.count), dim3(256), 0, s, a.count, down, up, first,
+                     a.scales, o.partial, b.d_down, b.d_up);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_adapters(ActType t, const AdapterArgs &a, bool out_f32, hipStream_t s) {
+  return t == ACT_BF16 ? adapters<bf16>(a, out_f32, s) : adapters<float>(a, out_f32, s);
+}
+
+size_t adapters_grad_workspace(ActType t, const AdapterArgs &a) { return GradSpace(t, a).bytes; }
+
+hipError_t launch_adapters_grad(ActType t, const AdapterArgs &a, const AdapterGradArgs &b, bool dx_f32, hipStream_t s) {
+  return t == ACT_BF16 ? adapters_grad<bf16>(a, b, dx_f32, s) : adapters_grad<float>(a, b, dx_f32, s);
+}
+
+}  // namespace fb

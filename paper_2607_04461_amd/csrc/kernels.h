@@ -162,4 +162,79 @@ struct SeamArgs {
 };
 hipError_t launch_norm_residual(ActType t, int M, const SeamArgs &a, hipStream_t s);
 
+// ---- the cross-attention branch with a prompt and an adapter per candidate, and its gradients
+// out (act) = (x - mean) rstd f + bias, f = weight + offset (weight null: 1); weight and bias [groups][D], one for each
+// `per` rows.  Any D from 1 to 6144; groups of the gradient times their chunks below 2^24.
+struct LayerNormArgs {
+  int64_t M;
+  int D, per;
+  float eps, offset;
+  const float *x, *weight, *bias;   // weight, bias may be null
+  void *out;
+  float *mean, *rstd;               // [M], may be null
+};
+hipError_t launch_layer_norm(ActType t, const LayerNormArgs &a, hipStream_t s);
+// dx = residual + the gradient of x; dweight, dbias [groups][D]: sums over each group's rows.  Every output may be null.
+struct LayerNormGradArgs {
+  int64_t M;
+  int D, per;
+  float offset;
+  const float *x, *weight, *mean, *rstd, *residual;
+  const void *dy;                   // act [M][D]
+  float *dx, *dweight, *dbias;
+  float *partial;                   // workspace
+  int rows, chunks;                 // filled in by the launcher
+};
+size_t layer_norm_grad_workspace(int64_t M, int D, int per);
+int64_t layer_norm_grad_blocks(int64_t M, int per);
+hipError_t launch_layer_norm_grad(ActType t, LayerNormGradArgs a, hipStream_t s);
+
+// Adapters: u [M][rank] = x down^T, out = base + gate s_a u up^T for each group of `per` rows with the adapter index[group]
+// (null: 0; none outside [0, count): u = 0, out = base).  N, K, rank % 8 == 0, rank <= 128, count <= 1024, M <= 2^22,
+// everything on 16 bytes.
+struct AdapterArgs {
+  int64_t M;
+  int N, K, rank, count, per;
+  const void *x, *down, *up;        // act [M][K], [count][rank][K], [count][N][rank]
+  const float *scales;              // [count] or null
+  const int32_t *index;             // device
+  const float *gate = nullptr;      // [N] or null
+  const void *base = nullptr;       // [M][N] or null
+  void *out = nullptr;              // [M][N], act or fp32 as base
+  float *u;                         // [M][rank]
+};
+hipError_t launch_adapters(ActType t, const AdapterArgs &a, bool out_f32, hipStream_t s);
+// dx = base + du down, d_down and d_up (fp32, the weights' shapes; an adapter without rows: 0); each may be null.
+struct AdapterGradArgs {
+  const void *dy;                   // act [M][N]
+  const void *base;                 // [M][K] of dx's type, or null
+  void *dx;
+  float *d_down, *d_up;
+  void *workspace;
+};
+size_t adapters_grad_workspace(ActType t, const AdapterArgs &a);
+hipError_t launch_adapters_grad(ActType t, const AdapterArgs &a, const AdapterGradArgs &b, bool dx_f32, hipStream_t s);
+
+// Attention of tq queries to the first kv_len[c] of tk keys, c = kv_index[b] (both clamped; null: tk, and c = b), query head
+// h to key head h kv_heads / heads.  lse [batch][heads][tq] may be null.  head_dim in {8, 16, 32, 64, 128}; everything on
+// 16 bytes; strides in elements.
+struct CrossArgs {
+  int batch, heads, kv_heads, head_dim, tq, tk, n_kv;
+  const void *q; int64_t q_bs, q_rs;
+  const void *k, *v; int64_t kv_bs, kv_rs;
+  const int32_t *kv_index, *kv_len;
+  void *out; int64_t o_bs, o_rs;
+  float *lse;
+};
+size_t cross_attention_workspace(ActType t, const CrossArgs &a);
+hipError_t launch_cross_attention(ActType t, const CrossArgs &a, void *workspace, size_t workspace_bytes, hipStream_t s);
+// dq (as q), dk and dv (as k and v, every row of every prompt written); dq, or dk and dv, may be null.  batch <= 4096.
+struct CrossGradArgs {
+  const void *dout;                 // as out
+  void *dq, *dk, *dv;
+  void *workspace;
+};
+size_t cross_attention_grad_workspace(ActType t, const CrossArgs &a);
+hipError_t launch_cross_attention_grad(ActType t, const CrossArgs &a, const CrossGradArgs &b, hipStream_t s);
+
 }  // namespace fb

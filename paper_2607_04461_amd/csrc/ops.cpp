@@ -1,6 +1,7 @@
 // Kernel-level entry points (flashbon_ops.h): validation, then one launch each.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <initializer_list>
@@ -46,6 +47,50 @@ bool overlaps(std::initializer_list<Span> outputs, std::initializer_list<Span> i
       if (overlap(i, *o)) return true;
   }
   return false;
+}
+
+// Bytes from the first to the last element of [n][rows][width] elements with the strides given; 0 rows: none.
+size_t extent(int64_t n, int64_t batch_stride, int64_t rows, int64_t row_stride, int64_t width, size_t es) {
+  return (size_t)((n - 1) * batch_stride + (rows - 1) * row_stride + width) * es;
+}
+// Whether [n][rows] rows of `width` elements share none.
+bool apart(int64_t n, int64_t batch_stride, int64_t rows, int64_t row_stride, int64_t width) {
+  return (rows == 1 || row_stride >= width) && (n == 1 || batch_stride >= (rows - 1) * row_stride + width);
+}
+bool aligned(std::initializer_list<const void *> addresses) {
+  for (const void *p : addresses)
+    if ((uintptr_t)p % 16) return false;
+  return true;
+}
+bool aligned(std::initializer_list<int64_t> strides, int64_t es) {
+  for (const int64_t s : strides)
+    if (s < 0 || s >= (int64_t)1 << 36 || s * es % 16) return false;
+  return true;
+}
+
+bool norm_sizes(int32_t M, int32_t D, int32_t per) {
+  return M >= 1 && D >= 1 && D <= 6144 && per >= 1 && layer_norm_grad_blocks(M, std::min(per, M)) < (1 << 24);
+}
+
+flashbon_status cross_sizes(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t tq,
+                            int32_t tk, int32_t n_kv) {
+  if (dtype != FLASHBON_FP32 && dtype != FLASHBON_BF16) return fail(FLASHBON_EINVAL, "bad dtype");
+  if (batch < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || tq < 1 || tk < 1 || tq > 1 << 24 || tk > 1 << 24 || n_kv < 1)
+    return fail(FLASHBON_ESHAPE, "need batch, heads, kv_heads, n_kv >= 1, heads % kv_heads == 0 and 1 <= tq, tk <= 2^24");
+  if (head_dim != 8 && head_dim != 16 && head_dim != 32 && head_dim != 64 && head_dim != 128)
+    return fail(FLASHBON_ESHAPE, "head_dim must be one of 8, 16, 32, 64, 128");
+  if ((double)batch * heads * ((tq + 63) / 64) >= 16777216.0 || (int64_t)n_kv * kv_heads > 65535)
+    return fail(FLASHBON_ESHAPE, "need batch heads ceil(tq / 64) < 2^24 and n_kv kv_heads <= 65535");
+  return FLASHBON_OK;
+}
+
+flashbon_status adapter_sizes(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t rank, int32_t count, int32_t per) {
+  if (dtype != FLASHBON_FP32 && dtype != FLASHBON_BF16) return fail(FLASHBON_EINVAL, "bad dtype");
+  if (M < 1 || M > 1 << 22 || N < 8 || K < 8 || N % 8 || K % 8 || N > 65536 || K > 65536)
+    return fail(FLASHBON_ESHAPE, "need 1 <= M <= 2^22, and N and K multiples of 8 up to 65536");
+  if (rank < 8 || rank % 8 || rank > 128) return fail(FLASHBON_ESHAPE, "rank must be a multiple of 8 up to 128");
+  if (count < 1 || count > 1024 || per < 1) return fail(FLASHBON_ESHAPE, "need 1 <= n_adapters <= 1024 and rows_per_group >= 1");
+  return FLASHBON_OK;
 }
 
 }  // namespace
@@ -253,6 +298,220 @@ flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, f
   a.x_out = x_out; a.out = out; a.q = q; a.q_scale = q_scale;
   ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
   return launched(launch_norm_residual(t, M, a, (hipStream_t)stream), "norm_residual");
+}
+
+flashbon_status flashbon_op_layer_norm(int32_t dtype, int32_t M, int32_t D, float eps, const float *x, int32_t rows_per_group,
+                                       const float *weight, int32_t modulated, const float *bias, void *out, float *mean,
+                                       float *rstd, void *stream) {
+  if (dtype != FLASHBON_FP32 && dtype != FLASHBON_BF16) return fail(FLASHBON_EINVAL, "bad dtype");
+  if (M < 1 || D < 1 || D > 6144 || rows_per_group < 1)
+    return fail(FLASHBON_ESHAPE, "need M, rows_per_group >= 1 and 1 <= D <= 6144");
+  if (!x || !out) return fail(FLASHBON_EINVAL, "x and out are required");
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(FLASHBON_EINVAL, "eps must be positive and finite");
+  const size_t m = M, d = D, es = dtype == FLASHBON_BF16 ? 2 : 4, groups = (m + rows_per_group - 1) / rows_per_group;
+  if (overlaps({{out, m * d * es}, {mean, 4 * m}, {rstd, 4 * m}}, {{x, 4 * m * d}, {weight, 4 * groups * d}, {bias, 4 * groups * d}}))
+    return fail(FLASHBON_EINVAL, "out, mean and rstd must not overlap an input or each other");
+  LayerNormArgs a;
+  a.M = M; a.D = D; a.per = std::min(rows_per_group, M); a.eps = eps; a.offset = modulated || !weight ? 1.f : 0.f;
+  a.x = x; a.weight = weight; a.bias = bias; a.out = out; a.mean = mean; a.rstd = rstd;
+  ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
+  return launched(launch_layer_norm(t, a, (hipStream_t)stream), "layer_norm");
+}
+
+size_t flashbon_op_layer_norm_grad_workspace(int32_t M, int32_t D, int32_t rows_per_group) {
+  if (!norm_sizes(M, D, rows_per_group)) return 0;
+  return layer_norm_grad_workspace(M, D, std::min(rows_per_group, M));
+}
+
+flashbon_status flashbon_op_layer_norm_grad(int32_t dtype, int32_t M, int32_t D, const float *x, int32_t rows_per_group,
+                                            const float *weight, int32_t modulated, const float *mean, const float *rstd,
+                                            const void *dy, const float *residual, float *dx, float *dweight, float *dbias,
+                                            void *workspace, size_t workspace_bytes, void *stream) {
+  if (dtype != FLASHBON_FP32 && dtype != FLASHBON_BF16) return fail(FLASHBON_EINVAL, "bad dtype");
+  if (!norm_sizes(M, D, rows_per_group))
+    return fail(FLASHBON_ESHAPE, "need M, rows_per_group >= 1, 1 <= D <= 6144, and fewer than 2^24 groups of rows");
+  if (!x || !mean || !rstd || !dy) return fail(FLASHBON_EINVAL, "x, mean, rstd and dy are required");
+  if (!dx && !dweight && !dbias) return fail(FLASHBON_EINVAL, "one of dx, dweight and dbias is required");
+  const size_t m = M, d = D, es = dtype == FLASHBON_BF16 ? 2 : 4, groups = (m + rows_per_group - 1) / rows_per_group;
+  const size_t need = dweight || dbias ? flashbon_op_layer_norm_grad_workspace(M, D, rows_per_group) : 0;
+  if (need && (!workspace || workspace_bytes < need)) return fail(FLASHBON_ESHAPE, "the workspace is too small");
+  if (need && !aligned({workspace})) return fail(FLASHBON_EINVAL, "the workspace must start on 16 bytes");
+  if (overlaps({{dx, 4 * m * d}, {dweight, 4 * groups * d}, {dbias, 4 * groups * d}, {need ? workspace : nullptr, need}},
+               {{x, 4 * m * d}, {weight, 4 * groups * d}, {mean, 4 * m}, {rstd, 4 * m}, {dy, m * d * es},
+                {residual == dx ? nullptr : residual, 4 * m * d}}))
+    return fail(FLASHBON_EINVAL, "outputs and workspace must not overlap an input (but dx residual, which it may be) or each other");
+  LayerNormGradArgs a{};
+  a.M = M; a.D = D; a.per = std::min(rows_per_group, M); a.offset = modulated || !weight ? 1.f : 0.f;
+  a.x = x; a.weight = weight; a.mean = mean; a.rstd = rstd; a.residual = residual; a.dy = dy;
+  a.dx = dx; a.dweight = dweight; a.dbias = dbias; a.partial = (float *)workspace;
+  ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
+  return launched(launch_layer_norm_grad(t, a, (hipStream_t)stream), "layer_norm_grad");
+}
+
+size_t flashbon_op_cross_attention_workspace(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                             int32_t tq, int32_t tk) {
+  if (cross_sizes(dtype, batch, heads, kv_heads, head_dim, tq, tk, 1) != FLASHBON_OK) return 0;
+  CrossArgs a{};
+  a.batch = batch; a.heads = heads; a.kv_heads = kv_heads; a.head_dim = head_dim; a.tq = tq; a.tk = tk; a.n_kv = 1;
+  return cross_attention_workspace(dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32, a);
+}
+
+flashbon_status flashbon_op_cross_attention(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                            int32_t tq, int32_t tk, const void *q, int64_t q_batch_stride,
+                                            int64_t q_row_stride, const void *k, const void *v, int64_t kv_batch_stride,
+                                            int64_t kv_row_stride, const int32_t *kv_index, int32_t n_kv,
+                                            const int32_t *kv_len, void *out, int64_t out_batch_stride,
+                                            int64_t out_row_stride, float *lse, void *workspace, size_t workspace_bytes,
+                                            void *stream) {
+  const flashbon_status st = cross_sizes(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv);
+  if (st != FLASHBON_OK) return st;
+  if (!kv_index && n_kv != batch) return fail(FLASHBON_ESHAPE, "n_kv must be batch without kv_index");
+  if (!q || !k || !v || !out) return fail(FLASHBON_EINVAL, "q, k, v and out are required");
+  const int64_t wide = (int64_t)heads * head_dim, narrow = (int64_t)kv_heads * head_dim, es = dtype == FLASHBON_BF16 ? 2 : 4;
+  if (!aligned({q, k, v, out}) || !aligned({q_batch_stride, q_row_stride, kv_batch_stride, kv_row_stride, out_batch_stride, out_row_stride}, es) ||
+      (uintptr_t)lse % 4)
+    return fail(FLASHBON_EINVAL, "addresses and strides must be multiples of 16 bytes, strides in [0, 2^36)");
+  if (!apart(batch, out_batch_stride, tq, out_row_stride, wide)) return fail(FLASHBON_EINVAL, "out's strides must keep its rows apart");
+  const size_t kv = extent(n_kv, kv_batch_stride, tk, kv_row_stride, narrow, es);
+  CrossArgs a{};
+  a.batch = batch; a.heads = heads; a.kv_heads = kv_heads; a.head_dim = head_dim; a.tq = tq; a.tk = tk; a.n_kv = n_kv;
+  a.q = q; a.q_bs = q_batch_stride; a.q_rs = q_row_stride;
+  a.k = k; a.v = v; a.kv_bs = kv_batch_stride; a.kv_rs = kv_row_stride;
+  a.kv_index = kv_index; a.kv_len = kv_len;
+  a.out = out; a.o_bs = out_batch_stride; a.o_rs = out_row_stride; a.lse = lse;
+  ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
+  const size_t need = workspace ? cross_attention_workspace(t, a) : 0;
+  const bool split = need && workspace_bytes >= need;
+  if (split && !aligned({workspace})) return fail(FLASHBON_EINVAL, "the workspace must start on 16 bytes");
+  if (overlaps({{out, extent(batch, out_batch_stride, tq, out_row_stride, wide, es)}, {lse, (size_t)4 * batch * heads * tq},
+                {split ? workspace : nullptr, need}},
+               {{q, extent(batch, q_batch_stride, tq, q_row_stride, wide, es)}, {k, kv}, {v, kv}, {kv_index, (size_t)4 * batch},
+                {kv_len, (size_t)4 * n_kv}}))
+    return fail(FLASHBON_EINVAL, "out, lse and workspace must not overlap an input or each other");
+  return launched(launch_cross_attention(t, a, split ? workspace : nullptr, need, (hipStream_t)stream), "cross_attention");
+}
+
+size_t flashbon_op_cross_attention_grad_workspace(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads,
+                                                  int32_t head_dim, int32_t tq, int32_t tk, int32_t n_kv) {
+  if (cross_sizes(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv) != FLASHBON_OK || batch > 4096) return 0;
+  CrossArgs a{};
+  a.batch = batch; a.heads = heads; a.kv_heads = kv_heads; a.head_dim = head_dim; a.tq = tq; a.tk = tk; a.n_kv = n_kv;
+  return cross_attention_grad_workspace(dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32, a);
+}
+
+flashbon_status flashbon_op_cross_attention_grad(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads,
+                                                 int32_t head_dim, int32_t tq, int32_t tk, const void *q,
+                                                 int64_t q_batch_stride, int64_t q_row_stride, const void *k, const void *v,
+                                                 int64_t kv_batch_stride, int64_t kv_row_stride, const int32_t *kv_index,
+                                                 int32_t n_kv, const int32_t *kv_len, const void *out,
+                                                 int64_t out_batch_stride, int64_t out_row_stride, const float *lse,
+                                                 const void *dout, void *dq, void *dk, void *dv, void *workspace,
+                                                 size_t workspace_bytes, void *stream) {
+  const flashbon_status st = cross_sizes(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv);
+  if (st != FLASHBON_OK) return st;
+  if (batch > 4096) return fail(FLASHBON_ESHAPE, "batch must be at most 4096");
+  if (!kv_index && n_kv != batch) return fail(FLASHBON_ESHAPE, "n_kv must be batch without kv_index");
+  if (!q || !k || !v || !out || !lse || !dout) return fail(FLASHBON_EINVAL, "q, k, v, out, lse and dout are required");
+  if ((dk == nullptr) != (dv == nullptr)) return fail(FLASHBON_EINVAL, "dk and dv go together");
+  if (!dq && !dk) return fail(FLASHBON_EINVAL, "dq, or dk and dv, are required");
+  const int64_t wide = (int64_t)heads * head_dim, narrow = (int64_t)kv_heads * head_dim, es = dtype == FLASHBON_BF16 ? 2 : 4;
+  if (!aligned({q, k, v, out, dout, dq, dk, dv, workspace}) || (uintptr_t)lse % 4 ||
+      !aligned({q_batch_stride, q_row_stride, kv_batch_stride, kv_row_stride, out_batch_stride, out_row_stride}, es))
+    return fail(FLASHBON_EINVAL, "addresses and strides must be multiples of 16 bytes, strides in [0, 2^36)");
+  if ((dq && !apart(batch, q_batch_stride, tq, q_row_stride, wide)) || (dk && !apart(n_kv, kv_batch_stride, tk, kv_row_stride, narrow)))
+    return fail(FLASHBON_EINVAL, "the strides of q, k and v must keep the rows of their gradients apart");
+  const size_t need = flashbon_op_cross_attention_grad_workspace(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv);
+  if (!workspace || workspace_bytes < need) return fail(FLASHBON_ESHAPE, "the workspace is too small");
+  const size_t qs = extent(batch, q_batch_stride, tq, q_row_stride, wide, es), kv = extent(n_kv, kv_batch_stride, tk, kv_row_stride, narrow, es);
+  const size_t os = extent(batch, out_batch_stride, tq, out_row_stride, wide, es);
+  const Span q_in{q, qs}, k_in{k, kv}, v_in{v, kv}, index{kv_index, (size_t)4 * batch}, len{kv_len, (size_t)4 * n_kv}, o_in{out, os},
+      lse_in{lse, (size_t)4 * batch * heads * tq}, do_in{dout, os}, dq_out{dq, qs}, dk_out{dk, kv}, dv_out{dv, kv}, ws{workspace, need};
+  // dk and dv may alternate row by row; each of them is held against everything else
+  bool clash = overlaps({dq_out, dk_out, ws}, {q_in, k_in, v_in, index, len, o_in, lse_in, do_in}) ||
+               overlaps({dq_out, dv_out, ws}, {q_in, k_in, v_in, index, len, o_in, lse_in, do_in});
+  if (dk && overlap(dk_out, dv_out)) {
+    const int64_t bytes = kv_row_stride * es, row = narrow * es;
+    const int64_t off = bytes ? (int64_t)(((intptr_t)dv - (intptr_t)dk) % bytes + bytes) % bytes : 0;
+    const bool regular = tk > 1 && bytes >= 2 * row && (n_kv == 1 || kv_batch_stride % kv_row_stride == 0);
+    clash = clash || !regular || off < row || off > bytes - row;
+  }
+  if (clash) return fail(FLASHBON_EINVAL, "outputs and workspace must not overlap an input or each other");
+  CrossArgs a{};
+  a.batch = batch; a.heads = heads; a.kv_heads = kv_heads; a.head_dim = head_dim; a.tq = tq; a.tk = tk; a.n_kv = n_kv;
+  a.q = q; a.q_bs = q_batch_stride; a.q_rs = q_row_stride;
+  a.k = k; a.v = v; a.kv_bs = kv_batch_stride; a.kv_rs = kv_row_stride;
+  a.kv_index = kv_index; a.kv_len = kv_len;
+  a.out = const_cast<void *>(out); a.o_bs = out_batch_stride; a.o_rs = out_row_stride; a.lse = const_cast<float *>(lse);
+  CrossGradArgs b;
+  b.dout = dout; b.dq = dq; b.dk = dk; b.dv = dv; b.workspace = workspace;
+  ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
+  return launched(launch_cross_attention_grad(t, a, b, (hipStream_t)stream), "cross_attention_grad");
+}
+
+flashbon_status flashbon_op_adapters(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t rank, int32_t n_adapters,
+                                     const void *x, const void *down, const void *up, const float *scales,
+                                     const int32_t *index, int32_t rows_per_group, int32_t epilogue, const float *gate,
+                                     const void *base, void *out, float *u, void *stream) {
+  const flashbon_status st = adapter_sizes(dtype, M, N, K, rank, n_adapters, rows_per_group);
+  if (st != FLASHBON_OK) return st;
+  if (epilogue != FLASHBON_EPI_STORE && epilogue != FLASHBON_EPI_STORE_F32 && epilogue != FLASHBON_EPI_RESIDUAL)
+    return fail(FLASHBON_EINVAL, "the epilogue must be STORE, STORE_F32 or RESIDUAL");
+  if (!x || !down || !up || !out || !u) return fail(FLASHBON_EINVAL, "x, down, up, out and u are required");
+  if (epilogue != FLASHBON_EPI_RESIDUAL) gate = nullptr;
+  if (!aligned({x, down, up, base, out, u}) || ((uintptr_t)scales | (uintptr_t)index | (uintptr_t)gate) % 4)
+    return fail(FLASHBON_EINVAL, "addresses must be on 16 bytes");
+  const size_t m = M, n = N, k = K, r = rank, c = n_adapters, es = dtype == FLASHBON_BF16 ? 2 : 4;
+  const bool f32 = epilogue != FLASHBON_EPI_STORE || dtype == FLASHBON_FP32;
+  const size_t outs = m * n * (f32 ? 4 : 2), groups = (m + rows_per_group - 1) / rows_per_group;
+  if (overlaps({{out, outs}, {u, 4 * m * r}},
+               {{x, m * k * es}, {down, c * r * k * es}, {up, c * n * r * es}, {scales, 4 * c}, {index, 4 * groups}, {gate, 4 * n},
+                {base == out ? nullptr : base, outs}}))
+    return fail(FLASHBON_EINVAL, "out and u must not overlap an input (but out base, which it may be) or each other");
+  AdapterArgs a;
+  a.M = M; a.N = N; a.K = K; a.rank = rank; a.count = n_adapters; a.per = std::min(rows_per_group, M);
+  a.x = x; a.down = down; a.up = up; a.scales = scales; a.index = index; a.gate = gate; a.base = base; a.out = out; a.u = u;
+  ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
+  return launched(launch_adapters(t, a, f32, (hipStream_t)stream), "adapters");
+}
+
+size_t flashbon_op_adapters_grad_workspace(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t rank, int32_t n_adapters,
+                                           int32_t rows_per_group) {
+  if (adapter_sizes(dtype, M, N, K, rank, n_adapters, rows_per_group) != FLASHBON_OK) return 0;
+  AdapterArgs a{};
+  a.M = M; a.N = N; a.K = K; a.rank = rank; a.count = n_adapters; a.per = std::min(rows_per_group, M);
+  return adapters_grad_workspace(dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32, a);
+}
+
+flashbon_status flashbon_op_adapters_grad(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t rank, int32_t n_adapters,
+                                          const void *x, const void *down, const void *up, const float *scales,
+                                          const int32_t *index, int32_t rows_per_group, const float *u, const void *dy,
+                                          int32_t epilogue, const void *base, void *dx, float *d_down, float *d_up,
+                                          void *workspace, size_t workspace_bytes, void *stream) {
+  const flashbon_status st = adapter_sizes(dtype, M, N, K, rank, n_adapters, rows_per_group);
+  if (st != FLASHBON_OK) return st;
+  if (epilogue != FLASHBON_EPI_STORE && epilogue != FLASHBON_EPI_STORE_F32)
+    return fail(FLASHBON_EINVAL, "the epilogue must be STORE or STORE_F32");
+  if (!x || !down || !up || !u || !dy) return fail(FLASHBON_EINVAL, "x, down, up, u and dy are required");
+  if (!dx && !d_down && !d_up) return fail(FLASHBON_EINVAL, "one of dx, d_down and d_up is required");
+  if (!dx) base = nullptr;
+  if (!aligned({x, down, up, u, dy, base, dx, d_down, d_up, workspace}) || ((uintptr_t)scales | (uintptr_t)index) % 4)
+    return fail(FLASHBON_EINVAL, "addresses must be on 16 bytes");
+  const size_t need = flashbon_op_adapters_grad_workspace(dtype, M, N, K, rank, n_adapters, rows_per_group);
+  if (!workspace || workspace_bytes < need) return fail(FLASHBON_ESHAPE, "the workspace is too small");
+  const size_t m = M, n = N, k = K, r = rank, c = n_adapters, es = dtype == FLASHBON_BF16 ? 2 : 4;
+  const bool f32 = epilogue == FLASHBON_EPI_STORE_F32 || dtype == FLASHBON_FP32;
+  const size_t dxs = m * k * (f32 ? 4 : 2), groups = (m + rows_per_group - 1) / rows_per_group;
+  if (overlaps({{dx, dxs}, {d_down, 4 * c * r * k}, {d_up, 4 * c * n * r}, {workspace, need}},
+               {{x, m * k * es}, {down, c * r * k * es}, {up, c * n * r * es}, {scales, 4 * c}, {index, 4 * groups}, {u, 4 * m * r},
+                {dy, m * n * es}, {base == dx ? nullptr : base, dxs}}))
+    return fail(FLASHBON_EINVAL, "outputs and workspace must not overlap an input (but dx base, which it may be) or each other");
+  AdapterArgs a;
+  a.M = M; a.N = N; a.K = K; a.rank = rank; a.count = n_adapters; a.per = std::min(rows_per_group, M);
+  a.x = x; a.down = down; a.up = up; a.scales = scales; a.index = index; a.u = const_cast<float *>(u);
+  AdapterGradArgs b;
+  b.dy = dy; b.base = base; b.dx = dx; b.d_down = d_down; b.d_up = d_up; b.workspace = workspace;
+  ActType t = dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32;
+  return launched(launch_adapters_grad(t, a, b, f32, (hipStream_t)stream), "adapters_grad");
 }
 
 }  // extern "C"

@@ -73,6 +73,10 @@ EXPORTS = [
     "flashbon_op_proxy", "flashbon_op_normals", "flashbon_op_unpatch_sde", "flashbon_select",
     "flashbon_refine_step_noalloc", "flashbon_op_linear_ws",
     "flashbon_op_quant_rows", "flashbon_op_linear_i8", "flashbon_op_norm_residual",
+    "flashbon_op_layer_norm", "flashbon_op_layer_norm_grad", "flashbon_op_layer_norm_grad_workspace",
+    "flashbon_op_cross_attention", "flashbon_op_cross_attention_workspace", "flashbon_op_cross_attention_grad",
+    "flashbon_op_cross_attention_grad_workspace", "flashbon_op_adapters", "flashbon_op_adapters_grad",
+    "flashbon_op_adapters_grad_workspace",
 ]
 NOALLOC_SCRATCH_BYTES = 128 << 20
 
@@ -145,6 +149,28 @@ def load() -> ctypes.CDLL:
     L.flashbon_op_linear_i8.restype = i32
     L.flashbon_op_norm_residual.argtypes = [i32, i32, i32, f32, vp, f32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
     L.flashbon_op_norm_residual.restype = i32
+    L.flashbon_op_layer_norm.argtypes = [i32, i32, i32, f32, vp, i32, vp, i32, vp, vp, vp, vp, vp]
+    L.flashbon_op_layer_norm.restype = i32
+    L.flashbon_op_layer_norm_grad.argtypes = [i32, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.flashbon_op_layer_norm_grad.restype = i32
+    L.flashbon_op_layer_norm_grad_workspace.argtypes = [i32] * 3
+    L.flashbon_op_layer_norm_grad_workspace.restype = sz
+    cross = [i32] * 7 + [vp, i64, i64, vp, vp, i64, i64, vp, i32, vp, vp, i64, i64, vp]
+    L.flashbon_op_cross_attention.argtypes = cross + [vp, sz, vp]
+    L.flashbon_op_cross_attention.restype = i32
+    L.flashbon_op_cross_attention_workspace.argtypes = [i32] * 7
+    L.flashbon_op_cross_attention_workspace.restype = sz
+    L.flashbon_op_cross_attention_grad.argtypes = cross + [vp, vp, vp, vp, vp, sz, vp]
+    L.flashbon_op_cross_attention_grad.restype = i32
+    L.flashbon_op_cross_attention_grad_workspace.argtypes = [i32] * 8
+    L.flashbon_op_cross_attention_grad_workspace.restype = sz
+    adapters = [i32] * 6 + [vp, vp, vp, vp, vp, i32]
+    L.flashbon_op_adapters.argtypes = adapters + [i32, vp, vp, vp, vp, vp]
+    L.flashbon_op_adapters.restype = i32
+    L.flashbon_op_adapters_grad.argtypes = adapters + [vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.flashbon_op_adapters_grad.restype = i32
+    L.flashbon_op_adapters_grad_workspace.argtypes = [i32] * 7
+    L.flashbon_op_adapters_grad_workspace.restype = sz
     L.flashbon_select.argtypes = [i32, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, ctypes.c_double,
                                   ctypes.c_double, JUDGE_FN, vp, ctypes.POINTER(ctypes.c_int32),
                                   ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)]
@@ -662,3 +688,225 @@ def flashbon_op_norm_residual(dtype, M, D, eps, x, y=None, *, alpha=1.0, post_no
                                                                        gate, shift, scale)
     _check(load().flashbon_op_norm_residual(dtype, M, D, eps, px, alpha, py, post_norm, pp, pg, ph, pre_norm, psh, psc, po,
                                             pq, pqs, _raw_stream(stream, x.get_device())), "flashbon_op_norm_residual")
+
+
+# The cross-attention branch with a prompt and an adapter per candidate, and its gradients.  Tensors are checked as above;
+# a workspace is a tensor of any type, of as many bytes as the ``_workspace`` function of the same sizes says.
+
+def _workspace_pointer(device: Optional[int], workspace) -> tuple:
+    """Address and bytes of a workspace (None: none)."""
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    if device is not None and workspace.get_device() != device:
+        raise ValueError(f"workspace must be on the current device (cuda:{device}), got {workspace.device}")
+    return workspace.data_ptr(), _nbytes(workspace)
+
+
+def _rows_of_heads(device: Optional[int], *wanted) -> list:
+    """Addresses of the tensors in ``wanted``, (name, tensor or None, dtype, batches, batch stride, rows, row stride, width,
+    required) each, strides in elements: views whose memory holds all of that."""
+    found = []
+    for name, t, dtype, n, batch_stride, rows, row_stride, width, required in wanted:
+        if t is None:
+            if required:
+                raise ValueError(f"{name} is required")
+            found.append(None)
+            continue
+        if t.dtype is not dtype:
+            raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+        if min(batch_stride, row_stride) < 0 or max(batch_stride, row_stride) >= 1 << 36:
+            raise ValueError(f"strides of {name} must be in [0, 2^36), got {batch_stride} and {row_stride}")
+        need = (n - 1) * batch_stride + (rows - 1) * row_stride + width
+        held = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        if held < need:
+            raise ValueError(f"{name} holds {held} elements from its first on, needs {need}")
+        if device is not None and t.get_device() != device:
+            raise ValueError(f"{name} must be on the current device (cuda:{device}), got {t.device}")
+        found.append(t.data_ptr())
+    return found
+
+
+def _groups(rows: int, rows_per_group: int) -> int:
+    if rows_per_group < 1:
+        raise ValueError(f"rows_per_group must be at least 1, got {rows_per_group}")
+    return -(-rows // rows_per_group)
+
+
+def validate_layer_norm(dtype, M, D, x, out, weight=None, bias=None, rows_per_group=1, mean=None, rstd=None, *,
+                        require_device: bool = True) -> list:
+    """Raise ValueError unless the tensors are what flashbon_op_layer_norm reads and writes; their addresses."""
+    act, device = _act(dtype), _current_device(require_device)
+    f32 = _torch.float32
+    _int32(M, D, rows_per_group)
+    vectors = _groups(M, rows_per_group) * D
+    return _pointers(device, ("x", x, f32, M * D, True), ("weight", weight, f32, vectors, False),
+                     ("bias", bias, f32, vectors, False), ("out", out, act, M * D, True), ("mean", mean, f32, M, False),
+                     ("rstd", rstd, f32, M, False))
+
+
+def flashbon_op_layer_norm(dtype, M, D, eps, x, out, *, weight=None, bias=None, rows_per_group=None, modulated=False,
+                           mean=None, rstd=None, stream=None):
+    """LayerNorm of x [M][D] times weight (``modulated``: 1 + weight) plus bias, a vector for each ``rows_per_group`` rows
+    (None: one for all); ``mean`` and ``rstd`` [M] for the gradient."""
+    per = max(int(M), 1) if rows_per_group is None else rows_per_group
+    px, pw, pb, po, pm, pr = validate_layer_norm(dtype, M, D, x, out, weight, bias, per, mean, rstd)
+    _check(load().flashbon_op_layer_norm(dtype, M, D, eps, px, per, pw, int(bool(modulated)), pb, po, pm, pr,
+                                         _raw_stream(stream, x.get_device())), "flashbon_op_layer_norm")
+
+
+def flashbon_op_layer_norm_grad_workspace(M, D, rows_per_group=None) -> int:
+    """Bytes of the workspace flashbon_op_layer_norm_grad needs."""
+    _int32(M, D)
+    return int(load().flashbon_op_layer_norm_grad_workspace(M, D, max(int(M), 1) if rows_per_group is None else rows_per_group))
+
+
+def validate_layer_norm_grad(dtype, M, D, x, mean, rstd, dy, dx=None, weight=None, rows_per_group=1, residual=None,
+                             dweight=None, dbias=None, workspace=None, *, require_device: bool = True) -> list:
+    """Raise ValueError unless the tensors are what flashbon_op_layer_norm_grad reads and writes; their addresses."""
+    act, device = _act(dtype), _current_device(require_device)
+    f32 = _torch.float32
+    _int32(M, D, rows_per_group)
+    vectors = _groups(M, rows_per_group) * D
+    return _pointers(device, ("x", x, f32, M * D, True), ("weight", weight, f32, vectors, False), ("mean", mean, f32, M, True),
+                     ("rstd", rstd, f32, M, True), ("dy", dy, act, M * D, True), ("residual", residual, f32, M * D, False),
+                     ("dx", dx, f32, M * D, False), ("dweight", dweight, f32, vectors, False),
+                     ("dbias", dbias, f32, vectors, False)) + list(_workspace_pointer(device, workspace))
+
+
+def flashbon_op_layer_norm_grad(dtype, M, D, x, mean, rstd, dy, dx=None, *, weight=None, rows_per_group=None, modulated=False,
+                                residual=None, dweight=None, dbias=None, workspace=None, stream=None):
+    """dx = residual + the gradient of x, and dweight and dbias, from dy and the saved statistics."""
+    per = max(int(M), 1) if rows_per_group is None else rows_per_group
+    px, pw, pm, pr, py, pres, pdx, pdw, pdb, ws, nbytes = validate_layer_norm_grad(
+        dtype, M, D, x, mean, rstd, dy, dx, weight, per, residual, dweight, dbias, workspace)
+    _check(load().flashbon_op_layer_norm_grad(dtype, M, D, px, per, pw, int(bool(modulated)), pm, pr, py, pres, pdx, pdw, pdb,
+                                              ws, nbytes, _raw_stream(stream, x.get_device())), "flashbon_op_layer_norm_grad")
+
+
+def _cross_tensors(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv, device, rows, vectors) -> list:
+    _int32(batch, heads, kv_heads, head_dim, tq, tk, n_kv)
+    if min(batch, heads, kv_heads, head_dim, tq, tk, n_kv) < 1:
+        raise ValueError("batch, heads, kv_heads, head_dim, tq, tk and n_kv must be at least 1")
+    return _rows_of_heads(device, *rows) + _pointers(device, *vectors)
+
+
+def validate_cross_attention(dtype, batch, heads, kv_heads, head_dim, tq, tk, q, q_bs, q_rs, k, v, kv_bs, kv_rs, kv_index, n_kv,
+                             kv_len, out, o_bs, o_rs, lse=None, workspace=None, *, require_device: bool = True) -> list:
+    """Raise ValueError unless the tensors are what flashbon_op_cross_attention reads and writes; their addresses."""
+    act, device = _act(dtype), _current_device(require_device)
+    wide, narrow, i32 = heads * head_dim, kv_heads * head_dim, _torch.int32
+    return _cross_tensors(
+        dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv, device,
+        (("q", q, act, batch, q_bs, tq, q_rs, wide, True), ("k", k, act, n_kv, kv_bs, tk, kv_rs, narrow, True),
+         ("v", v, act, n_kv, kv_bs, tk, kv_rs, narrow, True), ("out", out, act, batch, o_bs, tq, o_rs, wide, True)),
+        (("kv_index", kv_index, i32, batch, False), ("kv_len", kv_len, i32, n_kv, False),
+         ("lse", lse, _torch.float32, batch * heads * tq, False))) + list(_workspace_pointer(device, workspace))
+
+
+def flashbon_op_cross_attention(dtype, batch, heads, kv_heads, head_dim, tq, tk, q, q_bs, q_rs, k, v, kv_bs, kv_rs, kv_index,
+                                n_kv, kv_len, out, o_bs, o_rs, *, lse=None, workspace=None, stream=None):
+    """Attention of each batch row to the first kv_len of its prompt's tk keys; ``lse`` [batch][heads][tq] for the gradient."""
+    pq, pk, pv, po, pi, pn, pl, ws, nbytes = validate_cross_attention(
+        dtype, batch, heads, kv_heads, head_dim, tq, tk, q, q_bs, q_rs, k, v, kv_bs, kv_rs, kv_index, n_kv, kv_len, out, o_bs,
+        o_rs, lse, workspace)
+    _check(load().flashbon_op_cross_attention(dtype, batch, heads, kv_heads, head_dim, tq, tk, pq, q_bs, q_rs, pk, pv, kv_bs,
+                                              kv_rs, pi, n_kv, pn, po, o_bs, o_rs, pl, ws, nbytes,
+                                              _raw_stream(stream, q.get_device())), "flashbon_op_cross_attention")
+
+
+def flashbon_op_cross_attention_workspace(dtype, batch, heads, kv_heads, head_dim, tq, tk) -> int:
+    """Bytes of the workspace with which flashbon_op_cross_attention cuts long keys into ranges."""
+    _int32(batch, heads, kv_heads, head_dim, tq, tk)
+    return int(load().flashbon_op_cross_attention_workspace(dtype, batch, heads, kv_heads, head_dim, tq, tk))
+
+
+def validate_cross_attention_grad(dtype, batch, heads, kv_heads, head_dim, tq, tk, q, q_bs, q_rs, k, v, kv_bs, kv_rs, kv_index,
+                                  n_kv, kv_len, out, o_bs, o_rs, lse, dout, dq=None, dk=None, dv=None, workspace=None, *,
+                                  require_device: bool = True) -> list:
+    """Raise ValueError unless the tensors are what flashbon_op_cross_attention_grad reads and writes; their addresses."""
+    act, device = _act(dtype), _current_device(require_device)
+    wide, narrow, i32 = heads * head_dim, kv_heads * head_dim, _torch.int32
+    return _cross_tensors(
+        dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv, device,
+        (("q", q, act, batch, q_bs, tq, q_rs, wide, True), ("k", k, act, n_kv, kv_bs, tk, kv_rs, narrow, True),
+         ("v", v, act, n_kv, kv_bs, tk, kv_rs, narrow, True), ("out", out, act, batch, o_bs, tq, o_rs, wide, True),
+         ("dout", dout, act, batch, o_bs, tq, o_rs, wide, True), ("dq", dq, act, batch, q_bs, tq, q_rs, wide, False),
+         ("dk", dk, act, n_kv, kv_bs, tk, kv_rs, narrow, False), ("dv", dv, act, n_kv, kv_bs, tk, kv_rs, narrow, False)),
+        (("kv_index", kv_index, i32, batch, False), ("kv_len", kv_len, i32, n_kv, False),
+         ("lse", lse, _torch.float32, batch * heads * tq, True))) + list(_workspace_pointer(device, workspace))
+
+
+def flashbon_op_cross_attention_grad(dtype, batch, heads, kv_heads, head_dim, tq, tk, q, q_bs, q_rs, k, v, kv_bs, kv_rs,
+                                     kv_index, n_kv, kv_len, out, o_bs, o_rs, lse, dout, dq=None, dk=None, dv=None, *,
+                                     workspace=None, stream=None):
+    """dq (q's strides), dk and dv (k's) from dout (out's), out and lse; dq, or dk and dv, may be None."""
+    pq, pk, pv, po, pdo, pdq, pdk, pdv, pi, pn, pl, ws, nbytes = validate_cross_attention_grad(
+        dtype, batch, heads, kv_heads, head_dim, tq, tk, q, q_bs, q_rs, k, v, kv_bs, kv_rs, kv_index, n_kv, kv_len, out, o_bs,
+        o_rs, lse, dout, dq, dk, dv, workspace)
+    _check(load().flashbon_op_cross_attention_grad(dtype, batch, heads, kv_heads, head_dim, tq, tk, pq, q_bs, q_rs, pk, pv,
+                                                   kv_bs, kv_rs, pi, n_kv, pn, po, o_bs, o_rs, pl, pdo, pdq, pdk, pdv, ws,
+                                                   nbytes, _raw_stream(stream, q.get_device())),
+           "flashbon_op_cross_attention_grad")
+
+
+def flashbon_op_cross_attention_grad_workspace(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv) -> int:
+    """Bytes of the workspace flashbon_op_cross_attention_grad needs."""
+    _int32(batch, heads, kv_heads, head_dim, tq, tk, n_kv)
+    return int(load().flashbon_op_cross_attention_grad_workspace(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv))
+
+
+def validate_adapters(dtype, M, N, K, rank, n_adapters, x, down, up, scales, index, rows_per_group, epilogue, base, out, u,
+                      gate=None, *, require_device: bool = True) -> list:
+    """Raise ValueError unless the tensors are what flashbon_op_adapters reads and writes; their addresses."""
+    act, device = _act(dtype), _current_device(require_device)
+    f32 = _torch.float32
+    _int32(M, N, K, rank, n_adapters, rows_per_group, epilogue)
+    groups, outs = _groups(M, rows_per_group), act if epilogue == EPI_STORE else f32
+    return _pointers(device, ("x", x, act, M * K, True), ("down", down, act, n_adapters * rank * K, True),
+                     ("up", up, act, n_adapters * N * rank, True), ("scales", scales, f32, n_adapters, False),
+                     ("index", index, _torch.int32, groups, False),
+                     ("gate", gate if epilogue == EPI_RESIDUAL else None, f32, N, False), ("base", base, outs, M * N, False),
+                     ("out", out, outs, M * N, True), ("u", u, f32, M * rank, True))
+
+
+def flashbon_op_adapters(dtype, M, N, K, rank, n_adapters, x, down, up, scales, index, rows_per_group, epilogue, base, out, u,
+                         *, gate=None, stream=None):
+    """out = base + gate scales[a] (x down[a]^T) up[a]^T, a = index of each ``rows_per_group`` rows; u = x down^T (fp32)."""
+    px, pd, pu, ps, pi, pg, pb, po, pmid = validate_adapters(dtype, M, N, K, rank, n_adapters, x, down, up, scales, index,
+                                                             rows_per_group, epilogue, base, out, u, gate)
+    _check(load().flashbon_op_adapters(dtype, M, N, K, rank, n_adapters, px, pd, pu, ps, pi, rows_per_group, epilogue, pg, pb,
+                                       po, pmid, _raw_stream(stream, x.get_device())), "flashbon_op_adapters")
+
+
+def flashbon_op_adapters_grad_workspace(dtype, M, N, K, rank, n_adapters, rows_per_group) -> int:
+    """Bytes of the workspace flashbon_op_adapters_grad needs."""
+    _int32(M, N, K, rank, n_adapters, rows_per_group)
+    return int(load().flashbon_op_adapters_grad_workspace(dtype, M, N, K, rank, n_adapters, rows_per_group))
+
+
+def validate_adapters_grad(dtype, M, N, K, rank, n_adapters, x, down, up, scales, index, rows_per_group, u, dy, epilogue, base,
+                           dx=None, d_down=None, d_up=None, workspace=None, *, require_device: bool = True) -> list:
+    """Raise ValueError unless the tensors are what flashbon_op_adapters_grad reads and writes; their addresses."""
+    act, device = _act(dtype), _current_device(require_device)
+    f32 = _torch.float32
+    _int32(M, N, K, rank, n_adapters, rows_per_group, epilogue)
+    groups, outs = _groups(M, rows_per_group), act if epilogue == EPI_STORE else f32
+    downs, ups = n_adapters * rank * K, n_adapters * N * rank
+    return _pointers(device, ("x", x, act, M * K, True), ("down", down, act, downs, True), ("up", up, act, ups, True),
+                     ("scales", scales, f32, n_adapters, False), ("index", index, _torch.int32, groups, False),
+                     ("u", u, f32, M * rank, True), ("dy", dy, act, M * N, True), ("base", base, outs, M * K, False),
+                     ("dx", dx, outs, M * K, False), ("d_down", d_down, f32, downs, False),
+                     ("d_up", d_up, f32, ups, False)) + list(_workspace_pointer(device, workspace))
+
+
+def flashbon_op_adapters_grad(dtype, M, N, K, rank, n_adapters, x, down, up, scales, index, rows_per_group, u, dy, epilogue,
+                              base, dx=None, d_down=None, d_up=None, *, workspace=None, stream=None):
+    """dx = base + the adapters' gradient of x, d_down and d_up (fp32), from dy and u."""
+    px, pd, pu, ps, pi, pmid, py, pb, pdx, pdd, pdu, ws, nbytes = validate_adapters_grad(
+        dtype, M, N, K, rank, n_adapters, x, down, up, scales, index, rows_per_group, u, dy, epilogue, base, dx, d_down, d_up,
+        workspace)
+    _check(load().flashbon_op_adapters_grad(dtype, M, N, K, rank, n_adapters, px, pd, pu, ps, pi, rows_per_group, pmid, py,
+                                            epilogue, pb, pdx, pdd, pdu, ws, nbytes, _raw_stream(stream, x.get_device())),
+           "flashbon_op_adapters_grad")
