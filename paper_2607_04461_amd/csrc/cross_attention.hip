@@ -275,22 +275,28 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossP p) {
   }
 }
 
-// delta[b][h][i] = sum_d dout out: head_dim / 8 lanes a row
+// delta of a row: lane half g of two takes eights 2 c + g of the row, in order, and the halves are added.
+template <typename T>
+__device__ __forceinline__ float delta_part(float s, Frag<T> x, Frag<T> y) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s = fmaf(to_f32(x[e]), to_f32(y[e]), s);
+  return s;
+}
+
+// delta[b][h][i] = sum_d dout out, two lanes a row, 32 lanes apart
 template <typename T>
 __global__ __launch_bounds__(256) void k_cross_delta(CrossP p) {
   const CrossArgs &a = p.a;
-  const int lanes = a.head_dim / 8, at = threadIdx.x % lanes;
-  const int64_t rows = (int64_t)a.batch * a.tq * a.heads, step = (int64_t)gridDim.x * 256 / lanes;
-  // a wave's lanes leave the loop together: the exchange below needs all of a row's lanes, which share r
-  for (int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes; r < rows; r += step) {
+  const int li = threadIdx.x & 31, g = threadIdx.x >> 5 & 1;
+  const int64_t rows = (int64_t)a.batch * a.tq * a.heads, step = (int64_t)gridDim.x * 128;
+  for (int64_t r0 = (int64_t)blockIdx.x * 128 + (threadIdx.x >> 6) * 32; r0 < rows; r0 += step) {   // whole waves
+    const int64_t r = min(r0 + li, rows - 1);
     const int h = (int)(r % a.heads), i = (int)(r / a.heads % a.tq), b = (int)(r / a.heads / a.tq);
-    const int64_t from = b * a.o_bs + (int64_t)i * a.o_rs + h * a.head_dim + 8 * at;
-    const Frag<T> x = load_frag((const T *)a.out + from), y = load_frag((const T *)p.dout + from);
+    const int64_t from = b * a.o_bs + (int64_t)i * a.o_rs + h * a.head_dim;
     float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(to_f32(x[e]), to_f32(y[e]), s);
-    for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    if (at == 0) p.delta[((int64_t)b * a.heads + h) * a.tq + i] = s;
+    for (int c = 8 * g; c < a.head_dim; c += 16) s = delta_part<T>(s, load_frag((const T *)a.out + from + c), load_frag((const T *)p.dout + from + c));
+    s += __shfl_xor(s, 32, 64);
+    if (g == 0 && r0 + li < rows) p.delta[((int64_t)b * a.heads + h) * a.tq + i] = s;
   }
 }
 
@@ -393,7 +399,20 @@ __global__ __launch_bounds__(256) void k_cross_dq(CrossP p) {
   }
 }
 
-constexpr int MOST_BATCH = 4096;
+// The prompt's candidates in order into list, by the first wave; their number.
+__device__ __forceinline__ void list_candidates(const CrossArgs &a, int c, int *list, int *count) {
+  if (threadIdx.x < 64) {
+    int n = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+      const bool mine = b0 + (int)threadIdx.x < a.batch && prompt_of(a, b0 + threadIdx.x) == c;
+      const uint64_t votes = __ballot(mine);
+      if (mine) list[n + __popcll(votes & ((1ull << threadIdx.x) - 1))] = b0 + threadIdx.x;
+      n += __popcll(votes);
+    }
+    if (threadIdx.x == 0) *count = n;
+  }
+  __syncthreads();
+}
 
 // Keys [128 kb ...) of a prompt's key head against a range of the (candidate, head, query tile) triples that read them.
 template <typename T, int DH, int NK>
@@ -409,17 +428,7 @@ __global__ __launch_bounds__(256, 1) void k_cross_dkv(CrossP p) {
   const int kb = blockIdx.x, c = blockIdx.y / a.kv_heads, kh = blockIdx.y % a.kv_heads, split = blockIdx.z;
   const int len = keys_of(a, c), shared = a.heads / a.kv_heads;
   if (p.splits > 1 && kb * KB >= len) return;       // k_cross_sum writes those rows
-  if (threadIdx.x < 64) {                           // the prompt's candidates
-    int n = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 64) {
-      const bool mine = b0 + lane < a.batch && prompt_of(a, b0 + lane) == c;
-      const uint64_t votes = __ballot(mine);
-      if (mine) s_list[n + __popcll(votes & ((1ull << lane) - 1))] = b0 + lane;
-      n += __popcll(votes);
-    }
-    if (lane == 0) *s_count = n;
-  }
-  __syncthreads();
+  list_candidates(a, c, s_list, s_count);
   const int key0 = kb * KB + w * 16 * NK;
   const T *K = (const T *)a.k + c * a.kv_bs + kh * a.head_dim, *V = (const T *)a.v + c * a.kv_bs + kh * a.head_dim;
   Frag<T> kf[NK][NC], vf[NK][NC];
@@ -539,6 +548,386 @@ __global__ __launch_bounds__(256, 1) void k_cross_dkv(CrossP p) {
   }
 }
 
+// ---- bf16, head dims 64 and 128: 32 x 32 x 16 products, a wave's 32 queries (or keys) in registers.
+// A product's lane holds rows 8 (r >> 2) + 4 g + (r & 3) of column lane & 31 (g = lane >> 5, r < 16), so registers 8 c ..
+// 8 c + 7 are the right operand of the next product's 16 k of chunk c, in the order 4 g + 0..3, 8 + 4 g + 0..3.  Its left
+// operand comes out of a transposed copy of the tile in LDS whose groups of four are kept in that order, so that it is one
+// 16-byte read (gfx950's transposing reads pass 71 bytes a clock and CU here, 16-byte reads 190, and the products of one
+// candidate's tile need 128).  The copy costs each thread a few 8-byte reads, byte permutations and writes a tile.
+// Both corrections enter as the accumulators' first values: S starts at -lse, dP at -delta, so that a pair of exponent and
+// product is all that is left to do for an element.
+namespace x32 {
+
+constexpr int QT = 64;               // rows of a tile
+constexpr int TP = QT * 2 + 16;      // bytes of a row of the transposed copy
+// 16-byte chunk c of row r of a tile without padding is kept at c ^ swz(r): the 16 rows of a read phase at one chunk fall
+// into 16 different places of the banks' 256 bytes
+template <int DH> __device__ __forceinline__ int swz(int r) { return DH == 128 ? r & 15 : (r >> 1) & 7; }
+template <int DH> __device__ __forceinline__ int row_at(int r, int c) { return r * DH * 2 + ((c ^ swz<DH>(r)) << 4); }
+// place of the four rows 4 qg .. 4 qg + 3 of column d
+__device__ __forceinline__ int column_at(int d, int qg) {
+  const int gi = qg & 3, place = (gi & 1) << 1 | gi >> 1, slot = (qg >> 2) * 2 + (place >> 1);
+  return d * TP + ((slot ^ (d >> 4 & 7)) << 4) + (place & 1) * 8;
+}
+// Left operands.  Of a tile: row 32 x + li, chunk 2 k + g, at row_base ^ 32 k; of the copy: column 32 d + li, the rows of
+// chunk c and lane half g, whose place (2 c + g) ^ (2 d + li / 16) is 2 (c ^ d) + (g ^ li / 16).
+// v as a new value: what is computed from it inside a loop is not kept in registers across the loop
+__device__ __forceinline__ int fresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+template <int DH> __device__ __forceinline__ int row_base(int li, int g) { return row_at<DH>(li, g); }
+template <int DH> __device__ __forceinline__ bf16x8 row_frag(const char *t, int base, int x, int k) {
+  return *reinterpret_cast<const bf16x8 *>(t + 32 * x * DH * 2 + (base ^ (k << 5)));
+}
+__device__ __forceinline__ int column_base(int li, int g) { return li * TP + ((g ^ (li >> 4)) << 4); }
+__device__ __forceinline__ bf16x8 column_frag(const char *t, int base, int d, int c) {
+  return *reinterpret_cast<const bf16x8 *>(t + base + d * 32 * TP + ((c ^ d) << 5));
+}
+// Rows 4 qg .. + 3 of columns 4 dg .. + 3, a register pair a row.  In a tile: row e at (place ^ 16 e) + e rows; in the copy:
+// column e at place + e TP, with the rows of a column beside each other.
+template <int DH> __device__ __forceinline__ int block_rows(int dg, int qg) { return row_at<DH>(4 * qg, dg >> 1) + (dg & 1) * 8; }
+template <int DH> __device__ __forceinline__ int block_row(int place, int e) {
+  return (place ^ (DH == 128 ? e << 4 : (e >> 1) << 4)) + e * DH * 2;
+}
+__device__ __forceinline__ int block_columns(int dg, int qg) { return column_at(4 * dg, qg); }
+__device__ __forceinline__ void store_columns(char *t, const u32x2 (&r)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+    const int x = e >> 1;
+    *reinterpret_cast<u32x2 *>(t + e * TP) =
+        u32x2{__builtin_amdgcn_perm(r[1][x], r[0][x], sel), __builtin_amdgcn_perm(r[3][x], r[2][x], sel)};
+  }
+}
+// `valid` rows of dh elements at stride as a buffer: what lies past it reads as zero.  off(row): a row's offset, or past it
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const bf16 *at, int stride, int valid, int dh) {
+  const uint64_t x = (uint64_t)at;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  const uint32_t bytes = __builtin_amdgcn_readfirstlane((uint32_t)((valid - 1) * stride + dh) * 2u);
+  return __builtin_amdgcn_make_buffer_rsrc((void *)(((uint64_t)hi << 32) | lo), (short)0, (int)bytes, 0x00020000);
+}
+__device__ __forceinline__ uint32_t off(int row, int stride, int col, int valid) {
+  return row < valid ? (uint32_t)(row * stride + col) * 2u : 0x80000000u;
+}
+__device__ __forceinline__ f32x16 mma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+// registers 8 c .. 8 c + 7 as an operand
+__device__ __forceinline__ bf16x8 chunk_frag(const f32x16 &v, int c) {
+  bf16x8 f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = (bf16)v[8 * c + i];
+  return f;
+}
+
+// dq of 128 queries, 32 a wave; also delta, for k_dkv.
+template <int DH>
+__global__ __launch_bounds__(256, 2) void k_dq(CrossP p) {
+  constexpr int NC = DH / 16, ND = DH / 32, DG = DH / 4, BLOCKS = 16 * DG / 256, VN = 64 * DH / 8 / 256;
+  extern __shared__ __attribute__((aligned(16))) char s_mem[];
+  char *sk = s_mem, *sv = sk + QT * DH * 2, *st = sv + QT * DH * 2;     // k, v, k transposed
+  int b, h, qb;
+  if (!unit_of(p, blockIdx.x, b, h, qb)) return;
+  const CrossArgs &a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, g = lane >> 5, w = tid >> 6;
+  const int q0 = (qb * 4 + w) * 32, c = prompt_of(a, b), len = keys_of(a, c), kh = h / (a.heads / a.kv_heads);
+  const bool idle = q0 >= a.tq;
+  const int tiles = (len + QT - 1) / QT, i = q0 + li, at = min(i, a.tq - 1);
+  const bf16 *K = (const bf16 *)a.k + c * a.kv_bs + kh * DH, *V = (const bf16 *)a.v + c * a.kv_bs + kh * DH;
+  bf16x8 qf[NC], df[NC];
+  const int64_t r = ((int64_t)b * a.heads + h) * a.tq + at;
+  float delta = 0.f;
+  {
+    const bf16 *Q = (const bf16 *)a.q + b * a.q_bs + (int64_t)at * a.q_rs + h * DH;
+    const int64_t from = b * a.o_bs + (int64_t)at * a.o_rs + h * DH;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+      qf[k] = load_frag(Q + 16 * k + 8 * g);
+      df[k] = load_frag((const bf16 *)p.dout + from + 16 * k + 8 * g);
+      delta = delta_part<bf16>(delta, load_frag((const bf16 *)a.out + from + 16 * k + 8 * g), df[k]);
+    }
+    delta += __shfl_xor(delta, 32, 64);
+    if (g == 0 && i < a.tq) p.delta[r] = delta;
+  }
+  const float lse = a.lse[r] == -INFINITY ? INFINITY : a.lse[r] * LOG2E / p.qscale;
+  f32x16 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+  u32x2 kr[BLOCKS][4];
+  u32x4 vr[VN];
+  const int rs = (int)a.kv_rs, cb = column_base(li, g);
+  const int dg = tid % DG, qg = tid / DG, ch = tid % (DH / 8), vrow = tid / (DH / 8);
+  auto load = [&](int t) __attribute__((always_inline)) {
+    const int valid = min(QT, len - t * QT);
+    const __amdgpu_buffer_rsrc_t kt = rows_rsrc(K + (int64_t)t * QT * a.kv_rs, rs, valid, DH), vt = rows_rsrc(V + (int64_t)t * QT * a.kv_rs, rs, valid, DH);
+    const int kf = fresh(4 * qg), vf = fresh(vrow);
+#pragma unroll
+    for (int x = 0; x < BLOCKS; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        kr[x][e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(kt, off(kf + 1024 / DG * x + e, rs, 4 * dg, valid), 0, 0));
+#pragma unroll
+    for (int x = 0; x < VN; ++x)
+      vr[x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vt, off(vf + 2048 / DH * x, rs, 8 * ch, valid), 0, 0));
+  };
+  auto land = [&]() __attribute__((always_inline)) {
+    const int br = fresh(block_rows<DH>(dg, qg)), bc = fresh(block_columns(dg, qg)), vb = fresh(row_at<DH>(vrow, ch));
+#pragma unroll
+    for (int x = 0; x < BLOCKS; ++x) {      // 1024 / DG rows further: the same chunk, and a place 1024 / DG / 16 pairs on
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x2 *>(sk + block_row<DH>(br, e) + x * (1024 / DG) * DH * 2) = kr[x][e];
+      store_columns(st + (x ? block_columns(dg, qg + 256 / DG * x) : bc), kr[x]);
+    }
+#pragma unroll
+    for (int x = 0; x < VN; ++x) *reinterpret_cast<u32x4 *>(sv + vb + x * 2048 / DH * DH * 2) = vr[x];
+  };
+  if (tiles) load(0);
+  for (int t = 0; t < tiles; ++t) {
+    __syncthreads();          // the last tile has been read
+    land();
+    __syncthreads();
+    if (t + 1 < tiles) load(t + 1);
+    if (idle) continue;
+    const int rb = fresh(row_base<DH>(li, g));
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[e] = -lse;
+        dp[e] = -delta;
+      }
+      bf16x8 f[4][2], cf[2 * ND];       // operands, read two steps ahead
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        f[k][0] = row_frag<DH>(sk, rb, x, k);
+        f[k][1] = row_frag<DH>(sv, rb, x, k);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < NC; ++k) {
+        if (k + 2 < NC) {
+          f[(k + 2) & 3][0] = row_frag<DH>(sk, rb, x, k + 2);
+          f[(k + 2) & 3][1] = row_frag<DH>(sv, rb, x, k + 2);
+        } else {
+          cf[2 * (k + 2 - NC)] = column_frag(st, cb, 2 * (k + 2 - NC) % ND, 2 * x + 2 * (k + 2 - NC) / ND);
+          cf[2 * (k + 2 - NC) + 1] = column_frag(st, cb, (2 * (k + 2 - NC) + 1) % ND, 2 * x + (2 * (k + 2 - NC) + 1) / ND);
+        }
+        s = mma32(f[k & 3][0], qf[k], s);
+        dp = mma32(f[k & 3][1], df[k], dp);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dp[e] *= __builtin_amdgcn_exp2f(s[e] * p.qscale);
+      if ((t + 1) * QT > len) {        // keys past the end: exp(-lse) may be anything, and infinity times their zeros a NaN
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (t * QT + 32 * x + 8 * (e >> 2) + 4 * g + (e & 3) >= len) dp[e] = 0.f;
+      }
+      const bf16x8 df2[2] = {chunk_frag(dp, 0), chunk_frag(dp, 1)};
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int y = 0; y < 2 * ND; ++y) {
+        if (y + 4 < 2 * ND) cf[y + 4] = column_frag(st, cb, (y + 4) % ND, 2 * x + (y + 4) / ND);
+        o[y % ND] = mma32(cf[y], df2[y / ND], o[y % ND]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  if (i >= a.tq) return;
+  bf16 *O = (bf16 *)p.dq + b * a.q_bs + (int64_t)i * a.q_rs + h * DH + 4 * g;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<bf16x4 *>(O + 32 * d + 8 * e) = bf16x4{(bf16)(o[d][4 * e] * p.scale), (bf16)(o[d][4 * e + 1] * p.scale),
+                                                               (bf16)(o[d][4 * e + 2] * p.scale), (bf16)(o[d][4 * e + 3] * p.scale)};
+}
+
+constexpr int KEYS = 256;            // keys of a workgroup of k_dkv, 32 a wave
+
+// dk and dv of 256 keys of a prompt's key head against a range of the (candidate, head, query tile) triples that read them.
+// The tiles of q and dout reach LDS by loads that write it themselves, one tile ahead in two buffers; rows past tq are past
+// the buffer's range and read as zero.
+template <int DH>
+__global__ __launch_bounds__(512) void k_dkv(CrossP p) {
+  constexpr int NC = DH / 16, ND = DH / 32, RB = DH * 2, TILE_B = QT * RB, NCH = RB / 16, ROWS = 64 / NCH;
+  extern __shared__ __attribute__((aligned(16))) char s_mem[];
+  char *rows = s_mem, *tq = rows + 4 * TILE_B, *td = tq + DH * TP;      // [2][q, dout], then their transposed copies
+  float *s_lse = reinterpret_cast<float *>(td + DH * TP), *s_delta = s_lse + 2 * QT;
+  int *s_list = reinterpret_cast<int *>(s_delta + 2 * QT), *s_count = s_list + p.a.batch;
+  const CrossArgs &a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, g = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // the key blocks of one range of queries follow each other on one XCD, whose L2 then holds its q and dout
+  const int nkb = (a.tk + KEYS - 1) / KEYS, units = a.n_kv * a.kv_heads, rest = blockIdx.x >> 3;
+  const int kb = rest % nkb, uu = rest / nkb * 8 + (blockIdx.x & 7);
+  if (uu >= units * p.splits) return;
+  const int c = uu % units / a.kv_heads, kh = uu % a.kv_heads, split = uu / units;
+  const int len = keys_of(a, c), shared = a.heads / a.kv_heads;
+  if (p.splits > 1 && kb * KEYS >= len) return;       // k_cross_sum writes those rows
+  list_candidates(a, c, s_list, s_count);
+  const int key0 = kb * KEYS + w * 32, key = key0 + li;
+  const bf16 *K = (const bf16 *)a.k + c * a.kv_bs + (int64_t)min(key, a.tk - 1) * a.kv_rs + kh * DH;
+  const bf16 *V = (const bf16 *)a.v + c * a.kv_bs + (int64_t)min(key, a.tk - 1) * a.kv_rs + kh * DH;
+  bf16x8 kf[NC], vf[NC];
+#pragma unroll
+  for (int k = 0; k < NC; ++k) {
+    kf[k] = key < len ? load_frag(K + 16 * k + 8 * g) : zero_frag<bf16>();
+    vf[k] = key < len ? load_frag(V + 16 * k + 8 * g) : zero_frag<bf16>();
+  }
+  f32x16 dk[ND], dv[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dk[d][e] = dv[d][e] = 0.f;
+  const int nqt = (a.tq + QT - 1) / QT;
+  const int64_t all = kb * KEYS < len ? (int64_t)*s_count * shared * nqt : 0;
+  const int64_t u0 = all * split / p.splits, u1 = all * (split + 1) / p.splits;
+  constexpr int COPIES = 2 * 16 * (DH / 4) / 512;
+  const int cb = column_base(li, g), which = COPIES == 2 ? 0 : tid / 256, dg = tid % (DH / 4), qg = tid / (DH / 4) % 16;
+  const int q_rs = (int)a.q_rs, o_rs = (int)a.o_rs;
+  int qt = (int)(u0 % nqt), hs = (int)(u0 / nqt % shared), bi = (int)(u0 / nqt / shared);   // the triple to load next
+  float ls = 0.f, de = 0.f;
+  auto load = [&](int buf) __attribute__((always_inline)) {
+    const int h = kh * shared + hs, b = __builtin_amdgcn_readfirstlane(s_list[bi]), valid = min(QT, a.tq - qt * QT);
+    const __amdgpu_buffer_rsrc_t rq = rows_rsrc((const bf16 *)a.q + b * a.q_bs + (int64_t)qt * QT * a.q_rs + h * DH, q_rs, valid, DH);
+    const __amdgpu_buffer_rsrc_t rd = rows_rsrc((const bf16 *)p.dout + b * a.o_bs + (int64_t)qt * QT * a.o_rs + h * DH, o_rs, valid, DH);
+#pragma unroll
+    for (int x = 0; x < QT / ROWS / 8; ++x) {       // a load fills ROWS rows, 64 chunks; each wave takes its share of them
+      const int first = (w * (QT / ROWS / 8) + x) * ROWS, row = first + lane / NCH, ch = lane % NCH ^ swz<DH>(row);
+      char *to = rows + buf * 2 * TILE_B + first * RB;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (__attribute__((address_space(3))) void *)to, 16, off(row, q_rs, 8 * ch, valid), 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rd, (__attribute__((address_space(3))) void *)(to + TILE_B), 16,
+                                               off(row, o_rs, 8 * ch, valid), 0, 0, 0);
+    }
+    if (tid < QT) {
+      const bool ok = tid < valid;
+      const int64_t r = ((int64_t)b * a.heads + h) * a.tq + (ok ? qt * QT + tid : 0);
+      ls = ok && a.lse[r] != -INFINITY ? a.lse[r] * -LOG2E / p.qscale : -INFINITY;
+      de = ok ? -p.delta[r] : 0.f;
+    }
+    if (++qt == nqt) {       // the next triple
+      qt = 0;
+      if (++hs == shared) {
+        hs = 0;
+        ++bi;
+      }
+    }
+  };
+  const int steps = (int)(u1 - u0);
+  if (steps) load(0);
+  for (int u = 0; u < steps; ++u) {
+    const int buf = u & 1;
+    const char *rq = rows + buf * 2 * TILE_B, *rd = rq + TILE_B;
+    if (tid < QT) {
+      s_lse[buf * QT + tid] = ls;
+      s_delta[buf * QT + tid] = de;
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this tile's rows
+    __syncthreads();                      // ... of every wave; the last tile's copies have been read
+    if (u + 1 < steps) load(buf ^ 1);
+    {
+      const int br = fresh(block_rows<DH>(dg, qg)), bc = fresh(block_columns(dg, qg));
+#pragma unroll
+      for (int x = 0; x < COPIES; ++x) {       // head dim 128: a block of each tile a thread; 64: of one of them
+        const bool second = COPIES == 2 ? x : which;
+        u32x2 r[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = *reinterpret_cast<const u32x2 *>((second ? rd : rq) + block_row<DH>(br, e));
+        store_columns((second ? td : tq) + bc, r);
+      }
+    }
+    __syncthreads();
+    if (key0 >= len) continue;
+    const int rb = row_base<DH>(li, g);
+#pragma unroll 1
+    for (int x = 0; x < 2; ++x) {
+      const int rx = fresh(rb) + buf * 2 * TILE_B + 32 * x * RB;
+      // place 2 x + y of column tile d: (2 x + y) ^ d is (y ^ d) + 2 x, or less 2 x where y ^ d has that bit
+      const int up = fresh(cb) + 64 * x, down = up - 128 * x;
+      auto column = [&](const char *t, int d, int y) __attribute__((always_inline)) { return column_frag(t, (y ^ d) & 2 ? down : up, d, y); };
+      f32x16 s, dp;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 l4 = *reinterpret_cast<const f32x4 *>(s_lse + buf * QT + 32 * x + 8 * e + 4 * g);
+        const f32x4 d4 = *reinterpret_cast<const f32x4 *>(s_delta + buf * QT + 32 * x + 8 * e + 4 * g);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          s[4 * e + k] = l4[k];
+          dp[4 * e + k] = d4[k];
+        }
+      }
+      bf16x8 f[2][2], cf[2];       // operands, read a step ahead
+      f[0][0] = row_frag<DH>(rows, rx, 0, 0);
+      f[0][1] = row_frag<DH>(rows + TILE_B, rx, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < NC; ++k) {
+        if (k + 1 < NC) {
+          f[(k + 1) & 1][0] = row_frag<DH>(rows, rx, 0, k + 1);
+          f[(k + 1) & 1][1] = row_frag<DH>(rows + TILE_B, rx, 0, k + 1);
+        } else {
+          cf[0] = column(td, 0, 0);
+          cf[1] = column(tq, 0, 0);
+        }
+        s = mma32(f[k & 1][0], kf[k], s);
+        dp = mma32(f[k & 1][1], vf[k], dp);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[e] = __builtin_amdgcn_exp2f(s[e] * p.qscale);
+        dp[e] *= s[e];
+      }
+      const bf16x8 pf[2] = {chunk_frag(s, 0), chunk_frag(s, 1)}, sf[2] = {chunk_frag(dp, 0), chunk_frag(dp, 1)};
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int y = 0; y < 2 * ND; ++y) {
+        const bf16x8 c0 = cf[0], c1 = cf[1];
+        if (y + 1 < 2 * ND) {
+          cf[0] = column(td, (y + 1) % ND, (y + 1) / ND);
+          cf[1] = column(tq, (y + 1) % ND, (y + 1) / ND);
+        }
+        dv[y % ND] = mma32(c0, pf[y / ND], dv[y % ND]);
+        dk[y % ND] = mma32(c1, sf[y / ND], dk[y % ND]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  if (key >= a.tk || (p.splits > 1 && key >= len)) return;
+  const bool live = key < len;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = 32 * d + 8 * e + 4 * g;
+      f32x4 x, y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x[k] = live ? dk[d][4 * e + k] * p.scale : 0.f;
+        y[k] = live ? dv[d][4 * e + k] : 0.f;
+      }
+      if (p.splits > 1) {       // [split][prompt][tk][key head][2][dh]
+        float *dst = p.part + (((((int64_t)split * a.n_kv + c) * a.tk + key) * a.kv_heads + kh) * 2) * DH + at;
+        *reinterpret_cast<f32x4 *>(dst) = x;
+        *reinterpret_cast<f32x4 *>(dst + DH) = y;
+      } else {
+        const int64_t to = c * a.kv_bs + (int64_t)key * a.kv_rs + kh * DH + at;
+        *reinterpret_cast<bf16x4 *>((bf16 *)p.dk + to) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+        *reinterpret_cast<bf16x4 *>((bf16 *)p.dv + to) = bf16x4{(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+      }
+    }
+}
+
+template <int DH> constexpr size_t dq_lds() { return (size_t)2 * QT * DH * 2 + DH * TP; }
+template <int DH> constexpr size_t dkv_lds() { return (size_t)4 * QT * DH * 2 + 2 * DH * TP + 4 * QT * 4; }
+// Offsets of a tile's rows are 31 bits.
+bool takes(const CrossArgs &a) { return (a.head_dim == 64 || a.head_dim == 128) && a.q_rs < 1 << 23 && a.o_rs < 1 << 23 && a.kv_rs < 1 << 23; }
+
+}  // namespace x32
+
 // dk and dv out of the ranges' sums, in order, four elements a thread; rows past a prompt's end: 0
 template <typename T>
 __global__ __launch_bounds__(256) void k_cross_sum(CrossP p) {
@@ -579,13 +968,27 @@ template <typename T> int key_splits(const CrossArgs &a) {
   return (int)std::max<int64_t>(1, std::min(256 / wgs, tiles / 4));
 }
 
-// Into how many ranges the queries of k_cross_dkv are cut: four workgroups a CU, four tiles of queries each at least
-template <typename T> int query_splits(const CrossArgs &a, int keys) {
-  const int64_t wgs = (int64_t)a.n_kv * a.kv_heads * ((a.tk + keys - 1) / keys);
-  const int64_t tiles = (int64_t)a.batch * (a.heads / a.kv_heads) * ((a.tq + TILE<T> - 1) / TILE<T>) / a.n_kv;
-  return (int)std::max<int64_t>(1, std::min<int64_t>((1024 + wgs - 1) / wgs, tiles / 4));
-}
 template <typename T> constexpr int BLOCK_KEYS = sizeof(T) == 2 ? 128 : 64;
+
+// Into how many ranges the queries of k_cross_dkv and k_dkv are cut, for the least estimate of whole rounds of workgroups
+// (one a CU) at 2 us a tile of queries, and of the ranges' sums, written and read at 5 bytes a ps; four tiles each at least.
+// By the sizes alone, not by the kernel that takes the strides, since the workspace goes by it.
+template <typename T> int query_splits(const CrossArgs &a) {
+  const int keys = sizeof(T) == 2 && a.head_dim >= 64 ? x32::KEYS : BLOCK_KEYS<T>;
+  const int64_t wgs = (int64_t)a.n_kv * a.kv_heads * ((a.tk + keys - 1) / keys);
+  const double tiles = (double)a.batch * (a.heads / a.kv_heads) * ((a.tq + TILE<T> - 1) / TILE<T>) / a.n_kv;
+  const double bytes = 16.0 * a.n_kv * a.tk * a.kv_heads * a.head_dim;
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 64 && (s == 1 || tiles >= 4 * s); ++s) {
+    const double cost = (double)((wgs * s + 255) / 256) * tiles / s * 2.0 + (s > 1 ? s * bytes / 5e6 + 4 : 0);
+    if (s == 1 || cost < least) {
+      best = s;
+      least = cost;
+    }
+  }
+  return best;
+}
 
 template <typename T, int DH, int NQ>
 hipError_t forward(CrossP p, void *workspace, size_t bytes, hipStream_t s) {
@@ -620,23 +1023,45 @@ hipError_t gradient(CrossP p, const CrossGradArgs &b, hipStream_t s) {
   p.delta = (float *)b.workspace;
   const int64_t rows = (int64_t)a.batch * a.heads * a.tq;
   p.part = p.delta + (rows + 63) / 64 * 64;
-  hipLaunchKernelGGL((k_cross_delta<T>), dim3((unsigned)std::min<int64_t>((rows * (a.head_dim / 8) + 255) / 256, 1 << 16)), dim3(256), 0,
-                     s, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  hipError_t e = hipSuccess;
   constexpr size_t lds = tile_bytes<T, DH>();
+  const bool wide = sizeof(T) == 2 && x32::takes(a);
+  if (!wide || !b.dq) {
+    hipLaunchKernelGGL((k_cross_delta<T>), dim3((unsigned)std::min<int64_t>((rows + 127) / 128, 1 << 16)), dim3(256), 0, s, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   if (b.dq) {
-    constexpr int NQ = sizeof(T) == 2 ? 2 : 1;
-    p.nqb = (a.tq + 64 * NQ - 1) / (64 * NQ);
-    hipLaunchKernelGGL((k_cross_dq<T, DH, NQ>), dim3(unit_grid(p)), dim3(256), lds, s, p);
+    if constexpr (sizeof(T) == 2 && DH >= 64) {
+      if (wide) {
+        p.nqb = (a.tq + 127) / 128;
+        hipLaunchKernelGGL((x32::k_dq<DH>), dim3(unit_grid(p)), dim3(256), (x32::dq_lds<DH>()), s, p);
+      }
+    }
+    if (!wide) {
+      constexpr int NQ = sizeof(T) == 2 ? 2 : 1;
+      p.nqb = (a.tq + 64 * NQ - 1) / (64 * NQ);
+      hipLaunchKernelGGL((k_cross_dq<T, DH, NQ>), dim3(unit_grid(p)), dim3(256), lds, s, p);
+    }
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (b.dk) {
-    constexpr int NK = BLOCK_KEYS<T> / 64;
-    p.splits = query_splits<T>(a, BLOCK_KEYS<T>);
-    const size_t more = (2 * TILE<T> + a.batch + 1) * 4;
-    hipLaunchKernelGGL((k_cross_dkv<T, DH, NK>), dim3((a.tk + BLOCK_KEYS<T> - 1) / BLOCK_KEYS<T>, a.n_kv * a.kv_heads, p.splits),
-                       dim3(256), lds + more, s, p);
+    p.splits = query_splits<T>(a);
+    if constexpr (sizeof(T) == 2 && DH >= 64) {
+      if (wide) {
+        const int64_t sets = ((int64_t)a.n_kv * a.kv_heads * p.splits + 7) / 8 * 8 * ((a.tk + x32::KEYS - 1) / x32::KEYS);
+        const size_t bytes = x32::dkv_lds<DH>() + (a.batch + 1) * 4;
+        static const hipError_t set = hipFuncSetAttribute((const void *)x32::k_dkv<DH>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                          (int)(x32::dkv_lds<DH>() + 4097 * 4));
+        if (set != hipSuccess) return set;
+        hipLaunchKernelGGL((x32::k_dkv<DH>), dim3((unsigned)sets), dim3(512), bytes, s, p);
+      }
+    }
+    if (!wide) {
+      constexpr int NK = BLOCK_KEYS<T> / 64;
+      const size_t more = (2 * TILE<T> + a.batch + 1) * 4;
+      hipLaunchKernelGGL((k_cross_dkv<T, DH, NK>), dim3((a.tk + BLOCK_KEYS<T> - 1) / BLOCK_KEYS<T>, a.n_kv * a.kv_heads, p.splits),
+                         dim3(256), lds + more, s, p);
+    }
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (p.splits > 1) {
       const int64_t fours = (int64_t)a.n_kv * a.tk * a.kv_heads * a.head_dim / 2;
@@ -650,7 +1075,7 @@ hipError_t gradient(CrossP p, const CrossGradArgs &b, hipStream_t s) {
 template <typename T>
 size_t grad_bytes(const CrossArgs &a) {
   const int64_t rows = ((int64_t)a.batch * a.heads * a.tq + 63) / 64 * 64;
-  const int splits = query_splits<T>(a, BLOCK_KEYS<T>);
+  const int splits = query_splits<T>(a);
   return (size_t)(rows + (splits > 1 ? (int64_t)splits * a.n_kv * a.tk * a.kv_heads * 2 * a.head_dim : 0)) * 4;
 }
 
