@@ -571,6 +571,14 @@ __device__ __forceinline__ int column_at(int d, int qg) {
 }
 // Left operands.  Of a tile: row 32 x + li, chunk 2 k + g, at row_base ^ 32 k; of the copy: column 32 d + li, the rows of
 // chunk c and lane half g, whose place (2 c + g) ^ (2 d + li / 16) is 2 (c ^ d) + (g ^ li / 16).
+// A barrier for what is written to and read from LDS by instructions of its own: loads that write LDS stay in flight, which
+// __syncthreads would wait for.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 // v as a new value: what is computed from it inside a loop is not kept in registers across the loop
 __device__ __forceinline__ int fresh(int v) {
   asm volatile("" : "+v"(v));
@@ -794,9 +802,10 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
     const int h = kh * shared + hs, b = __builtin_amdgcn_readfirstlane(s_list[bi]), valid = min(QT, a.tq - qt * QT);
     const __amdgpu_buffer_rsrc_t rq = rows_rsrc((const bf16 *)a.q + b * a.q_bs + (int64_t)qt * QT * a.q_rs + h * DH, q_rs, valid, DH);
     const __amdgpu_buffer_rsrc_t rd = rows_rsrc((const bf16 *)p.dout + b * a.o_bs + (int64_t)qt * QT * a.o_rs + h * DH, o_rs, valid, DH);
+    const int at = fresh(lane);       // offsets are made anew for each tile: spilled ones would come back behind the loads
 #pragma unroll
     for (int x = 0; x < QT / ROWS / 8; ++x) {       // a load fills ROWS rows, 64 chunks; each wave takes its share of them
-      const int first = (w * (QT / ROWS / 8) + x) * ROWS, row = first + lane / NCH, ch = lane % NCH ^ swz<DH>(row);
+      const int first = (w * (QT / ROWS / 8) + x) * ROWS, row = first + at / NCH, ch = at % NCH ^ swz<DH>(row);
       char *to = rows + buf * 2 * TILE_B + first * RB;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (__attribute__((address_space(3))) void *)to, 16, off(row, q_rs, 8 * ch, valid), 0, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rd, (__attribute__((address_space(3))) void *)(to + TILE_B), 16,
@@ -805,8 +814,8 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
     if (tid < QT) {
       const bool ok = tid < valid;
       const int64_t r = ((int64_t)b * a.heads + h) * a.tq + (ok ? qt * QT + tid : 0);
-      ls = ok && a.lse[r] != -INFINITY ? a.lse[r] * -LOG2E / p.qscale : -INFINITY;
-      de = ok ? -p.delta[r] : 0.f;
+      ls = ok ? a.lse[r] : INFINITY;       // as they are: to use them here would wait for the tile
+      de = ok ? p.delta[r] : 0.f;
     }
     if (++qt == nqt) {       // the next triple
       qt = 0;
@@ -822,8 +831,8 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
     const int buf = u & 1;
     const char *rq = rows + buf * 2 * TILE_B, *rd = rq + TILE_B;
     if (tid < QT) {
-      s_lse[buf * QT + tid] = ls;
-      s_delta[buf * QT + tid] = de;
+      s_lse[buf * QT + tid] = ls == -INFINITY ? ls : -ls * LOG2E / p.qscale;
+      s_delta[buf * QT + tid] = -de;
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this tile's rows
     __syncthreads();                      // ... of every wave; the last tile's copies have been read
@@ -839,7 +848,7 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
         store_columns((second ? td : tq) + bc, r);
       }
     }
-    __syncthreads();
+    lds_barrier();
     if (key0 >= len) continue;
     const int rb = row_base<DH>(li, g);
 #pragma unroll 1
