@@ -275,28 +275,28 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossP p) {
   }
 }
 
-// delta of a row: lane half g of two takes eights 2 c + g of the row, in order, and the halves are added.
+// delta of a row: each of head_dim / 8 neighbouring lanes takes eight elements, then their sums are added.  The same in
+// k_cross_delta and in k_dq, so that dk and dv do not depend on whether dq is asked for.
 template <typename T>
-__device__ __forceinline__ float delta_part(float s, Frag<T> x, Frag<T> y) {
+__device__ __forceinline__ float row_delta(Frag<T> x, Frag<T> y, int lanes) {
+  float s = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) s = fmaf(to_f32(x[e]), to_f32(y[e]), s);
+  for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   return s;
 }
 
-// delta[b][h][i] = sum_d dout out, two lanes a row, 32 lanes apart
+// delta[b][h][i] = sum_d dout out
 template <typename T>
 __global__ __launch_bounds__(256) void k_cross_delta(CrossP p) {
   const CrossArgs &a = p.a;
-  const int li = threadIdx.x & 31, g = threadIdx.x >> 5 & 1;
-  const int64_t rows = (int64_t)a.batch * a.tq * a.heads, step = (int64_t)gridDim.x * 128;
-  for (int64_t r0 = (int64_t)blockIdx.x * 128 + (threadIdx.x >> 6) * 32; r0 < rows; r0 += step) {   // whole waves
-    const int64_t r = min(r0 + li, rows - 1);
+  const int lanes = a.head_dim / 8, at = threadIdx.x % lanes;
+  const int64_t rows = (int64_t)a.batch * a.tq * a.heads, step = (int64_t)gridDim.x * (256 / lanes);
+  for (int64_t r = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes; r < rows; r += step) {   // a row's lanes together
     const int h = (int)(r % a.heads), i = (int)(r / a.heads % a.tq), b = (int)(r / a.heads / a.tq);
-    const int64_t from = b * a.o_bs + (int64_t)i * a.o_rs + h * a.head_dim;
-    float s = 0.f;
-    for (int c = 8 * g; c < a.head_dim; c += 16) s = delta_part<T>(s, load_frag((const T *)a.out + from + c), load_frag((const T *)p.dout + from + c));
-    s += __shfl_xor(s, 32, 64);
-    if (g == 0 && r0 + li < rows) p.delta[((int64_t)b * a.heads + h) * a.tq + i] = s;
+    const int64_t from = b * a.o_bs + (int64_t)i * a.o_rs + h * a.head_dim + 8 * at;
+    const float s = row_delta<T>(load_frag((const T *)a.out + from), load_frag((const T *)p.dout + from), lanes);
+    if (at == 0) p.delta[((int64_t)b * a.heads + h) * a.tq + i] = s;
   }
 }
 
@@ -579,6 +579,11 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+// Between a wave's writes to LDS that only it uses and its reads of them: LDS works off a wave's instructions in order.
+__device__ __forceinline__ void own_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
 // v as a new value: what is computed from it inside a loop is not kept in registers across the loop
 __device__ __forceinline__ int fresh(int v) {
   asm volatile("" : "+v"(v));
@@ -618,6 +623,13 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const bf16 *at, int 
 __device__ __forceinline__ uint32_t off(int row, int stride, int col, int valid) {
   return row < valid ? (uint32_t)(row * stride + col) * 2u : 0x80000000u;
 }
+// 64 lanes' 16 bytes each to LDS, one behind the other from `to` on
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, char *to, uint32_t offset) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)to, 16, offset, 0, 0, 0);
+}
+__device__ __forceinline__ u32x2 load_pair(__amdgpu_buffer_rsrc_t r, uint32_t offset) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 0));
+}
 __device__ __forceinline__ f32x16 mma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 // registers 8 c .. 8 c + 7 as an operand
 __device__ __forceinline__ bf16x8 chunk_frag(const f32x16 &v, int c) {
@@ -630,100 +642,126 @@ __device__ __forceinline__ bf16x8 chunk_frag(const f32x16 &v, int c) {
 // dq of 128 queries, 32 a wave; also delta, for k_dkv.
 template <int DH>
 __global__ __launch_bounds__(256, 2) void k_dq(CrossP p) {
-  constexpr int NC = DH / 16, ND = DH / 32, DG = DH / 4, BLOCKS = 16 * DG / 256, VN = 64 * DH / 8 / 256;
+  constexpr int NC = DH / 16, ND = DH / 32, DG = DH / 4, BLOCKS = 16 * DG / 256, TILE_B = QT * DH * 2;
+  constexpr int CH = DH / 8, RPI = 64 / CH, N = 32 / RPI;      // chunks of a row; rows of a 64-lane load; loads of 32 rows
   extern __shared__ __attribute__((aligned(16))) char s_mem[];
-  char *sk = s_mem, *sv = sk + QT * DH * 2, *st = sv + QT * DH * 2;     // k, v, k transposed
+  char *sk = s_mem, *sv = sk + TILE_B, *st = sv + 2 * TILE_B;     // k; v of odd and even tiles; k transposed
   int b, h, qb;
   if (!unit_of(p, blockIdx.x, b, h, qb)) return;
   const CrossArgs &a = p.a;
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, g = lane >> 5, w = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, g = lane >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q0 = (qb * 4 + w) * 32, c = prompt_of(a, b), len = keys_of(a, c), kh = h / (a.heads / a.kv_heads);
   const bool idle = q0 >= a.tq;
   const int tiles = (len + QT - 1) / QT, i = q0 + li, at = min(i, a.tq - 1);
   const bf16 *K = (const bf16 *)a.k + c * a.kv_bs + kh * DH, *V = (const bf16 *)a.v + c * a.kv_bs + kh * DH;
-  bf16x8 qf[NC], df[NC];
-  const int64_t r = ((int64_t)b * a.heads + h) * a.tq + at;
-  float delta = 0.f;
-  {
-    const bf16 *Q = (const bf16 *)a.q + b * a.q_bs + (int64_t)at * a.q_rs + h * DH;
-    const int64_t from = b * a.o_bs + (int64_t)at * a.o_rs + h * DH;
+  u32x2 kr[BLOCKS][4];
+  const int rs = (int)a.kv_rs, cb = column_base(li, g);
+  const int dg = tid % DG, qg = tid / DG;
+  auto load = [&](int t) __attribute__((always_inline)) {
+    const int valid = min(QT, len - t * QT);
+    const __amdgpu_buffer_rsrc_t kt = rows_rsrc(K + (int64_t)t * QT * a.kv_rs, rs, valid, DH), vt = rows_rsrc(V + (int64_t)t * QT * a.kv_rs, rs, valid, DH);
+    const int kf = fresh(4 * qg), at = fresh(lane);      // offsets are made anew for each tile: they would be spilled
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      qf[k] = load_frag(Q + 16 * k + 8 * g);
-      df[k] = load_frag((const bf16 *)p.dout + from + 16 * k + 8 * g);
-      delta = delta_part<bf16>(delta, load_frag((const bf16 *)a.out + from + 16 * k + 8 * g), df[k]);
+    for (int x = 0; x < BLOCKS; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        kr[x][e] = load_pair(kt, off(kf + 1024 / DG * x + e, rs, 4 * dg, valid));
+#pragma unroll
+    for (int x = 0; x < QT / RPI / 4; ++x) {
+      const int first = (w * (QT / RPI / 4) + x) * RPI, row = first + at / CH;
+      load_to_lds(vt, sv + ((t & 1) ^ 1) * TILE_B + first * DH * 2, off(row, rs, 8 * (at % CH ^ swz<DH>(row)), valid));
     }
-    delta += __shfl_xor(delta, 32, 64);
+  };
+  auto land = [&]() __attribute__((always_inline)) {
+    const int br = fresh(block_rows<DH>(dg, qg));
+#pragma unroll
+    for (int x = 0; x < BLOCKS; ++x) {      // 1024 / DG rows further: the same chunk, and a place 1024 / DG / 16 pairs on
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x2 *>(sk + block_row<DH>(br, e) + x * (1024 / DG) * DH * 2) = kr[x][e];
+      store_columns(st + fresh(block_columns(dg, qg + 256 / DG * x)), kr[x]);
+    }
+  };
+  if (tiles) load(0);
+  // The wave's rows come and go as whole rows, through LDS: a lane's own pieces of one row would take each line of memory
+  // in several parts, and the loads and stores of a workgroup's queries half of its time.
+  char *mine = s_mem + w * 32 * DH * 2;
+  const int lrow = lane / CH, lch = lane % CH;
+  bf16x8 qf[NC], df[NC];
+  float lse = 0.f, delta = 0.f;
+  if (!idle) {
+    float *s_delta = reinterpret_cast<float *>(st) + 32 * w;
+    bf16x8 qv[N], dv[N], ov[N];
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const int row = min(q0 + RPI * x + lrow, a.tq - 1);
+      const int64_t from = b * a.o_bs + (int64_t)row * a.o_rs + h * DH + 8 * lch;
+      qv[x] = load_frag((const bf16 *)a.q + b * a.q_bs + (int64_t)row * a.q_rs + h * DH + 8 * lch);
+      dv[x] = load_frag((const bf16 *)p.dout + from);
+      ov[x] = load_frag((const bf16 *)a.out + from);
+    }
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const float s = row_delta<bf16>(ov[x], dv[x], CH);
+      if (lch == 0) s_delta[RPI * x + lrow] = s;
+      *reinterpret_cast<bf16x8 *>(mine + row_at<DH>(RPI * x + lrow, lch)) = qv[x];
+    }
+    const int rb = row_base<DH>(li, g);
+    own_lds();
+#pragma unroll
+    for (int k = 0; k < NC; ++k) qf[k] = row_frag<DH>(mine, rb, 0, k);
+    own_lds();
+#pragma unroll
+    for (int x = 0; x < N; ++x) *reinterpret_cast<bf16x8 *>(mine + row_at<DH>(RPI * x + lrow, lch)) = dv[x];
+    own_lds();
+#pragma unroll
+    for (int k = 0; k < NC; ++k) df[k] = row_frag<DH>(mine, rb, 0, k);
+    delta = s_delta[li];
+    const int64_t r = ((int64_t)b * a.heads + h) * a.tq + at;
+    lse = a.lse[r] == -INFINITY ? INFINITY : a.lse[r] * LOG2E / p.qscale;
     if (g == 0 && i < a.tq) p.delta[r] = delta;
   }
-  const float lse = a.lse[r] == -INFINITY ? INFINITY : a.lse[r] * LOG2E / p.qscale;
   f32x16 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-  u32x2 kr[BLOCKS][4];
-  u32x4 vr[VN];
-  const int rs = (int)a.kv_rs, cb = column_base(li, g);
-  const int dg = tid % DG, qg = tid / DG, ch = tid % (DH / 8), vrow = tid / (DH / 8);
-  auto load = [&](int t) __attribute__((always_inline)) {
-    const int valid = min(QT, len - t * QT);
-    const __amdgpu_buffer_rsrc_t kt = rows_rsrc(K + (int64_t)t * QT * a.kv_rs, rs, valid, DH), vt = rows_rsrc(V + (int64_t)t * QT * a.kv_rs, rs, valid, DH);
-    const int kf = fresh(4 * qg), vf = fresh(vrow);
-#pragma unroll
-    for (int x = 0; x < BLOCKS; ++x)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        kr[x][e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(kt, off(kf + 1024 / DG * x + e, rs, 4 * dg, valid), 0, 0));
-#pragma unroll
-    for (int x = 0; x < VN; ++x)
-      vr[x] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vt, off(vf + 2048 / DH * x, rs, 8 * ch, valid), 0, 0));
-  };
-  auto land = [&]() __attribute__((always_inline)) {
-    const int br = fresh(block_rows<DH>(dg, qg)), bc = fresh(block_columns(dg, qg)), vb = fresh(row_at<DH>(vrow, ch));
-#pragma unroll
-    for (int x = 0; x < BLOCKS; ++x) {      // 1024 / DG rows further: the same chunk, and a place 1024 / DG / 16 pairs on
-#pragma unroll
-      for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x2 *>(sk + block_row<DH>(br, e) + x * (1024 / DG) * DH * 2) = kr[x][e];
-      store_columns(st + (x ? block_columns(dg, qg + 256 / DG * x) : bc), kr[x]);
-    }
-#pragma unroll
-    for (int x = 0; x < VN; ++x) *reinterpret_cast<u32x4 *>(sv + vb + x * 2048 / DH * DH * 2) = vr[x];
-  };
-  if (tiles) load(0);
   for (int t = 0; t < tiles; ++t) {
-    __syncthreads();          // the last tile has been read
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this tile's v
+    __syncthreads();                      // ... of every wave; the last tile has been read
     land();
-    __syncthreads();
+    lds_barrier();
     if (t + 1 < tiles) load(t + 1);
+    const char *vt = sv + ((t & 1) ^ 1) * TILE_B;
     if (idle) continue;
-    const int rb = fresh(row_base<DH>(li, g));
-#pragma unroll
+#pragma unroll 1
     for (int x = 0; x < 2; ++x) {
+      const int rx = fresh(row_base<DH>(li, g)) + 32 * x * DH * 2;
+      // place 2 x + y of column tile d: (2 x + y) ^ d is (y ^ d) + 2 x, or less 2 x where y ^ d has that bit
+      const int up = fresh(cb) + 64 * x, down = up - 128 * x;
+      auto column = [&](int n) __attribute__((always_inline)) { return column_frag(st, (n / ND ^ n % ND) & 2 ? down : up, n % ND, n / ND); };
       f32x16 s, dp;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         s[e] = -lse;
         dp[e] = -delta;
       }
-      bf16x8 f[4][2], cf[2 * ND];       // operands, read two steps ahead
+      bf16x8 f[3][2], cf[3];            // operands, read two steps ahead
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        f[k][0] = row_frag<DH>(sk, rb, x, k);
-        f[k][1] = row_frag<DH>(sv, rb, x, k);
+        f[k][0] = row_frag<DH>(sk, rx, 0, k);
+        f[k][1] = row_frag<DH>(vt, rx, 0, k);
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int k = 0; k < NC; ++k) {
         if (k + 2 < NC) {
-          f[(k + 2) & 3][0] = row_frag<DH>(sk, rb, x, k + 2);
-          f[(k + 2) & 3][1] = row_frag<DH>(sv, rb, x, k + 2);
+          f[(k + 2) % 3][0] = row_frag<DH>(sk, rx, 0, k + 2);
+          f[(k + 2) % 3][1] = row_frag<DH>(vt, rx, 0, k + 2);
         } else {
-          cf[2 * (k + 2 - NC)] = column_frag(st, cb, 2 * (k + 2 - NC) % ND, 2 * x + 2 * (k + 2 - NC) / ND);
-          cf[2 * (k + 2 - NC) + 1] = column_frag(st, cb, (2 * (k + 2 - NC) + 1) % ND, 2 * x + (2 * (k + 2 - NC) + 1) / ND);
+          cf[k + 2 - NC] = column(k + 2 - NC);
         }
-        s = mma32(f[k & 3][0], qf[k], s);
-        dp = mma32(f[k & 3][1], df[k], dp);
+        s = mma32(f[k % 3][0], qf[k], s);
+        dp = mma32(f[k % 3][1], df[k], dp);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
@@ -737,20 +775,28 @@ __global__ __launch_bounds__(256, 2) void k_dq(CrossP p) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int y = 0; y < 2 * ND; ++y) {
-        if (y + 4 < 2 * ND) cf[y + 4] = column_frag(st, cb, (y + 4) % ND, 2 * x + (y + 4) / ND);
-        o[y % ND] = mma32(cf[y], df2[y / ND], o[y % ND]);
+        if (y + 2 < 2 * ND) cf[(y + 2) % 3] = column(y + 2);
+        o[y % ND] = mma32(cf[y % 3], df2[y / ND], o[y % ND]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
-  if (i >= a.tq) return;
-  bf16 *O = (bf16 *)p.dq + b * a.q_bs + (int64_t)i * a.q_rs + h * DH + 4 * g;
+  __syncthreads();            // the last tile has been read
+  if (idle) return;
 #pragma unroll
   for (int d = 0; d < ND; ++d)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      *reinterpret_cast<bf16x4 *>(O + 32 * d + 8 * e) = bf16x4{(bf16)(o[d][4 * e] * p.scale), (bf16)(o[d][4 * e + 1] * p.scale),
-                                                               (bf16)(o[d][4 * e + 2] * p.scale), (bf16)(o[d][4 * e + 3] * p.scale)};
+      *reinterpret_cast<bf16x4 *>(mine + row_at<DH>(li, 4 * d + e) + 8 * g) =
+          bf16x4{(bf16)(o[d][4 * e] * p.scale), (bf16)(o[d][4 * e + 1] * p.scale), (bf16)(o[d][4 * e + 2] * p.scale), (bf16)(o[d][4 * e + 3] * p.scale)};
+  own_lds();
+  bf16 *O = (bf16 *)p.dq + b * a.q_bs + h * DH + 8 * lch;
+#pragma unroll
+  for (int x = 0; x < N; ++x) {
+    const int row = q0 + RPI * x + lrow;
+    const bf16x8 v = *reinterpret_cast<const bf16x8 *>(mine + row_at<DH>(RPI * x + lrow, lch));
+    if (row < a.tq) store_frag(O + (int64_t)row * a.q_rs, v);
+  }
 }
 
 constexpr int KEYS = 256;            // keys of a workgroup of k_dkv, 32 a wave
@@ -807,9 +853,8 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
     for (int x = 0; x < QT / ROWS / 8; ++x) {       // a load fills ROWS rows, 64 chunks; each wave takes its share of them
       const int first = (w * (QT / ROWS / 8) + x) * ROWS, row = first + at / NCH, ch = at % NCH ^ swz<DH>(row);
       char *to = rows + buf * 2 * TILE_B + first * RB;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (__attribute__((address_space(3))) void *)to, 16, off(row, q_rs, 8 * ch, valid), 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rd, (__attribute__((address_space(3))) void *)(to + TILE_B), 16,
-                                               off(row, o_rs, 8 * ch, valid), 0, 0, 0);
+      load_to_lds(rq, to, off(row, q_rs, 8 * ch, valid));
+      load_to_lds(rd, to + TILE_B, off(row, o_rs, 8 * ch, valid));
     }
     if (tid < QT) {
       const bool ok = tid < valid;
@@ -930,7 +975,7 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
     }
 }
 
-template <int DH> constexpr size_t dq_lds() { return (size_t)2 * QT * DH * 2 + DH * TP; }
+template <int DH> constexpr size_t dq_lds() { return (size_t)3 * QT * DH * 2 + DH * TP; }
 template <int DH> constexpr size_t dkv_lds() { return (size_t)4 * QT * DH * 2 + 2 * DH * TP + 4 * QT * 4; }
 // Offsets of a tile's rows are 31 bits.
 bool takes(const CrossArgs &a) { return (a.head_dim == 64 || a.head_dim == 128) && a.q_rs < 1 << 23 && a.o_rs < 1 << 23 && a.kv_rs < 1 << 23; }
@@ -1036,13 +1081,16 @@ hipError_t gradient(CrossP p, const CrossGradArgs &b, hipStream_t s) {
   constexpr size_t lds = tile_bytes<T, DH>();
   const bool wide = sizeof(T) == 2 && x32::takes(a);
   if (!wide || !b.dq) {
-    hipLaunchKernelGGL((k_cross_delta<T>), dim3((unsigned)std::min<int64_t>((rows + 127) / 128, 1 << 16)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((k_cross_delta<T>), dim3((unsigned)std::min<int64_t>((rows * (a.head_dim / 8) + 255) / 256, 1 << 16)), dim3(256), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (b.dq) {
     if constexpr (sizeof(T) == 2 && DH >= 64) {
       if (wide) {
         p.nqb = (a.tq + 127) / 128;
+        static const hipError_t set = hipFuncSetAttribute((const void *)x32::k_dq<DH>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                          (int)x32::dq_lds<DH>());
+        if (set != hipSuccess) return set;
         hipLaunchKernelGGL((x32::k_dq<DH>), dim3(unit_grid(p)), dim3(256), (x32::dq_lds<DH>()), s, p);
       }
     }
