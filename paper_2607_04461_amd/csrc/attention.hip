@@ -36,6 +36,10 @@ struct AttnP {
   void *out; int64_t o_bs, o_rs;
   float qscale;  // log2(e) / sqrt(head_dim)
   float lazy_thr;  // k_attn_fa: how far a tile maximum may pass the running one before O is rescaled
+  // k_attn_fa<, true> (cross-attention to prompts of their own lengths)
+  int kv_heads = 0;
+  const int32_t *kv_len = nullptr;   // [n_kv] or null
+  float *lse = nullptr;              // [batch][heads][tq] or null
 };
 
 __device__ __forceinline__ int kv_batch(const AttnP &p, int b) {
@@ -139,7 +143,9 @@ constexpr int K_OFF = 0, V_OFF = 2 * TILE_B;
 // several partial pieces; staged, each store instruction writes 4 whole rows.  Measured (same box,
 // outputs bit-identical): cross-attention 110 -> 100 us, self-attention 308-320 -> 299-309 us, the
 // 1.3B-shaped pool's draft 238.9 -> 236.8 ms.
-template <bool LEAD>   // a wave in phase B goes ahead (see above)
+// OWN: a prompt's own length in place of tk, key heads shared by groups of query heads, an empty prompt's rows of zeros, and
+// the log-sum-exp (16 x 12 heads of 1560 queries to prompts of 512 to 77 keys: 77 us, where k_cross takes 173).
+template <bool LEAD, bool OWN = false>   // LEAD: a wave in phase B goes ahead (see above)
 __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
   using namespace fa2;
   constexpr int RW = KT / WAVES;     // K (V) tile rows each wave loads
@@ -153,10 +159,23 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
   const int q0 = qblk * QB + w * QW;
   const bool idle = q0 >= p.tq;   // loads its share of every tile and meets every barrier, nothing else
   const int kb = kv_batch(p, b);
+  int tk = p.tk, kh = h;
+  if constexpr (OWN) {
+    kh = h / (p.heads / p.kv_heads);
+    if (p.kv_len) tk = max(0, min(p.kv_len[kb], p.tk));
+    if (tk == 0) {
+      for (int i = tid; i < QB * DH / 8; i += 256) {
+        const int row = qblk * QB + i / (DH / 8);
+        if (row < p.tq) *reinterpret_cast<u32x4 *>((bf16 *)p.out + (int64_t)b * p.o_bs + (int64_t)row * p.o_rs + h * DH + i % (DH / 8) * 8) = u32x4{0, 0, 0, 0};
+      }
+      if (p.lse && tid < QB && qblk * QB + tid < p.tq) p.lse[((int64_t)b * p.heads + h) * p.tq + qblk * QB + tid] = -INFINITY;
+      return;
+    }
+  }
   const bf16 *Q = (const bf16 *)p.q + (int64_t)b * p.q_bs + h * DH;
-  const bf16 *Kb = (const bf16 *)p.k + (int64_t)kb * p.kv_bs + h * DH;
-  const bf16 *Vb = (const bf16 *)p.v + (int64_t)kb * p.kv_bs + h * DH;
-  const int nt = (p.tk + KT - 1) / KT;
+  const bf16 *Kb = (const bf16 *)p.k + (int64_t)kb * p.kv_bs + kh * DH;
+  const bf16 *Vb = (const bf16 *)p.v + (int64_t)kb * p.kv_bs + kh * DH;
+  const int nt = (tk + KT - 1) / KT;
   char *lds = reinterpret_cast<char *>(sm);
 
   const int qi = min(q0 + li, p.tq - 1);
@@ -166,7 +185,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
     qf[ks] = *reinterpret_cast<const bf16x8 *>(Q + (int64_t)qi * p.q_rs + 16 * ks + 8 * g);
 
   auto tile_rsrc = [&](const bf16 *base, int j) {
-    const int valid = min(KT, p.tk - j * KT);
+    const int valid = min(KT, tk - j * KT);
     const uint64_t a = (uint64_t)(base + (int64_t)j * KT * p.kv_rs);
     const uint32_t bytes = (uint32_t)((valid - 1) * p.kv_rs + DH) * 2u;
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
@@ -237,7 +256,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
   };
   // keys at or past tk get -inf (the ragged last tile j)
   auto mask_tail = [&](f32x16 (&sc)[2], int j) __attribute__((always_inline)) {
-    const int lim = p.tk - j * KT - 4 * g;
+    const int lim = tk - j * KT - 4 * g;
 #pragma unroll
     for (int sl = 0; sl < 2; ++sl)
 #pragma unroll
@@ -318,7 +337,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
       // chunks 0 and 1 and the row sum are formed in the slots above, not sunk past this branch to their
       // first use
       asm volatile("" : "+v"(pp[0]), "+v"(pp[1]), "+v"(lsum));
-      if ((j + 2) * KT > p.tk) mask_tail(sn, j + 1);
+      if ((j + 2) * KT > tk) mask_tail(sn, j + 1);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) epair(sc, i >> 2, 2 * (i & 3));
@@ -382,7 +401,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
     for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
       for (int sl = 0; sl < 2; ++sl) sa[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfrag(0, ks, sl), qf[ks], sa[sl], 0, 0, 0);
-    if (KT > p.tk) mask_tail(sa, 0);
+    if (KT > tk) mask_tail(sa, 0);
     advance(rowmax(sa));
   }
   using T_ = std::true_type;
@@ -400,6 +419,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
   }
   const float ltot = lsum + __shfl_xor(lsum, 32, 64);
   const float inv = 1.0f / ltot;
+  if constexpr (OWN)
+    if (p.lse && g == 0 && q0 + li < p.tq)
+      p.lse[((int64_t)b * p.heads + h) * p.tq + q0 + li] = (mrun * p.qscale + log2f(ltot)) * 0.6931471805599453f;
   __syncthreads();   // every wave has read its last K and V fragments: the rings are free
   // the wave's 32 x 128 output block goes through LDS (16-byte chunk c of row r at c ^ (r & 15)), so that
   // each global store writes 4 whole rows
@@ -827,6 +849,25 @@ hipError_t launch_attention(ActType t, const AttnArgs &a, hipStream_t s) {
     return hipGetLastError();
   }
   return t == ACT_BF16 ? launch_f32<bf16>(p, a.head_dim, s) : launch_f32<float>(p, a.head_dim, s);
+}
+
+bool attention_own_takes(const CrossArgs &a) { return a.head_dim == fa2::DH && a.kv_rs <= 1 << 23; }
+
+hipError_t launch_attention_own(const CrossArgs &a, hipStream_t s) {
+  AttnP p;
+  p.batch = a.batch; p.heads = a.heads; p.tq = a.tq; p.tk = a.tk;
+  p.q = a.q; p.q_bs = a.q_bs; p.q_rs = a.q_rs;
+  p.k = a.k; p.v = a.v; p.kv_bs = a.kv_bs; p.kv_rs = a.kv_rs;
+  p.kv_index = a.kv_index; p.n_kv = a.n_kv;
+  p.out = a.out; p.o_bs = a.o_bs; p.o_rs = a.o_rs;
+  p.kv_heads = a.kv_heads; p.kv_len = a.kv_len; p.lse = a.lse;
+  p.qscale = (float)(1.4426950408889634 / sqrt((double)a.head_dim));
+  p.lazy_thr = 8.0f / p.qscale;
+  p.nqb = (p.tq + fa2::QB - 1) / fa2::QB;
+  const int64_t units8 = ((int64_t)p.batch * p.heads + 7) / 8 * 8;
+  auto kern = p.tk > 8 * fa2::KT ? k_attn_fa<true, true> : k_attn_fa<false, true>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(units8 * p.nqb)), dim3(256), 0, s, p);
+  return hipGetLastError();
 }
 
 }  // namespace fb

@@ -1056,6 +1056,8 @@ hipError_t forward(CrossP p, void *workspace, size_t bytes, hipStream_t s) {
     if (e != hipSuccess) return e;
     const int64_t rows = (int64_t)p.a.batch * p.a.heads * p.a.tq;
     hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16)), dim3(256), 0, s, p);
+  } else if (NQ == 2 && attention_own_takes(p.a)) {
+    return launch_attention_own(p.a, s);
   } else {
     hipLaunchKernelGGL((k_cross<T, DH, NQ, false>), dim3(unit_grid(p)), dim3(256), (tile_bytes<T, DH>()), s, p);
   }

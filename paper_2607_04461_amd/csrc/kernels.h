@@ -226,6 +226,9 @@ struct CrossArgs {
   void *out; int64_t o_bs, o_rs;
   float *lse;
 };
+// The bf16 kernel of head dim 128 (attention.hip) on such prompts, for strides that it takes.
+bool attention_own_takes(const CrossArgs &a);
+hipError_t launch_attention_own(const CrossArgs &a, hipStream_t s);
 size_t cross_attention_workspace(ActType t, const CrossArgs &a);
 hipError_t launch_cross_attention(ActType t, const CrossArgs &a, void *workspace, size_t workspace_bytes, hipStream_t s);
 // dq (as q), dk and dv (as k and v, every row of every prompt written); dq, or dk and dv, may be null.  batch <= 4096.
