@@ -9,8 +9,8 @@
 //   * k_up: [rows][r] . [N][r]^T onto the base rows.  The weights feed the left operand with the rows of two tiles
 //     interleaved, so that a lane holds eight consecutive outputs of one row.
 //   * k_outer: the sum over rows of an outer product, both operands through LDS, the activations' columns by transposing
-//     reads.  Rows reach it through lists sorted by adapter (k_rows), in chunks; k_outer_sum adds the chunks' sums in order.
-//   * k_transpose: up and down the other way round for the gradient's two products, a few MB at most.
+//     reads.  Rows reach it through lists sorted by adapter, in chunks; k_outer_sum adds the chunks' sums in order.
+//   * k_prepare: those lists, and up and down the other way round for the gradient's two products.
 // u and du are fp32 and stay so: next to bf16 weights each is split into bf16 parts that are multiplied one by one, three
 // where the result is fp32 (24 bits) and two where it is bf16 (16 bits of it, against the 8 that are kept).
 #include <algorithm>
@@ -67,56 +67,55 @@ struct DownArgs {
   float *u;                     // [M][rank]
 };
 
-constexpr int DOWN_WAVES = 8;
+constexpr int WAVES = 8;        // each sums every eighth block of columns; their shares are added in order
 
+// The waves' shares of x down^T for a tile's rows, to s_part [WAVES][MT RT][256]; a barrier must follow.
 template <typename T, int MT, int RT>
-__global__ __launch_bounds__(64 * DOWN_WAVES) void k_down(DownArgs a) {
-  extern __shared__ float s_part[];     // [waves][MT RT][256]
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, g = lane >> 4;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Tile t = tile_at(blockIdx.x, 16 * MT, a.M, a.per);
-  if (t.rows <= 0) return;
-  const int ad = adapter_of(a.index, t.group, a.count);
-  if (ad < 0) {
-    for (int i = tid; i < t.rows * a.rank; i += 64 * DOWN_WAVES) a.u[t.row0 * a.rank + i] = 0.f;
-    return;
-  }
+__device__ __forceinline__ void down_shares(const DownArgs &a, const Tile &t, int ad, float *s_part) {
+  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   f32x4 acc[MT][RT];
   const T *xr[MT], *wr[RT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) xr[i] = (const T *)a.x + (t.row0 + min(16 * i + li, t.rows - 1)) * a.K;
 #pragma unroll
   for (int j = 0; j < RT; ++j) wr[j] = (const T *)a.w + ((int64_t)ad * a.rank + min(16 * j + li, a.rank - 1)) * a.K;
+  constexpr int SUB = 4 / sizeof(T), BLOCK = 32 * SUB;       // a wave takes whole lines of 128 bytes
+  Frag<T> xf[2][SUB][MT], wf[2][SUB][RT];
+  auto load = [&](int b, int block) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < SUB; ++c) {
+      const int k = BLOCK * block + 32 * c + 8 * g;
+      const bool in = k < a.K;      // K % 8 == 0
+#pragma unroll
+      for (int i = 0; i < MT; ++i) xf[b][c][i] = in ? load_frag(xr[i] + k) : zero_frag<T>();
+#pragma unroll
+      for (int j = 0; j < RT; ++j) wf[b][c][j] = in ? load_frag(wr[j] + k) : zero_frag<T>();
+    }
+  };
+  auto multiply = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < SUB; ++c)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) acc[i][j] = mma(xf[b][c][i], wf[b][c][j], acc[i][j]);
+  };
+  const int blocks = (a.K + BLOCK - 1) / BLOCK;
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Frag<T> xf[2][MT], wf[2][RT];
-  auto load = [&](int b, int step) __attribute__((always_inline)) {
-    const int k = 32 * step + 8 * g;
-    const bool in = k < a.K;      // K % 8 == 0
-#pragma unroll
-    for (int i = 0; i < MT; ++i) xf[b][i] = in ? load_frag(xr[i] + k) : zero_frag<T>();
-#pragma unroll
-    for (int j = 0; j < RT; ++j) wf[b][j] = in ? load_frag(wr[j] + k) : zero_frag<T>();
-  };
-  auto multiply = [&](int b) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < RT; ++j) acc[i][j] = mma(xf[b][i], wf[b][j], acc[i][j]);
-  };
-  const int steps = (a.K + 31) / 32;
   int s = w;
-  if (s < steps) load(0, s);
-  while (s < steps) {       // the next step's loads in flight under this one's products
-    if (s + DOWN_WAVES < steps) load(1, s + DOWN_WAVES);
+  if (s < blocks) load(0, s);
+  while (s < blocks) {       // the next block's loads in flight under this one's products
+    if (s + WAVES < blocks) load(1, s + WAVES);
     multiply(0);
-    s += DOWN_WAVES;
-    if (s >= steps) break;
-    if (s + DOWN_WAVES < steps) load(0, s + DOWN_WAVES);
+    s += WAVES;
+    if (s >= blocks) break;
+    if (s + WAVES < blocks) load(0, s + WAVES);
     multiply(1);
-    s += DOWN_WAVES;
+    s += WAVES;
   }
   // element (row 4 g + e, rank li) of tile (i, j)
 #pragma unroll
@@ -125,20 +124,41 @@ __global__ __launch_bounds__(64 * DOWN_WAVES) void k_down(DownArgs a) {
     for (int j = 0; j < RT; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s_part[(w * MT * RT + i * RT + j) * 256 + (4 * g + e) * 16 + li] = acc[i][j][e];
+}
+// Element p of [MT RT][256] out of the shares, in order: row and rank of it, and its sum
+template <int MT, int RT>
+__device__ __forceinline__ float down_sum(const float *s_part, int p, int &row, int &r) {
+  float v = 0.f;
+#pragma unroll
+  for (int k = 0; k < WAVES; ++k) v += s_part[k * MT * RT * 256 + p];
+  row = p / (RT * 256) * 16 + (p & 255) / 16;
+  r = p / 256 % RT * 16 + (p & 15);
+  return v;
+}
+
+template <typename T, int MT, int RT>
+__global__ __launch_bounds__(64 * WAVES) void k_down(DownArgs a) {
+  extern __shared__ __attribute__((aligned(16))) float s_part[];
+  const Tile t = tile_at(blockIdx.x, 16 * MT, a.M, a.per);
+  if (t.rows <= 0) return;
+  const int ad = adapter_of(a.index, t.group, a.count);
+  if (ad < 0) {
+    for (int i = threadIdx.x; i < t.rows * a.rank; i += 64 * WAVES) a.u[t.row0 * a.rank + i] = 0.f;
+    return;
+  }
+  down_shares<T, MT, RT>(a, t, ad, s_part);
   __syncthreads();
   const float scale = a.scales ? a.scales[ad] : 1.f;
-  for (int p = tid; p < MT * RT * 256; p += 64 * DOWN_WAVES) {
-    float v = 0.f;
-#pragma unroll
-    for (int k = 0; k < DOWN_WAVES; ++k) v += s_part[k * MT * RT * 256 + p];
-    const int row = p / (RT * 256) * 16 + (p & 255) / 16, r = p / 256 % RT * 16 + (p & 15);
-    if (row < t.rows && r < a.rank) a.u[(t.row0 + row) * a.rank + r] = v * scale;
+  for (int p = threadIdx.x; p < MT * RT * 256; p += 64 * WAVES) {
+    int row, r;
+    const float v = down_sum<MT, RT>(s_part, p, row, r) * scale;
+    if (row < t.rows && r < a.rank) a.u[(t.row0 + row) * a.rank + r] = v;
   }
 }
 
 struct UpArgs {
   int64_t M;
-  int per, N, rank, count, cols;      // cols: columns of a workgroup, a multiple of 128
+  int per, N, rank, count, cols, parts;      // cols: columns of a workgroup, whole turns; workgroups a row
   const float *u;                     // [M][rank]
   const void *w;                      // [count][N][rank]
   const int32_t *index;
@@ -147,80 +167,231 @@ struct UpArgs {
   void *out;
 };
 
+template <typename T, typename O> constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(O) == 4 ? 3 : 2;
+
+// out = base + f u up^T for a tile's rows and the columns [from, to), 256 bytes of a row a turn from wave `first` of `waves` on.
+// uf: the parts of u, row li of each sixteen.  The products cross s_out, which only this wave uses, so that base and out pass
+// as 256 bytes of four rows at a time: in the products' own layout, 64 bytes of sixteen, 24960 x 1536 took 50 us for 38.
+template <typename O> constexpr int TURN = 256 / sizeof(O);
+template <typename O> constexpr int OUT_PITCH = TURN<O> + 4;
+template <typename O> constexpr size_t OUT_BYTES = 16 * OUT_PITCH<O> * 4;      // of a wave
 template <typename T, typename O, int MT, int RK>
-__global__ __launch_bounds__(256) void k_up(UpArgs a) {
-  constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(O) == 4 ? 3 : 2;
+__device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, int ad, const Frag<T> (&uf)[MT][RK][PARTS<T, O>], float *s_out,
+                                           int from, int to, int first, int waves) {
+  constexpr int E = 16 / sizeof(O), Q = TURN<O> / 32;        // elements of a lane's piece; groups of 32 columns
+  typedef O Piece __attribute__((ext_vector_type(E)));
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Tile t = tile_at(blockIdx.x, 16 * MT, a.M, a.per);
-  if (t.rows <= 0) return;
-  const int ad = adapter_of(a.index, t.group, a.count);
-  if (ad < 0 && a.base == a.out) return;
-  const int from = blockIdx.y * a.cols, to = min(from + a.cols, a.N);
-  int64_t row[MT];
-  bool in[MT];
-  Frag<T> uf[MT][RK][PARTS];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    in[i] = 16 * i + li < t.rows;
-    row[i] = t.row0 + min(16 * i + li, t.rows - 1);
-#pragma unroll
-    for (int c = 0; c < RK; ++c) {
-      const int r = 32 * c + 8 * g;
-      split<T, PARTS>(r < a.rank ? load_frag(a.u + row[i] * a.rank + r) : zero_frag<float>(), uf[i][c]);
-    }
-  }
   const float scale = ad < 0 ? 0.f : a.scales ? a.scales[ad] : 1.f;
   const T *W = (const T *)a.w + (int64_t)max(ad, 0) * a.N * a.rank;
   // column of row li of tile h: four of each eight
   const int col = 8 * (li >> 2) + (li & 3);
-  for (int n0 = from + 32 * w; n0 < to; n0 += 128) {
-    const int n = n0 + 8 * g;                  // this lane's eight columns; N % 8 == 0
-    const bool ok = n < to;
-    Frag<T> wf[2][RK];
+  for (int n0 = from + TURN<O> * first; n0 < to; n0 += TURN<O> * waves) {
+    const int n = n0 + E * li;                               // this lane's columns of rows 4 x + g; N % 8 == 0
+    Piece b[MT][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int c = 0; c < RK; ++c) {
-        const int r = 32 * c + 8 * g;
-        wf[h][c] = r < a.rank && ad >= 0 ? load_frag(W + (int64_t)min(n0 + col + 4 * h, a.N - 1) * a.rank + r) : zero_frag<T>();
+      for (int x = 0; x < 4; ++x) {
+        const int row = 16 * i + 4 * x + g;
+        if (a.base && n < to && row < t.rows) b[i][x] = *reinterpret_cast<const Piece *>((const O *)a.base + (t.row0 + row) * a.N + n);
+        else b[i][x] = (Piece)((O)0.f);
       }
-    Frag<O> b[MT];
+    Frag<T> wf[Q][2][RK];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) b[i] = a.base && ok && in[i] ? load_frag((const O *)a.base + row[i] * a.N + n) : zero_frag<O>();
-    float f[8];
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = a.gate && ok ? scale * a.gate[n + e] : scale;
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < RK; ++c) {
+          const int r = 32 * c + 8 * g;
+          wf[q][h][c] = r < a.rank && ad >= 0 ? load_frag(W + (int64_t)min(n0 + 32 * q + col + 4 * h, a.N - 1) * a.rank + r) : zero_frag<T>();
+        }
+    float f[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) f[e] = a.gate && n < to ? scale * a.gate[n + e] : scale;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      if (ad >= 0) {
 #pragma unroll
-      for (int p = PARTS - 1; p >= 0; --p)     // the small parts first
+        for (int q = 0; q < Q; ++q) {
+          f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int c = 0; c < RK; ++c)
+          for (int p = PARTS<T, O> - 1; p >= 0; --p)     // the small parts first
 #pragma unroll
-          for (int h = 0; h < 2; ++h) acc[h] = mma(wf[h][c], uf[i][c][p], acc[h]);
-      Frag<O> o;
+            for (int c = 0; c < RK; ++c)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float v = to_f32(b[i][e]);
-        o[e] = from_f32<O>(ad < 0 ? v : fmaf(f[e], acc[e >> 2][e & 3], v));
+              for (int h = 0; h < 2; ++h) acc[h] = mma(wf[q][h][c], uf[i][c][p], acc[h]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4 *>(s_out + li * OUT_PITCH<O> + 32 * q + 8 * g + 4 * h) = acc[h];
+        }
+        own_lds();
       }
-      if (ok && in[i]) store_frag((O *)a.out + row[i] * a.N + n, o);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int row = 16 * i + 4 * x + g;
+        Piece o = b[i][x];
+        if (ad >= 0) {
+#pragma unroll
+          for (int y = 0; y < E / 4; ++y) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(s_out + (4 * x + g) * OUT_PITCH<O> + E * li + 4 * y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[4 * y + e] = from_f32<O>(fmaf(f[4 * y + e], v[e], to_f32(o[4 * y + e])));
+          }
+        }
+        if (n < to && row < t.rows) *reinterpret_cast<Piece *>((O *)a.out + (t.row0 + row) * a.N + n) = o;
+      }
+      own_lds();
     }
   }
 }
 
-// out[z][c][r] = in[z][r][c] for `count` matrices of each of two shapes
-struct TransposeArgs {
+template <typename T, typename O, int MT, int RK>
+__global__ __launch_bounds__(256) void k_up(UpArgs a) {
+  extern __shared__ __attribute__((aligned(16))) float s_part[];
+  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tile t = tile_at(blockIdx.x / a.parts, 16 * MT, a.M, a.per);      // a row's workgroups follow each other
+  if (t.rows <= 0) return;
+  const int ad = adapter_of(a.index, t.group, a.count);
+  if (ad < 0 && a.base == a.out) return;
+  Frag<T> uf[MT][RK][PARTS<T, O>];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int c = 0; c < RK; ++c) {
+      const int r = 32 * c + 8 * g;
+      split<T, PARTS<T, O>>(r < a.rank ? load_frag(a.u + (t.row0 + min(16 * i + li, t.rows - 1)) * a.rank + r) : zero_frag<float>(), uf[i][c]);
+    }
+  const int from = blockIdx.x % a.parts * a.cols;
+  up_columns<T, O, MT, RK>(a, t, ad, uf, s_part + w * (OUT_BYTES<O> / 4), from, min(from + a.cols, a.N), w, 4);
+}
+
+template <typename O, int MT, int RT> constexpr size_t both_lds() {
+  const size_t shares = WAVES * MT * RT * 1024, outs = WAVES * OUT_BYTES<O>;
+  return (shares > outs ? shares : outs) + 16 * MT * ((RT < 2 ? 32 : 16 * RT) + 4) * 4;
+}
+
+// Both in one launch: u's tile stays in LDS.  d.u, its scales and the sums' order as in k_down, so the bits are the same.
+template <typename T, typename O, int MT, int RT>
+__global__ __launch_bounds__(64 * WAVES) void k_both(DownArgs d, UpArgs a) {
+  constexpr int RK = RT < 2 ? 1 : RT / 2, PITCH = 32 * RK + 4;
+  extern __shared__ __attribute__((aligned(16))) float s_part[];
+  // u's tile [16 MT][PITCH], zero past the rank, behind the larger of the shares and the waves' products
+  float *su = s_part + (both_lds<O, MT, RT>() / 4 - 16 * MT * PITCH);
+  const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
+  const Tile t = tile_at(blockIdx.x, 16 * MT, a.M, a.per);
+  if (t.rows <= 0) return;
+  const int ad = adapter_of(a.index, t.group, a.count);
+  Frag<T> uf[MT][RK][PARTS<T, O>];
+  if (ad < 0) {
+    for (int i = threadIdx.x; i < t.rows * a.rank; i += 64 * WAVES) d.u[t.row0 * a.rank + i] = 0.f;
+    if (a.base == a.out) return;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int c = 0; c < RK; ++c)
+#pragma unroll
+        for (int p = 0; p < PARTS<T, O>; ++p) uf[i][c][p] = zero_frag<T>();
+  } else {
+    down_shares<T, MT, RT>(d, t, ad, s_part);
+    __syncthreads();
+    const float scale = d.scales ? d.scales[ad] : 1.f;
+    for (int p = threadIdx.x; p < MT * RT * 256; p += 64 * WAVES) {
+      int row, r;
+      const float v = down_sum<MT, RT>(s_part, p, row, r) * scale;
+      if (row < t.rows && r < a.rank) d.u[(t.row0 + row) * a.rank + r] = v;
+      su[row * PITCH + r] = r < a.rank ? v : 0.f;
+      if (RT == 1) su[row * PITCH + r + 16] = 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int c = 0; c < RK; ++c) split<T, PARTS<T, O>>(load_frag(su + (16 * i + li) * PITCH + 32 * c + 8 * g), uf[i][c]);
+  }
+  // u's tile has been read; the shares' place serves the products
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  up_columns<T, O, MT, RK>(a, t, ad, uf, s_part + w * (OUT_BYTES<O> / 4), 0, a.N, w, WAVES);
+}
+
+// What the gradient needs first, in one launch of [blocks][2 count + count]: the transposed weights, out[z][c][r] =
+// in[z][r][c] for `count` matrices of each of two shapes, and the lists of rows (k_prepare's last planes).
+struct PrepareArgs {
   const void *in[2];
   void *out[2];
   int rows[2], cols[2], count;
+  int64_t M;
+  int per, chunk, chunks;
+  const int32_t *index;
+  int32_t *list, *chunk_adapter, *first;     // null: no lists
 };
+
+// The rows of adapter `me`, in order, as a list that starts at a multiple of `chunk` and is filled up with -1:
+// `list`; chunk_adapter[c]: the adapter of a chunk, -1 past the last; first[a], first[count + a]: an adapter's chunks.
+// Workgroup `slice` of `slices` writes its share of the list.  The counts are integers, so the order of their additions
+// changes nothing.
+__device__ __forceinline__ void list_rows(const PrepareArgs &a, int me, int slice, int slices) {
+  __shared__ int s_rows[1024], s_group[256], s_wave[4], s_sum[2];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, M = (int)a.M, groups = (M + a.per - 1) / a.per;
+  for (int i = tid; i < 1024; i += 256) s_rows[i] = 0;
+  if (tid < 2) s_sum[tid] = 0;
+  __syncthreads();
+  for (int i = tid; i < groups; i += 256) {
+    const int ad = adapter_of(a.index, i, a.count);
+    if (ad >= 0) atomicAdd(&s_rows[ad], min(a.per, M - i * a.per));
+  }
+  __syncthreads();
+  for (int i = tid; i < a.count; i += 256) {
+    const int n = (s_rows[i] + a.chunk - 1) / a.chunk;
+    if (n && i < me) atomicAdd(&s_sum[0], n);
+    if (n) atomicAdd(&s_sum[1], n);
+  }
+  __syncthreads();
+  const int before = s_sum[0], total = s_sum[1], mine = s_rows[me], own = (mine + a.chunk - 1) / a.chunk;
+  if (slice == 0) {
+    if (tid == 0) {
+      a.first[me] = before;
+      a.first[a.count + me] = own;
+    }
+    for (int i = tid; i < own; i += 256) a.chunk_adapter[before + i] = me;
+    if (me == 0)
+      for (int i = total + tid; i < a.chunks; i += 256) a.chunk_adapter[i] = -1;
+  }
+  int32_t *at = a.list + (int64_t)before * a.chunk;
+  if (slice == 0)
+    for (int i = mine + tid; i < own * a.chunk; i += 256) at[i] = -1;
+  for (int g0 = 0; g0 < groups; g0 += 256) {
+    const bool match = g0 + tid < groups && adapter_of(a.index, g0 + tid, a.count) == me;
+    const uint64_t votes = __ballot(match);
+    if (lane == 0) s_wave[w] = __popcll(votes);
+    __syncthreads();
+    int slot = __popcll(votes & ((1ull << lane) - 1)), all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i < w) slot += s_wave[i];
+      all += s_wave[i];
+    }
+    if (match) s_group[slot] = g0 + tid;
+    __syncthreads();
+    // every group but the last of all is whole, so an adapter's rows are dense; fewer than M + per of them
+    const uint32_t items = (uint32_t)all * a.per;
+    for (uint32_t i = slice * 256 + tid; i < items; i += slices * 256) {
+      const uint32_t k = i / (uint32_t)a.per, row = (uint32_t)s_group[k] * a.per + (i - k * a.per);
+      if (row < (uint32_t)M) at[i] = (int32_t)row;
+    }
+    at += items;
+    __syncthreads();
+  }
+}
+
 template <typename T>
-__global__ __launch_bounds__(256) void k_transpose(TransposeArgs a) {
+__global__ __launch_bounds__(256) void k_prepare(PrepareArgs a) {
   __shared__ T s[32][33];
-  const int job = blockIdx.z >= a.count, z = blockIdx.z - job * a.count;
+  if ((int)blockIdx.y >= 2 * a.count) {
+    const int slices = min((int)gridDim.x, 16);
+    if (a.list && (int)blockIdx.x < slices) list_rows(a, blockIdx.y - 2 * a.count, blockIdx.x, slices);
+    return;
+  }
+  const int job = (int)blockIdx.y >= a.count, z = blockIdx.y - job * a.count;
   const int rows = a.rows[job], cols = a.cols[job], tc = (cols + 31) / 32;
   if ((int64_t)blockIdx.x >= (int64_t)tc * ((rows + 31) / 32)) return;
   const int r0 = blockIdx.x / tc * 32, c0 = blockIdx.x % tc * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
@@ -231,61 +402,6 @@ __global__ __launch_bounds__(256) void k_transpose(TransposeArgs a) {
   __syncthreads();
   for (int i = y; i < 32; i += 8)
     if (c0 + i < cols && r0 + x < rows) out[(int64_t)(c0 + i) * rows + r0 + x] = s[x][i];
-}
-
-// The rows of each adapter, in order, as a list that starts at a multiple of `chunk` and is filled up with -1:
-// `list`; chunk_adapter[c]: the adapter of a chunk, -1 past the last; first[a], first[count + a]: an adapter's chunks.
-// One workgroup an adapter; the counts are integers, so the order of their additions changes nothing.
-__global__ __launch_bounds__(1024) void k_rows(int64_t M, int per, int count, const int32_t *index, int chunk, int chunks,
-                                               int32_t *list, int32_t *chunk_adapter, int32_t *first) {
-  __shared__ int s_rows[1024], s_group[1024], s_wave[16], s_sum[2];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, me = blockIdx.x;
-  const int64_t groups = (M + per - 1) / per;
-  s_rows[tid] = 0;
-  if (tid < 2) s_sum[tid] = 0;
-  __syncthreads();
-  for (int64_t i = tid; i < groups; i += 1024) {
-    const int a = adapter_of(index, i, count);
-    if (a >= 0) atomicAdd(&s_rows[a], (int)min((int64_t)per, M - i * per));
-  }
-  __syncthreads();
-  if (tid < count) {
-    const int n = (s_rows[tid] + chunk - 1) / chunk;
-    if (n && tid < me) atomicAdd(&s_sum[0], n);
-    if (n) atomicAdd(&s_sum[1], n);
-  }
-  __syncthreads();
-  const int before = s_sum[0], total = s_sum[1], mine = s_rows[me], own = (mine + chunk - 1) / chunk;
-  if (tid == 0) {
-    first[me] = before;
-    first[count + me] = own;
-  }
-  for (int i = tid; i < own; i += 1024) chunk_adapter[before + i] = me;
-  if (me == 0)
-    for (int i = total + tid; i < chunks; i += 1024) chunk_adapter[i] = -1;
-  int32_t *at = list + (int64_t)before * chunk;
-  for (int64_t g0 = 0; g0 < groups; g0 += 1024) {
-    const bool match = g0 + tid < groups && adapter_of(index, g0 + tid, count) == me;
-    const uint64_t votes = __ballot(match);
-    if (lane == 0) s_wave[w] = __popcll(votes);
-    __syncthreads();
-    int slot = __popcll(votes & ((1ull << lane) - 1)), all = 0;
-    for (int i = 0; i < 16; ++i) {
-      if (i < w) slot += s_wave[i];
-      all += s_wave[i];
-    }
-    if (match) s_group[slot] = (int)(g0 + tid);
-    __syncthreads();
-    // every group but the last of all is whole, so an adapter's rows are dense
-    for (int64_t i = tid; i < (int64_t)all * per; i += 1024) {
-      const int64_t row = (int64_t)s_group[i / per] * per + i % per;
-      if (row < M) at[i] = (int32_t)row;
-    }
-    at += (int64_t)all * per;
-    __syncthreads();
-  }
-  at = list + (int64_t)before * chunk;
-  for (int i = mine + tid; i < own * chunk; i += 1024) at[i] = -1;
 }
 
 struct OuterArgs {
@@ -394,21 +510,38 @@ __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
   }
 }
 
+// An adapter's gradients out of its chunks' sums: 64 lanes of four elements, every fourth chunk to each of four waves, whose
+// sums are added in order.
 __global__ __launch_bounds__(256) void k_outer_sum(int count, int64_t down, int64_t up, const int32_t *first, const float *scales,
                                                    const float *partial, float *d_down, float *d_up) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= down + up) return;
+  __shared__ double s_part[3][64][4];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t e = ((int64_t)blockIdx.x * 64 + lane) * 4, all = down + up;      // multiples of eight
   for (int a = blockIdx.y; a < count; a += gridDim.y) {
-    const int c0 = first[a], n = first[count + a];
-    const float *p = partial + c0 * (down + up) + e;
-    double s = 0;
+    const int n = first[count + a];
+    const float *p = partial + first[a] * all + e;
+    double s[4] = {0, 0, 0, 0};
+    if (e < all) {
 #pragma unroll 4
-    for (int c = 0; c < n; ++c) s += (double)p[c * (down + up)];
-    if (e < down) {
-      if (d_down) d_down[a * down + e] = (float)s;
-    } else if (d_up) {
-      d_up[a * up + e - down] = (float)(s * (double)(scales ? scales[a] : 1.f));
+      for (int c = w; c < n; c += 4) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(p + c * all);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] += (double)v[k];
+      }
     }
+    if (w)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s_part[w - 1][lane][k] = s[k];
+    __syncthreads();
+    if (w == 0 && e < all) {
+      const double scale = e < down ? 1.0 : (double)(scales ? scales[a] : 1.f);
+      f32x4 v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = (float)((((s[k] + s_part[0][lane][k]) + s_part[1][lane][k]) + s_part[2][lane][k]) * scale);
+      float *dst = e < down ? d_down : d_up;
+      if (dst) *reinterpret_cast<f32x4 *>(dst + (e < down ? a * down + e : a * up + e - down)) = v;
+    }
+    __syncthreads();
   }
 }
 
@@ -422,8 +555,7 @@ int64_t tiles_of(int64_t M, int per, int rows) { return (M + per - 1) / per * ((
 
 template <typename T, int MT, int RT>
 hipError_t down_tile(const DownArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((k_down<T, MT, RT>), dim3((unsigned)tiles_of(a.M, a.per, 16 * MT)), dim3(64 * DOWN_WAVES),
-                     DOWN_WAVES * MT * RT * 1024, s, a);
+  hipLaunchKernelGGL((k_down<T, MT, RT>), dim3((unsigned)tiles_of(a.M, a.per, 16 * MT)), dim3(64 * WAVES), WAVES * MT * RT * 1024, s, a);
   return hipGetLastError();
 }
 // the waves' sums take MT RT 8 KB of LDS: 64 KB at most, two workgroups a CU
@@ -444,10 +576,12 @@ hipError_t launch_down(const DownArgs &a, hipStream_t s) {
 template <typename T, typename O, int MT, int RK>
 hipError_t up_tile(UpArgs a, hipStream_t s) {
   const int64_t tiles = tiles_of(a.M, a.per, 16 * MT);
-  // columns of a workgroup: enough workgroups for eight a CU, 128 columns at least
-  const int64_t parts = std::min<int64_t>((a.N + 127) / 128, std::max<int64_t>(1, 2048 / tiles));
-  a.cols = (int)((((a.N + 127) / 128 + parts - 1) / parts) * 128);
-  hipLaunchKernelGGL((k_up<T, O, MT, RK>), dim3((unsigned)tiles, (unsigned)((a.N + a.cols - 1) / a.cols)), dim3(256), 0, s, a);
+  // columns of a workgroup: enough workgroups for eight a CU, a turn of its four waves at least
+  constexpr int turn = 4 * TURN<O>;
+  const int64_t turns = (a.N + turn - 1) / turn, parts = std::min<int64_t>(turns, std::max<int64_t>(1, 2048 / tiles));
+  a.cols = (int)((turns + parts - 1) / parts * turn);
+  a.parts = (a.N + a.cols - 1) / a.cols;
+  hipLaunchKernelGGL((k_up<T, O, MT, RK>), dim3((unsigned)(tiles * a.parts)), dim3(256), 4 * OUT_BYTES<O>, s, a);
   return hipGetLastError();
 }
 template <typename T, typename O>
@@ -459,6 +593,34 @@ hipError_t launch_up(const UpArgs &a, hipStream_t s) {
   const int mt = tile_rows(a.M, a.per, 2);
   if (a.rank <= 64) return mt == 2 ? up_tile<T, O, 2, 2>(a, s) : up_tile<T, O, 1, 2>(a, s);
   return mt == 2 ? up_tile<T, O, 2, 4>(a, s) : up_tile<T, O, 1, 4>(a, s);
+}
+
+template <typename T, typename O, int MT, int RT>
+hipError_t both_tile(const DownArgs &d, const UpArgs &a, hipStream_t s) {
+  constexpr size_t lds = both_lds<O, MT, RT>();
+  if (lds > 65536) {
+    static const hipError_t set = hipFuncSetAttribute((const void *)k_both<T, O, MT, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (set != hipSuccess) return set;
+  }
+  hipLaunchKernelGGL((k_both<T, O, MT, RT>), dim3((unsigned)tiles_of(a.M, a.per, 16 * MT)), dim3(64 * WAVES), lds, s, d, a);
+  return hipGetLastError();
+}
+
+// u = d.scales x down^T, then out = base + a.gate a.scales u up^T.  In one launch where the rows fill the card or a workgroup
+// has few turns of 512 columns; else the columns of few rows go to several workgroups.
+template <typename T, typename O>
+hipError_t launch_both(const DownArgs &d, const UpArgs &a, hipStream_t s) {
+  const bool wide = sizeof(T) == 4 && a.rank > 32;       // fp32 operands of many ranks: no registers for two tiles of rows
+  const int mt = tile_rows(a.M, a.per, wide ? 1 : 2);
+  if ((tiles_of(a.M, a.per, 16 * mt) < 256 && a.N > 2048) || (sizeof(T) == 4 && a.rank > 64)) {
+    const hipError_t e = launch_down<T>(d, s);
+    return e != hipSuccess ? e : launch_up<T, O>(a, s);
+  }
+  if (a.rank <= 16) return mt == 2 ? both_tile<T, O, 2, 1>(d, a, s) : both_tile<T, O, 1, 1>(d, a, s);
+  if (a.rank <= 32) return mt == 2 ? both_tile<T, O, 2, 2>(d, a, s) : both_tile<T, O, 1, 2>(d, a, s);
+  if constexpr (sizeof(T) == 4) return both_tile<T, O, 1, 4>(d, a, s);
+  if (a.rank <= 64) return mt == 2 ? both_tile<T, O, 2, 4>(d, a, s) : both_tile<T, O, 1, 4>(d, a, s);
+  return both_tile<T, O, 1, 8>(d, a, s);
 }
 
 template <typename T, int RT>
@@ -506,12 +668,10 @@ hipError_t adapters(const AdapterArgs &a, bool out_f32, hipStream_t s) {
   DownArgs d;
   d.M = a.M; d.per = a.per; d.K = a.K; d.rank = a.rank; d.count = a.count;
   d.x = a.x; d.w = a.down; d.index = a.index; d.scales = nullptr; d.u = a.u;
-  const hipError_t e = launch_down<T>(d, s);
-  if (e != hipSuccess) return e;
   UpArgs p;
-  p.M = a.M; p.per = a.per; p.N = a.N; p.rank = a.rank; p.count = a.count; p.cols = 0;
+  p.M = a.M; p.per = a.per; p.N = a.N; p.rank = a.rank; p.count = a.count; p.cols = p.parts = 0;
   p.u = a.u; p.w = a.up; p.index = a.index; p.scales = a.scales; p.gate = a.gate; p.base = a.base; p.out = a.out;
-  return out_f32 ? launch_up<T, float>(p, s) : launch_up<T, T>(p, s);
+  return out_f32 ? launch_both<T, float>(d, p, s) : launch_both<T, T>(d, p, s);
 }
 
 template <typename T>
@@ -519,29 +679,28 @@ hipError_t adapters_grad(const AdapterArgs &a, const AdapterGradArgs &b, bool dx
   const GradSpace g(sizeof(T) == 2 ? ACT_BF16 : ACT_F32, a);
   char *ws = (char *)b.workspace;
   float *du = (float *)(ws + g.du);
-  TransposeArgs t;
+  int32_t *list = (int32_t *)(ws + g.list), *chunk_adapter = (int32_t *)(ws + g.chunk_adapter), *first = (int32_t *)(ws + g.first);
+  PrepareArgs t;
   t.in[0] = a.up; t.out[0] = ws + g.up_t; t.rows[0] = a.N; t.cols[0] = a.rank;
   t.in[1] = a.down; t.out[1] = ws + g.down_t; t.rows[1] = a.rank; t.cols[1] = a.K;
-  t.count = a.count;
+  t.count = a.count; t.M = a.M; t.per = a.per; t.chunk = g.chunk; t.chunks = (int)g.chunks; t.index = a.index;
+  t.list = b.d_down || b.d_up ? list : nullptr; t.chunk_adapter = chunk_adapter; t.first = first;
   const int across = std::max(a.N, a.K);
-  hipLaunchKernelGGL((k_transpose<T>), dim3((across + 31) / 32 * ((a.rank + 31) / 32), 1, 2 * a.count), dim3(256), 0, s, t);
+  hipLaunchKernelGGL((k_prepare<T>), dim3((across + 31) / 32 * ((a.rank + 31) / 32), 3 * a.count), dim3(256), 0, s, t);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   DownArgs d;
   d.M = a.M; d.per = a.per; d.K = a.N; d.rank = a.rank; d.count = a.count;
   d.x = b.dy; d.w = ws + g.up_t; d.index = a.index; d.scales = a.scales; d.u = du;
-  if ((e = launch_down<T>(d, s)) != hipSuccess) return e;
-  if (b.dx) {
+  if (!b.dx) {
+    if ((e = launch_down<T>(d, s)) != hipSuccess) return e;
+  } else {
     UpArgs p;
-    p.M = a.M; p.per = a.per; p.N = a.K; p.rank = a.rank; p.count = a.count; p.cols = 0;
+    p.M = a.M; p.per = a.per; p.N = a.K; p.rank = a.rank; p.count = a.count; p.cols = p.parts = 0;
     p.u = du; p.w = ws + g.down_t; p.index = a.index; p.scales = nullptr; p.gate = nullptr; p.base = b.base; p.out = b.dx;
-    if ((e = dx_f32 ? launch_up<T, float>(p, s) : launch_up<T, T>(p, s)) != hipSuccess) return e;
+    if ((e = dx_f32 ? launch_both<T, float>(d, p, s) : launch_both<T, T>(d, p, s)) != hipSuccess) return e;
   }
   if (!b.d_down && !b.d_up) return hipSuccess;
-  int32_t *list = (int32_t *)(ws + g.list), *chunk_adapter = (int32_t *)(ws + g.chunk_adapter), *first = (int32_t *)(ws + g.first);
-  hipLaunchKernelGGL(k_rows, dim3(a.count), dim3(1024), 0, s, a.M, a.per, a.count, a.index, g.chunk, (int)g.chunks, list,
-                     chunk_adapter, first);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
   OuterArgs o;
   o.rank = a.rank; o.chunk = g.chunk;
   o.cols[0] = a.K; o.cols[1] = a.N; o.x[0] = a.x; o.x[1] = b.dy; o.u[0] = du; o.u[1] = a.u;
@@ -551,7 +710,7 @@ hipError_t adapters_grad(const AdapterArgs &a, const AdapterGradArgs &b, bool dx
       : a.rank <= 64 ? outer_rank<T, 4>(o, grid, s) : outer_rank<T, 8>(o, grid, s);
   if (e != hipSuccess) return e;
   const int64_t down = (int64_t)a.rank * a.K, up = (int64_t)a.rank * a.N;
-  hipLaunchKernelGGL(k_outer_sum, dim3((unsigned)((down + up + 255) / 256), a.count), dim3(256), 0, s, a.count, down, up, first,
+  hipLaunchKernelGGL(k_outer_sum, dim3((unsigned)((down + up + 255) / 256), std::min(a.count, 65535)), dim3(256), 0, s, a.count, down, up, first,
                      a.scales, o.partial, b.d_down, b.d_up);
   return hipGetLastError();
 }

@@ -579,11 +579,6 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
-// Between a wave's writes to LDS that only it uses and its reads of them: LDS works off a wave's instructions in order.
-__device__ __forceinline__ void own_lds() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_wave_barrier();
-}
 // v as a new value: what is computed from it inside a loop is not kept in registers across the loop
 __device__ __forceinline__ int fresh(int v) {
   asm volatile("" : "+v"(v));

@@ -41,6 +41,12 @@ __device__ __forceinline__ void store_frag(float *p, f32x8 v) {
   reinterpret_cast<f32x4 *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
 }
 
+// Between a wave's writes to LDS that only it uses and its reads of them: LDS works off a wave's instructions in order.
+__device__ __forceinline__ void own_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Eight k of one column out of row-major LDS: column lane & 15 of the 16 at `col`, rows k0 + 0..3 and k1 + 0..3 of `pitch`
 // elements.  bf16: gfx950's transposing LDS read; in each group of 16 lanes, lane j addresses four consecutive columns of
 // row j >> 2, and lane l receives column l of the four rows.  8-byte alignment: pitch and col are multiples of four.
