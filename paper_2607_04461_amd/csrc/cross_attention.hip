@@ -107,6 +107,9 @@ template <typename T> constexpr int TILE = sizeof(T) == 2 ? 64 : 32;    // rows 
 template <typename T, int DH, int NQ, bool SPLIT>
 __global__ __launch_bounds__(256) void k_cross(CrossP p) {
   constexpr int KT = TILE<T>, NS = KT / 16, NC = DH / 32, ND = DH / 16;
+  // 16 queries a wave are bound by the reading of k and v: P may as well go in two bf16 parts (16 bits),
+  // which leaves the output its own rounding only
+  constexpr int PARTS = sizeof(T) == 2 && NQ == 1 ? 2 : 1;
   typedef Stage<T, KT, DH, 256> St;
   extern __shared__ __attribute__((aligned(16))) char s_mem[];
   T *sk = reinterpret_cast<T *>(s_mem), *sv = sk + KT * St::PITCH;
@@ -196,14 +199,28 @@ __global__ __launch_bounds__(256) void k_cross(CrossP p) {
     }
 #pragma unroll
     for (int j = 0; j < NS; j += 2) {
-      Frag<T> pf[NQ];
+      Frag<T> pf[NQ], rest[NQ];
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) pf[n] = pair_frag<T>(s[n][j], s[n][j + 1]);
+      for (int n = 0; n < NQ; ++n) {
+        pf[n] = pair_frag<T>(s[n][j], s[n][j + 1]);
+        if constexpr (PARTS == 2) {
+          f32x4 lo = s[n][j], hi = s[n][j + 1];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            lo[e] -= to_f32(pf[n][e]);
+            hi[e] -= to_f32(pf[n][4 + e]);
+          }
+          rest[n] = pair_frag<T>(lo, hi);
+        }
+      }
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
         const Frag<T> vf = load_column_frag(sv, St::PITCH, 16 * d, 16 * j + 4 * g, 16 * j + 16 + 4 * g);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) o[n][d] = mma(vf, pf[n], o[n][d]);
+        for (int n = 0; n < NQ; ++n) {
+          o[n][d] = mma(vf, pf[n], o[n][d]);
+          if constexpr (PARTS == 2) o[n][d] = mma(vf, rest[n], o[n][d]);
+        }
       }
     }
   }
@@ -252,19 +269,29 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossP p) {
     const int i = (int)(r % a.tq), h = (int)(r / a.tq % a.heads), b = (int)(r / a.tq / a.heads);
     const int pitch = a.head_dim + 4;
     const float *src = p.part + r * p.splits * pitch;
-    float top = -INFINITY;
-    for (int s = 0; s < p.splits; ++s)
-      if (src[s * pitch + a.head_dim + 1] != 0.f) top = fmaxf(top, src[s * pitch + a.head_dim]);
-    const float off = top == -INFINITY ? 0.f : top;
-    float l = 0.f, o[2] = {0.f, 0.f};
-    for (int s = 0; s < p.splits; ++s) {
-      const float ls = src[s * pitch + a.head_dim + 1];
-      if (ls == 0.f) continue;
-      const float f = __builtin_amdgcn_exp2f(src[s * pitch + a.head_dim] - off);
-      l = fmaf(f, ls, l);
+    // lane s: the maximum and sum of range s (at most 64), then its factor and the row's sum
+    const float ls = lane < p.splits ? src[lane * pitch + a.head_dim + 1] : 0.f;
+    const float ms = lane < p.splits ? src[lane * pitch + a.head_dim] : -INFINITY;
+    float v[16][2];        // the first ranges' sums, on their way meanwhile
+    auto load = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (lane + 64 * e < a.head_dim) o[e] = fmaf(f, src[s * pitch + lane + 64 * e], o[e]);
+      for (int s = 0; s < 16; ++s)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) v[s][e] = s0 + s < p.splits && lane + 64 * e < a.head_dim ? src[(s0 + s) * pitch + lane + 64 * e] : 0.f;
+    };
+    load(0);
+    const float top = wave_max(ls != 0.f ? ms : -INFINITY);
+    const float mine = ls != 0.f ? __builtin_amdgcn_exp2f(ms - (top == -INFINITY ? 0.f : top)) : 0.f;
+    const float l = wave_sum(mine * ls);
+    float o[2] = {0.f, 0.f};
+    for (int s0 = 0; s0 < p.splits; s0 += 16) {
+      if (s0) load(s0);
+#pragma unroll
+      for (int s = 0; s < 16; ++s) {
+        const float f = __shfl(mine, s0 + s, 64);      // splits <= 64; 0 past them and for an empty range
+#pragma unroll
+        for (int e = 0; e < 2; ++e) o[e] = fmaf(f, f != 0.f ? v[s][e] : 0.f, o[e]);
+      }
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     T *O = (T *)a.out + b * a.o_bs + (int64_t)i * a.o_rs + h * a.head_dim;
@@ -1009,12 +1036,13 @@ unsigned unit_grid(const CrossP &p) { return (unsigned)(((int64_t)p.a.batch * p.
 // queries of a wave: 32 where a candidate has more than a workgroup of 16s
 template <typename T> int wave_queries(const CrossArgs &a) { return sizeof(T) == 2 && a.tq > 64 ? 32 : 16; }
 
-// Into how many ranges the keys are cut: a workgroup a CU out of one candidate's (so that its bits do not depend on the
-// pool), four tiles of keys each at least.
+// Into how many ranges the keys are cut: two workgroups a CU out of one candidate's (so that its bits do not depend on the
+// pool), four tiles of keys each at least, and none for more than 64 queries, which fill the card by themselves.
 template <typename T> int key_splits(const CrossArgs &a) {
   const int64_t wgs = (int64_t)a.heads * ((a.tq + 4 * wave_queries<T>(a) - 1) / (4 * wave_queries<T>(a)));
   const int64_t tiles = (a.tk + TILE<T> - 1) / TILE<T>;
-  return (int)std::max<int64_t>(1, std::min(256 / wgs, tiles / 4));
+  if (a.tq > 64) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(64, std::min(512 / wgs, tiles / 4)));
 }
 
 template <typename T> constexpr int BLOCK_KEYS = sizeof(T) == 2 ? 128 : 64;

@@ -289,10 +289,10 @@ hipError_t grad_by_width(const LayerNormGradArgs &a, int64_t blocks, bool vec, h
 #undef FB_CALL
 }
 
-// Rows of a chunk: four workgroups a CU (by the 256 of the card, not those seen: the order of the sums goes by it),
-// and not fewer than 16 rows, below which the partial sums' bytes pass a tenth of the rows'.
+// Rows of a chunk: four workgroups a CU (by the 256 of the card, not those seen: the order of the sums goes by it), and not
+// fewer than a row a wave (1037 x 701 in chunks of 16 rows 17 us, of 4 rows REPLACE).
 int chunk_rows(int64_t M, int per) {
-  return (int)std::min<int64_t>(per, std::max<int64_t>(16, (M + 1023) / 1024));
+  return (int)std::min<int64_t>(per, std::max<int64_t>(4, (M + 1023) / 1024));
 }
 
 }  // namespace

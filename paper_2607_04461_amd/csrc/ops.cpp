@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <cstdlib>
 #include <initializer_list>
 #include <string>
 
@@ -429,11 +430,10 @@ flashbon_status flashbon_op_cross_attention_grad(int32_t dtype, int32_t batch, i
   // dk and dv may alternate row by row; each of them is held against everything else
   bool clash = overlaps({dq_out, dk_out, ws}, {q_in, k_in, v_in, index, len, o_in, lse_in, do_in}) ||
                overlaps({dq_out, dv_out, ws}, {q_in, k_in, v_in, index, len, o_in, lse_in, do_in});
-  if (dk && overlap(dk_out, dv_out)) {
-    const int64_t bytes = kv_row_stride * es, row = narrow * es;
-    const int64_t off = bytes ? (int64_t)(((intptr_t)dv - (intptr_t)dk) % bytes + bytes) % bytes : 0;
-    const bool regular = tk > 1 && bytes >= 2 * row && (n_kv == 1 || kv_batch_stride % kv_row_stride == 0);
-    clash = clash || !regular || off < row || off > bytes - row;
+  if (dk && overlap(dk_out, dv_out)) {      // a row of both within a row's stride, and the last one within a prompt's
+    const int64_t row = narrow * es, away = std::abs((int64_t)((intptr_t)dv - (intptr_t)dk)), both = away + row;
+    clash = clash || away < row || (tk > 1 && both > kv_row_stride * es) ||
+            (n_kv > 1 && (tk - 1) * kv_row_stride * es + both > kv_batch_stride * es);
   }
   if (clash) return fail(FLASHBON_EINVAL, "outputs and workspace must not overlap an input or each other");
   CrossArgs a{};

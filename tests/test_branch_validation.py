@@ -49,7 +49,9 @@ REFUSED = [
     ("cross_attention_grad", CROSS_GRAD, fb.EINVAL, [{"lse": None}, {"dout": None}, {"dk": None}, {"dv": None},
                                                      {"dq": None, "dk": None, "dv": None}, {"dq": at(9) + 8}, {"q_rs": 56},
                                                      {"q_bs": 0}, {"kv_rs": 24}, {"kv_bs": 0}, {"dq": at(0)}, {"dk": at(1)},
-                                                     {"dv": at(10)}, {"dv": at(10) + 32}, {"dq": at(8)}, {"dk": at(7)},
+                                                     {"dv": at(10)}, {"dv": at(10) + 32}, {"dv": at(10) + 64},
+                                                     {"dv": at(10) - 64}, {"dv": at(10) + 64, "kv_rs": 56},
+                                                     {"dv": at(10) + 64, "kv_rs": 64, "kv_bs": 312}, {"dq": at(8)}, {"dk": at(7)},
                                                      {"workspace": at(5)}, {"workspace": at(7) + 4}, {"dv": at(9)}]),
     ("cross_attention_grad", CROSS_GRAD, fb.ESHAPE, [{"batch": 4097}, {"workspace": None}, {"workspace_bytes": 16},
                                                      {"head_dim": 12}, {"kv_index": None, "n_kv": 1}]),

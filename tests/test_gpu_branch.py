@@ -302,6 +302,35 @@ def test_cross_attention_grad(dtype, shape):
     assert torch.equal(alone, dq) and torch.equal(alone_kv, dkv)
 
 
+@pytest.mark.parametrize("tk,pad,swap", [(1, 0, False), (1, 8, True), (5, 8, False), (5, 24, True), (1, 0, True)])
+def test_cross_attention_grad_into_fused_rows(tk, pad, swap):
+    """dk and dv in one buffer of alternating rows, one key a prompt among them, and prompts further apart than their rows:
+    the same as in two buffers, and what lies between is left as it was."""
+    heads, dh, tq, prompts = 2, 16, 9, 3
+    d, g = heads * dh, gen(18)
+    bs = tk * 2 * d + pad
+    store = normal(g, prompts * bs, dtype=torch.bfloat16).cuda()
+    first, second = store[: prompts * bs - d], store[d:]
+    k, v = (second, first) if swap else (first, second)
+    q, dout = normal(g, prompts, tq, d, dtype=torch.bfloat16).cuda(), normal(g, prompts, tq, d, dtype=torch.bfloat16).cuda()
+    out, lse = torch.empty_like(q), torch.empty(prompts, heads, tq, device="cuda")
+    sizes, qs = (fb.BF16, prompts, heads, heads, dh, tq, tk), (tq * d, d)
+    fb.flashbon_op_cross_attention(*sizes, q, *qs, k, v, bs, 2 * d, None, prompts, None, out, *qs, lse=lse)
+    ws = torch.empty(fb.flashbon_op_cross_attention_grad_workspace(*sizes, prompts), dtype=torch.uint8, device="cuda")
+    args = (*sizes, q, *qs, k, v, bs, 2 * d, None, prompts, None, out, *qs, lse, dout)
+    fused = torch.full_like(store, 9.0)
+    one, two = fused[: prompts * bs - d], fused[d:]
+    dk, dv = (two, one) if swap else (one, two)
+    fb.flashbon_op_cross_attention_grad(*args, None, dk, dv, workspace=ws)
+    apart = [torch.full_like(store, 9.0) for _ in range(2)]
+    fb.flashbon_op_cross_attention_grad(*args, None, *apart, workspace=ws)
+    rows = lambda t: torch.stack([t[c * bs:c * bs + tk * 2 * d].view(tk, 2, d) for c in range(prompts)])  # noqa: E731
+    got, half = rows(fused), 1 if swap else 0
+    assert torch.equal(got[:, :, half], rows(apart[0])[:, :, 0]) and torch.equal(got[:, :, 1 - half], rows(apart[1])[:, :, 0])
+    if pad:
+        assert all(bool((fused[c * bs + tk * 2 * d:(c + 1) * bs] == 9.0).all()) for c in range(prompts))
+
+
 def test_cross_attention_without_tables():
     """No index: batch row b has prompt b; no lengths: all keys; no lse, no workspace."""
     q, kv, _, _ = cross_inputs("bf16", 3, 2, 2, 128, 40, 30, 3, [30, 30, 30], 13)
