@@ -225,7 +225,8 @@ size_t flashbon_op_cross_attention_workspace(int32_t dtype, int32_t batch, int32
  *   P = exp(S - lse), S = q k^T / sqrt(head_dim);   dS = P (dout v^T - sum_d dout out) / sqrt(head_dim);
  *   dq = dS k;   dk = dS^T q, dv = P^T dout, summed over the batch rows and the query heads that read the key head.
  * dq (act) has q's strides, dk and dv those of k and v; q's and k's strides must keep their rows apart.  Every row of dk and
- * dv up to tk is written, zeros at or past kv_len[c] and for prompts that no row reads.  dq may be NULL, and so may dk
+ * dv up to tk is written, zeros at or past kv_len[c] and for prompts that no row reads.  The one key of a prompt of length 1
+ * has P = 1: dq and dk are 0 there.  dq may be NULL, and so may dk
  * and dv together.  The outputs must not overlap the extent of an input or each other, but rows of dk and dv may alternate
  * as those of fused keys and values do (FLASHBON_EINVAL).  batch <= 4096; sizes and alignment otherwise as above; a
  * workspace of flashbon_op_cross_attention_grad_workspace bytes (FLASHBON_ESHAPE if it is smaller). */

@@ -599,8 +599,8 @@ template <typename T, typename O, int MT, int RT>
 hipError_t both_tile(const DownArgs &d, const UpArgs &a, hipStream_t s) {
   constexpr size_t lds = both_lds<O, MT, RT>();
   if (lds > 65536) {
-    static const hipError_t set = hipFuncSetAttribute((const void *)k_both<T, O, MT, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (set != hipSuccess) return set;
+    const hipError_t e = hipFuncSetAttribute((const void *)k_both<T, O, MT, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL((k_both<T, O, MT, RT>), dim3((unsigned)tiles_of(a.M, a.per, 16 * MT)), dim3(64 * WAVES), lds, s, d, a);
   return hipGetLastError();

@@ -83,6 +83,18 @@ __device__ __forceinline__ Frag<T> pair_frag(f32x4 lo, f32x4 hi) {
   return f;
 }
 
+// What rounding two tiles to f left.  A second product with it gives a sum the digits of fp32 operands: P and dS rounded to
+// bf16 are off by 2^-8 each, which counts as much in a result as its own rounding.
+template <typename T>
+__device__ __forceinline__ Frag<T> rest_frag(f32x4 lo, f32x4 hi, Frag<T> f) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    lo[e] -= to_f32(f[e]);
+    hi[e] -= to_f32(f[4 + e]);
+  }
+  return pair_frag<T>(lo, hi);
+}
+
 __device__ __forceinline__ float across(float v, bool maximum) {   // over the four lanes of a column
 #pragma unroll
   for (int o = 16; o < 64; o <<= 1) {
@@ -107,9 +119,8 @@ template <typename T> constexpr int TILE = sizeof(T) == 2 ? 64 : 32;    // rows 
 template <typename T, int DH, int NQ, bool SPLIT>
 __global__ __launch_bounds__(256) void k_cross(CrossP p) {
   constexpr int KT = TILE<T>, NS = KT / 16, NC = DH / 32, ND = DH / 16;
-  // 16 queries a wave are bound by the reading of k and v: P may as well go in two bf16 parts (16 bits),
-  // which leaves the output its own rounding only
-  constexpr int PARTS = sizeof(T) == 2 && NQ == 1 ? 2 : 1;
+  // 16 queries a wave are bound by the reading of k and v, and small heads by the scores: there P goes in two parts
+  constexpr int PARTS = sizeof(T) == 2 && (NQ == 1 || DH == 32) ? 2 : 1;
   typedef Stage<T, KT, DH, 256> St;
   extern __shared__ __attribute__((aligned(16))) char s_mem[];
   T *sk = reinterpret_cast<T *>(s_mem), *sv = sk + KT * St::PITCH;
@@ -203,15 +214,7 @@ __global__ __launch_bounds__(256) void k_cross(CrossP p) {
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
         pf[n] = pair_frag<T>(s[n][j], s[n][j + 1]);
-        if constexpr (PARTS == 2) {
-          f32x4 lo = s[n][j], hi = s[n][j + 1];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            lo[e] -= to_f32(pf[n][e]);
-            hi[e] -= to_f32(pf[n][4 + e]);
-          }
-          rest[n] = pair_frag<T>(lo, hi);
-        }
+        if constexpr (PARTS == 2) rest[n] = rest_frag<T>(s[n][j], s[n][j + 1], pf[n]);
       }
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
@@ -302,6 +305,9 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossP p) {
   }
 }
 
+// The keys that dq sums over: one key alone has P = 1 whatever its score, and dP - delta would be the rounding of both.
+__device__ __forceinline__ int scored_keys(int len) { return len == 1 ? 0 : len; }
+
 // delta of a row: each of head_dim / 8 neighbouring lanes takes eight elements, then their sums are added.  The same in
 // k_cross_delta and in k_dq, so that dk and dv do not depend on whether dq is asked for.
 template <typename T>
@@ -339,7 +345,7 @@ __global__ __launch_bounds__(256) void k_cross_dq(CrossP p) {
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
   const int q0 = (qb * 4 + w) * 16 * NQ, c = prompt_of(a, b), len = keys_of(a, c), kh = h / (a.heads / a.kv_heads);
   const bool idle = q0 >= a.tq;
-  const int tiles = (len + KT - 1) / KT;
+  const int tiles = (scored_keys(len) + KT - 1) / KT;
   const T *K = (const T *)a.k + c * a.kv_bs + kh * a.head_dim, *V = (const T *)a.v + c * a.kv_bs + kh * a.head_dim;
   Frag<T> qf[NQ][NC], df[NQ][NC];
   float lse[NQ], delta[NQ];       // base 2; +inf: the row's probabilities are 0
@@ -386,7 +392,7 @@ __global__ __launch_bounds__(256) void k_cross_dq(CrossP p) {
           }
         }
       }
-      Frag<T> pf[NQ];
+      Frag<T> pf[NQ], rest[NQ];
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
 #pragma unroll
@@ -399,12 +405,16 @@ __global__ __launch_bounds__(256) void k_cross_dq(CrossP p) {
             s[n][x][e] = in ? pr * (dp[n][x][e] - delta[n]) : 0.f;
           }
         pf[n] = pair_frag<T>(s[n][0], s[n][1]);
+        if constexpr (sizeof(T) == 2) rest[n] = rest_frag<T>(s[n][0], s[n][1], pf[n]);
       }
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
         const Frag<T> kf = load_column_frag(sk, St::PITCH, 16 * d, 16 * j + 4 * g, 16 * j + 16 + 4 * g);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) o[n][d] = mma(kf, pf[n], o[n][d]);
+        for (int n = 0; n < NQ; ++n) {
+          o[n][d] = mma(kf, pf[n], o[n][d]);
+          if constexpr (sizeof(T) == 2) o[n][d] = mma(kf, rest[n], o[n][d]);
+        }
       }
     }
   }
@@ -525,11 +535,15 @@ __global__ __launch_bounds__(256, 1) void k_cross_dkv(CrossP p) {
             dp[n][x][e] = s[n][x][e] * (dp[n][x][e] - d4[e]);
           }
       }
-      Frag<T> pf[NK], sf[NK];
+      Frag<T> pf[NK], sf[NK], pr[NK], sr[NK];
 #pragma unroll
       for (int n = 0; n < NK; ++n) {
         pf[n] = pair_frag<T>(s[n][0], s[n][1]);
         sf[n] = pair_frag<T>(dp[n][0], dp[n][1]);
+        if constexpr (sizeof(T) == 2) {
+          pr[n] = rest_frag<T>(s[n][0], s[n][1], pf[n]);
+          sr[n] = rest_frag<T>(dp[n][0], dp[n][1], sf[n]);
+        }
       }
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
@@ -539,6 +553,10 @@ __global__ __launch_bounds__(256, 1) void k_cross_dkv(CrossP p) {
         for (int n = 0; n < NK; ++n) {
           dk[n][d] = mma(qf, sf[n], dk[n][d]);
           dv[n][d] = mma(df, pf[n], dv[n][d]);
+          if constexpr (sizeof(T) == 2) {
+            dk[n][d] = mma(qf, sr[n], dk[n][d]);
+            dv[n][d] = mma(df, pr[n], dv[n][d]);
+          }
         }
       }
     }
@@ -554,7 +572,7 @@ __global__ __launch_bounds__(256, 1) void k_cross_dkv(CrossP p) {
       f32x4 x = dk[n][d], y = dv[n][d];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[e] = i < len ? x[e] * p.scale : 0.f;      // rows past the prompt's end
+        x[e] = i < scored_keys(len) ? x[e] * p.scale : 0.f;      // also rows past the prompt's end
         y[e] = i < len ? y[e] : 0.f;
       }
       if (p.splits > 1) {       // [split][prompt][tk][key head][2][dh]
@@ -661,8 +679,15 @@ __device__ __forceinline__ bf16x8 chunk_frag(const f32x16 &v, int c) {
   return f;
 }
 
-// dq of 128 queries, 32 a wave; also delta, for k_dkv.
-template <int DH>
+__device__ __forceinline__ bf16x8 chunk_rest(const f32x16 &v, int c, bf16x8 f) {
+  bf16x8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (bf16)(v[8 * c + i] - (float)f[i]);
+  return r;
+}
+
+// dq of 128 queries, 32 a wave; also delta, for k_dkv.  TWO: dS in two parts (see two_parts).
+template <int DH, bool TWO>
 __global__ __launch_bounds__(256, 2) void k_dq(CrossP p) {
   constexpr int NC = DH / 16, ND = DH / 32, DG = DH / 4, BLOCKS = 16 * DG / 256, TILE_B = QT * DH * 2;
   constexpr int CH = DH / 8, RPI = 64 / CH, N = 32 / RPI;      // chunks of a row; rows of a 64-lane load; loads of 32 rows
@@ -674,7 +699,7 @@ __global__ __launch_bounds__(256, 2) void k_dq(CrossP p) {
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, g = lane >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q0 = (qb * 4 + w) * 32, c = prompt_of(a, b), len = keys_of(a, c), kh = h / (a.heads / a.kv_heads);
   const bool idle = q0 >= a.tq;
-  const int tiles = (len + QT - 1) / QT, i = q0 + li, at = min(i, a.tq - 1);
+  const int tiles = (scored_keys(len) + QT - 1) / QT, i = q0 + li, at = min(i, a.tq - 1);
   const bf16 *K = (const bf16 *)a.k + c * a.kv_bs + kh * DH, *V = (const bf16 *)a.v + c * a.kv_bs + kh * DH;
   u32x2 kr[BLOCKS][4];
   const int rs = (int)a.kv_rs, cb = column_base(li, g);
@@ -794,11 +819,17 @@ __global__ __launch_bounds__(256, 2) void k_dq(CrossP p) {
           if (t * QT + 32 * x + 8 * (e >> 2) + 4 * g + (e & 3) >= len) dp[e] = 0.f;
       }
       const bf16x8 df2[2] = {chunk_frag(dp, 0), chunk_frag(dp, 1)};
+      bf16x8 dr2[2];
+      if constexpr (TWO) {
+        dr2[0] = chunk_rest(dp, 0, df2[0]);
+        dr2[1] = chunk_rest(dp, 1, df2[1]);
+      }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int y = 0; y < 2 * ND; ++y) {
         if (y + 2 < 2 * ND) cf[(y + 2) % 3] = column(y + 2);
         o[y % ND] = mma32(cf[y % 3], df2[y / ND], o[y % ND]);
+        if constexpr (TWO) o[y % ND] = mma32(cf[y % 3], dr2[y / ND], o[y % ND]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -826,7 +857,7 @@ constexpr int KEYS = 256;            // keys of a workgroup of k_dkv, 32 a wave
 // dk and dv of 256 keys of a prompt's key head against a range of the (candidate, head, query tile) triples that read them.
 // The tiles of q and dout reach LDS by loads that write it themselves, one tile ahead in two buffers; rows past tq are past
 // the buffer's range and read as zero.
-template <int DH>
+template <int DH, bool TWO>
 __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
   constexpr int NC = DH / 16, ND = DH / 32, RB = DH * 2, TILE_B = QT * RB, NCH = RB / 16, ROWS = 64 / NCH;
   extern __shared__ __attribute__((aligned(16))) char s_mem[];
@@ -958,6 +989,13 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
         dp[e] *= s[e];
       }
       const bf16x8 pf[2] = {chunk_frag(s, 0), chunk_frag(s, 1)}, sf[2] = {chunk_frag(dp, 0), chunk_frag(dp, 1)};
+      bf16x8 pr[2], sr[2];
+      if constexpr (TWO)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          pr[y] = chunk_rest(s, y, pf[y]);
+          sr[y] = chunk_rest(dp, y, sf[y]);
+        }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int y = 0; y < 2 * ND; ++y) {
@@ -968,6 +1006,10 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
         }
         dv[y % ND] = mma32(c0, pf[y / ND], dv[y % ND]);
         dk[y % ND] = mma32(c1, sf[y / ND], dk[y % ND]);
+        if constexpr (TWO) {
+          dv[y % ND] = mma32(c0, pr[y / ND], dv[y % ND]);
+          dk[y % ND] = mma32(c1, sr[y / ND], dk[y % ND]);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -982,7 +1024,7 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
       f32x4 x, y;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        x[k] = live ? dk[d][4 * e + k] * p.scale : 0.f;
+        x[k] = live && len > 1 ? dk[d][4 * e + k] * p.scale : 0.f;
         y[k] = live ? dv[d][4 * e + k] : 0.f;
       }
       if (p.splits > 1) {       // [split][prompt][tk][key head][2][dh]
@@ -997,6 +1039,9 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
     }
 }
 
+// P and dS go in two parts where that costs next to nothing: few keys, or few queries, which are bound by the reading of the
+// other side.
+bool two_parts(const CrossArgs &a) { return a.tk <= QT || a.tq <= QT; }
 template <int DH> constexpr size_t dq_lds() { return (size_t)3 * QT * DH * 2 + DH * TP; }
 template <int DH> constexpr size_t dkv_lds() { return (size_t)4 * QT * DH * 2 + 2 * DH * TP + 4 * QT * 4; }
 // Offsets of a tile's rows are 31 bits.
@@ -1113,10 +1158,9 @@ hipError_t gradient(CrossP p, const CrossGradArgs &b, hipStream_t s) {
     if constexpr (sizeof(T) == 2 && DH >= 64) {
       if (wide) {
         p.nqb = (a.tq + 127) / 128;
-        static const hipError_t set = hipFuncSetAttribute((const void *)x32::k_dq<DH>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                          (int)x32::dq_lds<DH>());
-        if (set != hipSuccess) return set;
-        hipLaunchKernelGGL((x32::k_dq<DH>), dim3(unit_grid(p)), dim3(256), (x32::dq_lds<DH>()), s, p);
+        auto kern = x32::two_parts(a) ? x32::k_dq<DH, true> : x32::k_dq<DH, false>;
+        if ((e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)x32::dq_lds<DH>())) != hipSuccess) return e;
+        hipLaunchKernelGGL(kern, dim3(unit_grid(p)), dim3(256), (x32::dq_lds<DH>()), s, p);
       }
     }
     if (!wide) {
@@ -1132,10 +1176,9 @@ hipError_t gradient(CrossP p, const CrossGradArgs &b, hipStream_t s) {
       if (wide) {
         const int64_t sets = ((int64_t)a.n_kv * a.kv_heads * p.splits + 7) / 8 * 8 * ((a.tk + x32::KEYS - 1) / x32::KEYS);
         const size_t bytes = x32::dkv_lds<DH>() + (a.batch + 1) * 4;
-        static const hipError_t set = hipFuncSetAttribute((const void *)x32::k_dkv<DH>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                          (int)(x32::dkv_lds<DH>() + 4097 * 4));
-        if (set != hipSuccess) return set;
-        hipLaunchKernelGGL((x32::k_dkv<DH>), dim3((unsigned)sets), dim3(512), bytes, s, p);
+        auto kern = x32::two_parts(a) ? x32::k_dkv<DH, true> : x32::k_dkv<DH, false>;
+        if ((e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes)) != hipSuccess) return e;
+        hipLaunchKernelGGL(kern, dim3((unsigned)sets), dim3(512), bytes, s, p);
       }
     }
     if (!wide) {

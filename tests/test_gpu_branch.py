@@ -302,6 +302,24 @@ def test_cross_attention_grad(dtype, shape):
     assert torch.equal(alone, dq) and torch.equal(alone_kv, dkv)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dh", [16, 64, 128])
+def test_cross_attention_grad_of_one_key(dtype, dh):
+    """One key has probability 1 whatever its score: nothing reaches q and k, and dv is the sum of dout."""
+    q, kv, _, dout = cross_inputs(dtype, 2, 2, 1, dh, 70, 3, 2, [1, 1], 19)
+    out, lse = cross_call(dtype, q, kv, [0, 1], [1, 1])
+    sizes, qs, ks = (CODE[dtype], 2, 2, 1, dh, 70, 3), (70 * 2 * dh, 2 * dh), (3 * 2 * dh, 2 * dh)
+    dq, dkv = torch.full_like(q, 9.0).cuda(), torch.full_like(kv, 9.0).cuda()
+    ws = torch.empty(fb.flashbon_op_cross_attention_grad_workspace(*sizes, 2), dtype=torch.uint8, device="cuda")
+    kvd, i32 = kv.cuda(), lambda t: torch.tensor(t, dtype=torch.int32, device="cuda")  # noqa: E731
+    fb.flashbon_op_cross_attention_grad(*sizes, q.cuda(), *qs, kvd[:, :, 0], kvd[:, :, 1], *ks, i32([0, 1]), 2, i32([1, 1]), out, *qs, lse,
+                                        dout.cuda(), dq, dkv[:, :, 0], dkv[:, :, 1], workspace=ws)
+    assert not dq.any() and not dkv[:, :, 0].any() and not dkv[:, 1:].any()
+    want = wide(dout).sum((1, 2))
+    # 140 terms of P = 1 within 16 E and a rounding, summed in fp32
+    near(dkv[:, 0, 1, 0], want, U[ACT[dtype]] * np.abs(want) + (U[ACT[dtype]] + 170 * E) * np.abs(wide(dout)).sum((1, 2)), "dv")
+
+
 @pytest.mark.parametrize("tk,pad,swap", [(1, 0, False), (1, 8, True), (5, 8, False), (5, 24, True), (1, 0, True)])
 def test_cross_attention_grad_into_fused_rows(tk, pad, swap):
     """dk and dv in one buffer of alternating rows, one key a prompt among them, and prompts further apart than their rows:
@@ -337,6 +355,41 @@ def test_cross_attention_without_tables():
     got, _ = cross_call("bf16", q, kv, None, None, lse=False, workspace=False)
     want, _ = cross_call("bf16", q, kv, [0, 1, 2], [30, 30, 30])
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("which", ["q", "kv"])
+def test_cross_attention_rows_far_apart(which):
+    """Rows 2^23 elements apart take the kernels whose offsets are 64 bits: within the tolerance of the others, whose rounding of
+    P and dS they share or better."""
+    batch, heads, dh, tq, tk = 1, 1, 128, 70, 67
+    q, kv, _, dout = cross_inputs("bf16", batch, heads, heads, dh, tq, tk, 1, [tk], 20)
+    want, lse = cross_call("bf16", q, kv, [0], [tk])
+    far = 1 << 23
+    room = torch.zeros(70 * far, dtype=torch.bfloat16, device="cuda")
+    view = room.view(70, far)[:, :dh]
+    sizes = (fb.BF16, batch, heads, heads, dh, tq, tk)
+    qd, kd, vd, dd = q.cuda().view(tq, dh), kv[0, :, 0, 0].contiguous().cuda(), kv[0, :, 1, 0].contiguous().cuda(), dout.cuda()
+    strides = {"q": (0, dh), "kv": (0, dh)}
+    if which == "q":
+        view[:tq] = qd
+        qd, strides["q"] = view, (0, far)
+    else:
+        view[:tk] = kd
+        other = torch.zeros(70 * far, dtype=torch.bfloat16, device="cuda").view(70, far)[:, :dh]
+        other[:tk] = vd
+        kd, vd, strides["kv"] = view, other, (0, far)
+    out, ls = torch.empty(tq, dh, dtype=torch.bfloat16, device="cuda"), torch.empty(tq, device="cuda")
+    fb.flashbon_op_cross_attention(*sizes, qd, *strides["q"], kd, vd, *strides["kv"], None, 1, None, out, 0, dh, lse=ls)
+    exact, _ = branch.cross_attention(wide(q), wide(kv[:, :, 0]), wide(kv[:, :, 1]), [0], [tk])
+    mass, _ = branch.cross_attention(wide(q), wide(kv[:, :, 0]), np.abs(wide(kv[:, :, 1])), [0], [tk])
+    near(out, exact[0, :, 0], 2.0 ** -8 * np.abs(exact[0, :, 0]) + (2.0 ** -8 + 500 * E) * mass[0, :, 0], "out")
+    ws = torch.empty(fb.flashbon_op_cross_attention_grad_workspace(*sizes, 1), dtype=torch.uint8, device="cuda")
+    dq, dk, dv = torch.zeros_like(room).view(70, far)[:, :dh] if which == "q" else torch.zeros_like(out), None, None
+    fb.flashbon_op_cross_attention_grad(*sizes, qd, *strides["q"], kd, vd, *strides["kv"], None, 1, None, out, 0, dh, ls, dd, dq, workspace=ws)
+    tq_, _, _ = branch.cross_attention_grad(wide(q), wide(kv[:, :, 0]), wide(kv[:, :, 1]), wide(out).reshape(1, tq, 1, dh), wide(ls).reshape(1, 1, tq),
+                                            wide(dout), [0], [tk])
+    err = np.linalg.norm(wide(dq)[:tq] - tq_[0, :, 0]) / np.linalg.norm(tq_)
+    assert err <= 2 * 2.0 ** -8, err          # two roundings of 2^-8 at most each, of independent signs
 
 
 def test_cross_attention_values_of_tables_are_clamped():
