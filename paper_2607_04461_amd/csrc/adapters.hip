@@ -3,13 +3,15 @@
 //   u = x down_a^T,   out = base + gate s_a u up_a^T
 //   du = s_a dy up_a,   dx = base + du down_a,   d_down_a = sum_m du^T x,   d_up_a = s_a sum_m dy^T u
 // A projection adds 2 r flops to each element it reads and writes, so with r <= 128 all of it is bound by memory: by HBM
-// for many rows, by the latency of two or three launches for few.  Four kernels carry both directions:
-//   * k_down: [rows][K] . [r][K]^T.  A workgroup takes 16 to 64 rows of one group and all ranks, its eight waves every
-//     eighth 32 columns each, straight from memory to the matrix cores; their sums meet in LDS.  x is read once.
-//   * k_up: [rows][r] . [N][r]^T onto the base rows.  The weights feed the left operand with the rows of two tiles
-//     interleaved, so that a lane holds eight consecutive outputs of one row.
+// for many rows, by the latency of its launches for few.  The kernels carry both directions:
+//   * k_both: a tile of rows of one adapter through both products.  x goes straight from memory to the matrix cores, every
+//     eighth block of columns on each of eight waves, whose sums meet in LDS; u's tile stays there for the second product.
+//     24960 rows, 1536 to 1536, rank 32, bf16: 59 us, 3.7 TB/s (as k_down and k_up 75, most of it rows in 64-byte pieces).
+//   * k_down, k_up: the same in two launches, for few rows on large weights, whose ranks and columns then go to many
+//     workgroups.
 //   * k_outer: the sum over rows of an outer product, both operands through LDS, the activations' columns by transposing
-//     reads.  Rows reach it through lists sorted by adapter, in chunks; k_outer_sum adds the chunks' sums in order.
+//     reads: 39 us for both gradients of the case above, x and dy at 3.9 TB/s.  Rows reach it through lists sorted by
+//     adapter, in chunks; k_outer_sum adds the chunks' sums in order.
 //   * k_prepare: those lists, and up and down the other way round for the gradient's two products.
 // u and du are fp32 and stay so: next to bf16 weights each is split into bf16 parts that are multiplied one by one, three
 // where the result is fp32 (24 bits) and two where it is bf16 (16 bits of it, against the 8 that are kept).
@@ -44,18 +46,58 @@ __device__ __forceinline__ void split(f32x8 v, Frag<T> (&p)[P]) {
     }
 }
 
-struct Tile {     // rows [row0, row0 + rows) of one group
-  int64_t group, row0;
-  int rows;
+// Rows of a workgroup, all of one adapter (-1: none): [row0, row0 + rows) of one group, or those in a list in LDS.
+struct Tile {
+  int64_t row0;
+  const int *list;
+  int rows, ad;
+  __device__ __forceinline__ int64_t row(int i) const { return list ? list[i] : row0 + i; }
 };
-__device__ __forceinline__ Tile tile_at(int64_t id, int size, int64_t M, int per) {
+__device__ __forceinline__ Tile group_tile(int64_t id, int size, int64_t M, int per, const int32_t *index, int count) {
   const int tiles = (per + size - 1) / size;
+  const int64_t group = id / tiles, from = (id % tiles) * size;
   Tile t;
-  t.group = id / tiles;
-  const int64_t from = (id % tiles) * size;
-  t.row0 = t.group * per + from;
+  t.row0 = group * per + from;
+  t.list = nullptr;
   t.rows = (int)max((int64_t)0, min(min((int64_t)size, per - from), M - t.row0));
+  t.ad = t.rows > 0 ? adapter_of(index, group, count) : -1;
   return t;
+}
+// Rows 16 j .. 16 j + 15 of those with adapter id % (count + 1), the last of which is none, j = id / (count + 1): where groups
+// are shorter than a tile, so that the rows of an adapter share a reading of its weights.  Each workgroup searches the index.
+__device__ __forceinline__ Tile gathered_tile(int id, int64_t M, int per, const int32_t *index, int count, int *s_list, int *s_wave) {
+  const int me = id % (count + 1), from = id / (count + 1) * 16, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int waves = blockDim.x >> 6, rows = (int)M;
+  int seen = 0;
+  for (int m0 = 0; m0 < rows && seen < from + 16; m0 += blockDim.x) {
+    const int m = m0 + threadIdx.x, ad = m < rows ? adapter_of(index, m / per, count) : -2;
+    const bool match = ad == (me == count ? -1 : me);
+    const uint64_t votes = __ballot(match);
+    if (lane == 0) s_wave[w] = __popcll(votes);
+    __syncthreads();
+    int slot = seen + __popcll(votes & ((1ull << lane) - 1)) - from;
+    for (int i = 0; i < waves; ++i) {
+      if (i < w) slot += s_wave[i];
+      seen += s_wave[i];
+    }
+    if (match && slot >= 0 && slot < 16) s_list[slot] = m;
+    __syncthreads();
+  }
+  Tile t;
+  t.row0 = 0;
+  t.list = s_list;
+  t.rows = max(0, min(16, seen - from));
+  t.ad = me == count ? -1 : me;
+  return t;
+}
+template <int SIZE, bool GATHER>
+__device__ __forceinline__ Tile tile_of(int64_t id, int64_t M, int per, const int32_t *index, int count) {
+  if constexpr (GATHER) {
+    __shared__ int s_list[16], s_wave[8];
+    return gathered_tile((int)id, M, per, index, count, s_list, s_wave);
+  } else {
+    return group_tile(id, SIZE, M, per, index, count);
+  }
 }
 
 struct DownArgs {
@@ -71,17 +113,19 @@ constexpr int WAVES = 8;        // each sums every eighth block of columns; thei
 
 // The waves' shares of x down^T for a tile's rows, to s_part [WAVES][MT RT][256]; a barrier must follow.
 template <typename T, int MT, int RT>
-__device__ __forceinline__ void down_shares(const DownArgs &a, const Tile &t, int ad, float *s_part) {
+__device__ __forceinline__ void down_shares(const DownArgs &a, const Tile &t, int rank0, float *s_part) {
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   f32x4 acc[MT][RT];
   const T *xr[MT], *wr[RT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) xr[i] = (const T *)a.x + (t.row0 + min(16 * i + li, t.rows - 1)) * a.K;
+  for (int i = 0; i < MT; ++i) xr[i] = (const T *)a.x + t.row(min(16 * i + li, t.rows - 1)) * a.K;
 #pragma unroll
-  for (int j = 0; j < RT; ++j) wr[j] = (const T *)a.w + ((int64_t)ad * a.rank + min(16 * j + li, a.rank - 1)) * a.K;
+  for (int j = 0; j < RT; ++j) wr[j] = (const T *)a.w + ((int64_t)t.ad * a.rank + min(rank0 + 16 * j + li, a.rank - 1)) * a.K;
   constexpr int SUB = 4 / sizeof(T), BLOCK = 32 * SUB;       // a wave takes whole lines of 128 bytes
-  Frag<T> xf[2][SUB][MT], wf[2][SUB][RT];
+  // blocks in flight: as many as their registers allow, since the few rows of a small tile wait on nothing else
+  constexpr int DEPTH = MT == 1 && RT * sizeof(T) <= 4 ? 4 : 2;
+  Frag<T> xf[DEPTH][SUB][MT], wf[DEPTH][SUB][RT];
   auto load = [&](int b, int block) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < SUB; ++c) {
@@ -106,16 +150,18 @@ __device__ __forceinline__ void down_shares(const DownArgs &a, const Tile &t, in
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int s = w;
-  if (s < blocks) load(0, s);
-  while (s < blocks) {       // the next block's loads in flight under this one's products
-    if (s + WAVES < blocks) load(1, s + WAVES);
-    multiply(0);
-    s += WAVES;
-    if (s >= blocks) break;
-    if (s + WAVES < blocks) load(0, s + WAVES);
-    multiply(1);
-    s += WAVES;
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d)
+    if (w + d * WAVES < blocks) load(d, w + d * WAVES);
+  for (int s0 = w; s0 < blocks; s0 += DEPTH * WAVES) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int s = s0 + d * WAVES;
+      if (s < blocks) {
+        multiply(d);
+        if (s + DEPTH * WAVES < blocks) load(d, s + DEPTH * WAVES);
+      }
+    }
   }
   // element (row 4 g + e, rank li) of tile (i, j)
 #pragma unroll
@@ -136,23 +182,23 @@ __device__ __forceinline__ float down_sum(const float *s_part, int p, int &row, 
   return v;
 }
 
-template <typename T, int MT, int RT>
+template <typename T, int MT, int RT, bool GATHER>
 __global__ __launch_bounds__(64 * WAVES) void k_down(DownArgs a) {
   extern __shared__ __attribute__((aligned(16))) float s_part[];
-  const Tile t = tile_at(blockIdx.x, 16 * MT, a.M, a.per);
+  const Tile t = tile_of<16 * MT, GATHER>(blockIdx.x, a.M, a.per, a.index, a.count);
   if (t.rows <= 0) return;
-  const int ad = adapter_of(a.index, t.group, a.count);
-  if (ad < 0) {
-    for (int i = threadIdx.x; i < t.rows * a.rank; i += 64 * WAVES) a.u[t.row0 * a.rank + i] = 0.f;
+  const int rank0 = blockIdx.y * 16 * RT, ranks = min(16 * RT, a.rank - rank0);
+  if (t.ad < 0) {
+    for (int i = threadIdx.x; i < t.rows * ranks; i += 64 * WAVES) a.u[t.row(i / ranks) * a.rank + rank0 + i % ranks] = 0.f;
     return;
   }
-  down_shares<T, MT, RT>(a, t, ad, s_part);
+  down_shares<T, MT, RT>(a, t, rank0, s_part);
   __syncthreads();
-  const float scale = a.scales ? a.scales[ad] : 1.f;
+  const float scale = a.scales ? a.scales[t.ad] : 1.f;
   for (int p = threadIdx.x; p < MT * RT * 256; p += 64 * WAVES) {
     int row, r;
     const float v = down_sum<MT, RT>(s_part, p, row, r) * scale;
-    if (row < t.rows && r < a.rank) a.u[(t.row0 + row) * a.rank + r] = v;
+    if (row < t.rows && r < ranks) a.u[t.row(row) * a.rank + rank0 + r] = v;
   }
 }
 
@@ -176,11 +222,12 @@ template <typename O> constexpr int TURN = 256 / sizeof(O);
 template <typename O> constexpr int OUT_PITCH = TURN<O> + 4;
 template <typename O> constexpr size_t OUT_BYTES = 16 * OUT_PITCH<O> * 4;      // of a wave
 template <typename T, typename O, int MT, int RK>
-__device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, int ad, const Frag<T> (&uf)[MT][RK][PARTS<T, O>], float *s_out,
+__device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, const Frag<T> (&uf)[MT][RK][PARTS<T, O>], float *s_out,
                                            int from, int to, int first, int waves) {
   constexpr int E = 16 / sizeof(O), Q = TURN<O> / 32;        // elements of a lane's piece; groups of 32 columns
   typedef O Piece __attribute__((ext_vector_type(E)));
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
+  const int ad = t.ad;
   const float scale = ad < 0 ? 0.f : a.scales ? a.scales[ad] : 1.f;
   const T *W = (const T *)a.w + (int64_t)max(ad, 0) * a.N * a.rank;
   // column of row li of tile h: four of each eight
@@ -193,7 +240,7 @@ __device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, int a
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int row = 16 * i + 4 * x + g;
-        if (a.base && n < to && row < t.rows) b[i][x] = *reinterpret_cast<const Piece *>((const O *)a.base + (t.row0 + row) * a.N + n);
+        if (a.base && n < to && row < t.rows) b[i][x] = *reinterpret_cast<const Piece *>((const O *)a.base + t.row(row) * a.N + n);
         else b[i][x] = (Piece)((O)0.f);
       }
     Frag<T> wf[Q][2][RK];
@@ -238,31 +285,29 @@ __device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, int a
             for (int e = 0; e < 4; ++e) o[4 * y + e] = from_f32<O>(fmaf(f[4 * y + e], v[e], to_f32(o[4 * y + e])));
           }
         }
-        if (n < to && row < t.rows) *reinterpret_cast<Piece *>((O *)a.out + (t.row0 + row) * a.N + n) = o;
+        if (n < to && row < t.rows) *reinterpret_cast<Piece *>((O *)a.out + t.row(row) * a.N + n) = o;
       }
       own_lds();
     }
   }
 }
 
-template <typename T, typename O, int MT, int RK>
+template <typename T, typename O, int MT, int RK, bool GATHER>
 __global__ __launch_bounds__(256) void k_up(UpArgs a) {
   extern __shared__ __attribute__((aligned(16))) float s_part[];
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Tile t = tile_at(blockIdx.x / a.parts, 16 * MT, a.M, a.per);      // a row's workgroups follow each other
-  if (t.rows <= 0) return;
-  const int ad = adapter_of(a.index, t.group, a.count);
-  if (ad < 0 && a.base == a.out) return;
+  const Tile t = tile_of<16 * MT, GATHER>(blockIdx.x / a.parts, a.M, a.per, a.index, a.count);      // a row's workgroups follow each other
+  if (t.rows <= 0 || (t.ad < 0 && a.base == a.out)) return;
   Frag<T> uf[MT][RK][PARTS<T, O>];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int c = 0; c < RK; ++c) {
       const int r = 32 * c + 8 * g;
-      split<T, PARTS<T, O>>(r < a.rank ? load_frag(a.u + (t.row0 + min(16 * i + li, t.rows - 1)) * a.rank + r) : zero_frag<float>(), uf[i][c]);
+      split<T, PARTS<T, O>>(r < a.rank ? load_frag(a.u + t.row(min(16 * i + li, t.rows - 1)) * a.rank + r) : zero_frag<float>(), uf[i][c]);
     }
   const int from = blockIdx.x % a.parts * a.cols;
-  up_columns<T, O, MT, RK>(a, t, ad, uf, s_part + w * (OUT_BYTES<O> / 4), from, min(from + a.cols, a.N), w, 4);
+  up_columns<T, O, MT, RK>(a, t, uf, s_part + w * (OUT_BYTES<O> / 4), from, min(from + a.cols, a.N), w, 4);
 }
 
 template <typename O, int MT, int RT> constexpr size_t both_lds() {
@@ -271,19 +316,19 @@ template <typename O, int MT, int RT> constexpr size_t both_lds() {
 }
 
 // Both in one launch: u's tile stays in LDS.  d.u, its scales and the sums' order as in k_down, so the bits are the same.
-template <typename T, typename O, int MT, int RT>
+template <typename T, typename O, int MT, int RT, bool GATHER>
 __global__ __launch_bounds__(64 * WAVES) void k_both(DownArgs d, UpArgs a) {
   constexpr int RK = RT < 2 ? 1 : RT / 2, PITCH = 32 * RK + 4;
   extern __shared__ __attribute__((aligned(16))) float s_part[];
   // u's tile [16 MT][PITCH], zero past the rank, behind the larger of the shares and the waves' products
   float *su = s_part + (both_lds<O, MT, RT>() / 4 - 16 * MT * PITCH);
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
-  const Tile t = tile_at(blockIdx.x, 16 * MT, a.M, a.per);
+  const Tile t = tile_of<16 * MT, GATHER>(blockIdx.x, a.M, a.per, a.index, a.count);
   if (t.rows <= 0) return;
-  const int ad = adapter_of(a.index, t.group, a.count);
+  const int ad = t.ad;
   Frag<T> uf[MT][RK][PARTS<T, O>];
   if (ad < 0) {
-    for (int i = threadIdx.x; i < t.rows * a.rank; i += 64 * WAVES) d.u[t.row0 * a.rank + i] = 0.f;
+    for (int i = threadIdx.x; i < t.rows * a.rank; i += 64 * WAVES) d.u[t.row(i / a.rank) * a.rank + i % a.rank] = 0.f;
     if (a.base == a.out) return;
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -292,13 +337,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_both(DownArgs d, UpArgs a) {
 #pragma unroll
         for (int p = 0; p < PARTS<T, O>; ++p) uf[i][c][p] = zero_frag<T>();
   } else {
-    down_shares<T, MT, RT>(d, t, ad, s_part);
+    down_shares<T, MT, RT>(d, t, 0, s_part);
     __syncthreads();
     const float scale = d.scales ? d.scales[ad] : 1.f;
     for (int p = threadIdx.x; p < MT * RT * 256; p += 64 * WAVES) {
       int row, r;
       const float v = down_sum<MT, RT>(s_part, p, row, r) * scale;
-      if (row < t.rows && r < a.rank) d.u[(t.row0 + row) * a.rank + r] = v;
+      if (row < t.rows && r < a.rank) d.u[t.row(row) * a.rank + r] = v;
       su[row * PITCH + r] = r < a.rank ? v : 0.f;
       if (RT == 1) su[row * PITCH + r + 16] = 0.f;
     }
@@ -310,7 +355,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_both(DownArgs d, UpArgs a) {
   }
   // u's tile has been read; the shares' place serves the products
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  up_columns<T, O, MT, RK>(a, t, ad, uf, s_part + w * (OUT_BYTES<O> / 4), 0, a.N, w, WAVES);
+  up_columns<T, O, MT, RK>(a, t, uf, s_part + w * (OUT_BYTES<O> / 4), 0, a.N, w, WAVES);
 }
 
 // What the gradient needs first, in one launch of [blocks][2 count + count]: the transposed weights, out[z][c][r] =
@@ -545,7 +590,8 @@ __global__ __launch_bounds__(256) void k_outer_sum(int count, int64_t down, int6
   }
 }
 
-// Rows of a tile: as many as leave a tile a CU at least, and no more than a group has (measured at the launches below).
+// Rows of a tile: as many as leave a tile a CU at least, and no more than a group has.  More rows read the weights less often,
+// fewer leave more workgroups in flight: 24960 x 1536 x 1536, rank 32, both products 69 us on 32 rows, 71 on 64, 78 on 16.
 int tile_rows(int64_t M, int per, int most) {
   int mt = most;
   while (mt > 1 && (16 * (mt / 2) >= per || (M + 16 * mt - 1) / (16 * mt) < 256)) mt /= 2;
@@ -553,39 +599,49 @@ int tile_rows(int64_t M, int per, int most) {
 }
 int64_t tiles_of(int64_t M, int per, int rows) { return (M + per - 1) / per * ((per + rows - 1) / rows); }
 
-template <typename T, int MT, int RT>
+// Whether rows are gathered by their adapters: groups shorter than a tile, where that takes not many more workgroups and the
+// search of the index stays short.  254 fp32 rows of 11 adapters, rank 128, 13824 to 5120: 118 us, in a tile a row 386.
+bool gathers(int64_t M, int per, int count) {
+  return per < 16 && M <= 8192 && (M + 15) / 16 * (count + 1) <= 2 * ((M + per - 1) / per);
+}
+template <bool GATHER> int64_t tiles_for(int64_t M, int per, int count, int rows) {
+  return GATHER ? (M + 15) / 16 * (count + 1) : tiles_of(M, per, rows);
+}
+
+template <typename T, int MT, int RT, bool GATHER = false>
 hipError_t down_tile(const DownArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((k_down<T, MT, RT>), dim3((unsigned)tiles_of(a.M, a.per, 16 * MT)), dim3(64 * WAVES), WAVES * MT * RT * 1024, s, a);
+  hipLaunchKernelGGL((k_down<T, MT, RT, GATHER>), dim3((unsigned)tiles_for<GATHER>(a.M, a.per, a.count, 16 * MT), (a.rank + 16 * RT - 1) / (16 * RT)),
+                     dim3(64 * WAVES), WAVES * MT * RT * 1024, s, a);
   return hipGetLastError();
 }
-// the waves' sums take MT RT 8 KB of LDS: 64 KB at most, two workgroups a CU
+// The waves' sums take MT RT 8 KB of LDS: 64 KB at most, two workgroups a CU.  Few tiles share the ranks among workgroups:
+// two rows, 64 ranks of 8960 to 1536, took 41 us on one CU each and take 18.
 template <typename T>
 hipError_t launch_down(const DownArgs &a, hipStream_t s) {
-  if (a.rank <= 16) {
-    const int mt = tile_rows(a.M, a.per, 4);
-    return mt == 4 ? down_tile<T, 4, 1>(a, s) : mt == 2 ? down_tile<T, 2, 1>(a, s) : down_tile<T, 1, 1>(a, s);
-  }
-  if (a.rank <= 32) {
-    const int mt = tile_rows(a.M, a.per, 4);
-    return mt == 4 ? down_tile<T, 4, 2>(a, s) : mt == 2 ? down_tile<T, 2, 2>(a, s) : down_tile<T, 1, 2>(a, s);
-  }
-  if (a.rank <= 64) return tile_rows(a.M, a.per, 2) == 2 ? down_tile<T, 2, 4>(a, s) : down_tile<T, 1, 4>(a, s);
+  if (gathers(a.M, a.per, a.count)) return down_tile<T, 1, 1, true>(a, s);
+  const int mt = tile_rows(a.M, a.per, 4);
+  if (mt == 1 && tiles_of(a.M, a.per, 16) < 256) return down_tile<T, 1, 1>(a, s);
+  if (a.rank <= 16) return mt == 4 ? down_tile<T, 4, 1>(a, s) : mt == 2 ? down_tile<T, 2, 1>(a, s) : down_tile<T, 1, 1>(a, s);
+  if (a.rank <= 32) return mt == 4 ? down_tile<T, 4, 2>(a, s) : mt == 2 ? down_tile<T, 2, 2>(a, s) : down_tile<T, 1, 2>(a, s);
+  if (a.rank <= 64) return mt >= 2 ? down_tile<T, 2, 4>(a, s) : down_tile<T, 1, 4>(a, s);
   return down_tile<T, 1, 8>(a, s);
 }
 
-template <typename T, typename O, int MT, int RK>
+template <typename T, typename O, int MT, int RK, bool GATHER = false>
 hipError_t up_tile(UpArgs a, hipStream_t s) {
-  const int64_t tiles = tiles_of(a.M, a.per, 16 * MT);
+  const int64_t tiles = tiles_for<GATHER>(a.M, a.per, a.count, 16 * MT);
   // columns of a workgroup: enough workgroups for eight a CU, a turn of its four waves at least
   constexpr int turn = 4 * TURN<O>;
   const int64_t turns = (a.N + turn - 1) / turn, parts = std::min<int64_t>(turns, std::max<int64_t>(1, 2048 / tiles));
   a.cols = (int)((turns + parts - 1) / parts * turn);
   a.parts = (a.N + a.cols - 1) / a.cols;
-  hipLaunchKernelGGL((k_up<T, O, MT, RK>), dim3((unsigned)(tiles * a.parts)), dim3(256), 4 * OUT_BYTES<O>, s, a);
+  hipLaunchKernelGGL((k_up<T, O, MT, RK, GATHER>), dim3((unsigned)(tiles * a.parts)), dim3(256), 4 * OUT_BYTES<O>, s, a);
   return hipGetLastError();
 }
 template <typename T, typename O>
 hipError_t launch_up(const UpArgs &a, hipStream_t s) {
+  if (gathers(a.M, a.per, a.count))
+    return a.rank <= 32 ? up_tile<T, O, 1, 1, true>(a, s) : a.rank <= 64 ? up_tile<T, O, 1, 2, true>(a, s) : up_tile<T, O, 1, 4, true>(a, s);
   if (a.rank <= 32) {
     const int mt = tile_rows(a.M, a.per, 4);
     return mt == 4 ? up_tile<T, O, 4, 1>(a, s) : mt == 2 ? up_tile<T, O, 2, 1>(a, s) : up_tile<T, O, 1, 1>(a, s);
@@ -595,27 +651,30 @@ hipError_t launch_up(const UpArgs &a, hipStream_t s) {
   return mt == 2 ? up_tile<T, O, 2, 4>(a, s) : up_tile<T, O, 1, 4>(a, s);
 }
 
-template <typename T, typename O, int MT, int RT>
+template <typename T, typename O, int MT, int RT, bool GATHER = false>
 hipError_t both_tile(const DownArgs &d, const UpArgs &a, hipStream_t s) {
   constexpr size_t lds = both_lds<O, MT, RT>();
   if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute((const void *)k_both<T, O, MT, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    const hipError_t e = hipFuncSetAttribute((const void *)k_both<T, O, MT, RT, GATHER>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_both<T, O, MT, RT>), dim3((unsigned)tiles_of(a.M, a.per, 16 * MT)), dim3(64 * WAVES), lds, s, d, a);
+  hipLaunchKernelGGL((k_both<T, O, MT, RT, GATHER>), dim3((unsigned)tiles_for<GATHER>(a.M, a.per, a.count, 16 * MT)), dim3(64 * WAVES), lds, s, d, a);
   return hipGetLastError();
 }
 
-// u = d.scales x down^T, then out = base + a.gate a.scales u up^T.  In one launch where the rows fill the card or a workgroup
-// has few turns of 512 columns; else the columns of few rows go to several workgroups.
+// u = d.scales x down^T, then out = base + a.gate a.scales u up^T.  In one launch where the rows fill the card, or the weights
+// are so small that one CU passes them in the time of a second launch; else the columns and ranks of few rows go to several
+// workgroups.
 template <typename T, typename O>
 hipError_t launch_both(const DownArgs &d, const UpArgs &a, hipStream_t s) {
   const bool wide = sizeof(T) == 4 && a.rank > 32;       // fp32 operands of many ranks: no registers for two tiles of rows
   const int mt = tile_rows(a.M, a.per, wide ? 1 : 2);
-  if ((tiles_of(a.M, a.per, 16 * mt) < 256 && a.N > 2048) || (sizeof(T) == 4 && a.rank > 64)) {
+  const bool gather = gathers(a.M, a.per, a.count), small = a.rank <= 32 && a.N <= 2048 && d.K <= 2048;
+  if ((gather || tiles_of(a.M, a.per, 16 * mt) < 256 ? !small : false) || (sizeof(T) == 4 && a.rank > 64)) {
     const hipError_t e = launch_down<T>(d, s);
     return e != hipSuccess ? e : launch_up<T, O>(a, s);
   }
+  if (gather) return a.rank <= 16 ? both_tile<T, O, 1, 1, true>(d, a, s) : both_tile<T, O, 1, 2, true>(d, a, s);
   if (a.rank <= 16) return mt == 2 ? both_tile<T, O, 2, 1>(d, a, s) : both_tile<T, O, 1, 1>(d, a, s);
   if (a.rank <= 32) return mt == 2 ? both_tile<T, O, 2, 2>(d, a, s) : both_tile<T, O, 1, 2>(d, a, s);
   if constexpr (sizeof(T) == 4) return both_tile<T, O, 1, 4>(d, a, s);

@@ -5,14 +5,17 @@
 // dk and dv are summed over the prompt's candidates and the heads that share the key head, in their order; no atomics.
 //
 // All kernels keep one side in registers and take the other in tiles through LDS, and form the scores so that a lane's
-// values belong to one row of the side it keeps: the 16 x 16 products of two tiles then are the right operand of the next
-// product as they stand, with its k in the order 4 g + 0..3, 16 + 4 g + 0..3, which the left operand's transposing LDS
-// reads follow.  P and dS are rounded to the operands' type for that product (bf16: 8 bits, as the values they meet).
+// values belong to one row of the side it keeps: the products of two tiles then are the right operand of the next product as
+// they stand, with its k in an order that the left operand follows.  P and dS are rounded to the operands' type for that
+// product (bf16: 8 bits, as the values they meet; in two parts where that is free).
 //   * k_cross: a wave keeps 16 or 32 queries.  One pass over the keys with the running maximum and sum.
 //   * k_cross_dq: the same with dout and lse: two products give P and dP, the third dq.
 //   * k_cross_dkv: a wave keeps keys and values; the queries and dout of all candidates of the prompt pass by.
+//   * x32::k_dq, x32::k_dkv: the same for bf16 and head dims 64 and 128, on 32 x 32 x 16 products.
+// bf16 of head dim 128 with more than 64 queries runs forward on k_attn_fa (attention.hip).
 // Bound by the matrix cores for many queries, by the reading of k and v for few: then ranges of keys go to several
-// workgroups and k_cross_join joins them.
+// workgroups and k_cross_join joins them (one query of 40 heads to 4001 keys: 18 us and 4, 82 MB at 4.5 TB/s).  fp32, 4 x 12
+// heads of 1560 x 512, head dim 128: forward 211 us (93 TFLOP/s of 154), gradient 741.
 #include <algorithm>
 
 #include "fragments.h"
@@ -599,6 +602,9 @@ __global__ __launch_bounds__(256, 1) void k_cross_dkv(CrossP p) {
 // operand comes out of a transposed copy of the tile in LDS whose groups of four are kept in that order, so that it is one
 // 16-byte read (gfx950's transposing reads pass 71 bytes a clock and CU here, 16-byte reads 190, and the products of one
 // candidate's tile need 128).  The copy costs each thread a few 8-byte reads, byte permutations and writes a tile.
+// 4 x 40 heads of 4096 queries, head dim 128, prompts of 512 and 300 keys (341 GFLOP as five products, 478 as the seven that
+// two kernels form): k_dq 320 us, 140 of them its rows in and out at HBM's rate, k_dkv 355, k_cross_sum 23; with every prompt
+// of 512 keys 715 us in all.  On 16 x 16 products k_cross_dq took 533, k_cross_dkv 670 and delta, now formed by k_dq, 65.
 // Both corrections enter as the accumulators' first values: S starts at -lse, dP at -delta, so that a pair of exponent and
 // product is all that is left to do for an element.
 namespace x32 {
@@ -854,6 +860,8 @@ __global__ __launch_bounds__(256, 2) void k_dq(CrossP p) {
 
 constexpr int KEYS = 256;            // keys of a workgroup of k_dkv, 32 a wave
 
+// Measured and not kept: 64 keys a wave on one wave a SIMD, half the LDS reads: 320 accumulators are more than the 256
+// accumulation registers, and moving them took 860 us; operands read two steps ahead: they spill.
 // dk and dv of 256 keys of a prompt's key head against a range of the (candidate, head, query tile) triples that read them.
 // The tiles of q and dout reach LDS by loads that write it themselves, one tile ahead in two buffers; rows past tq are past
 // the buffer's range and read as zero.
@@ -1093,7 +1101,7 @@ template <typename T> int key_splits(const CrossArgs &a) {
 template <typename T> constexpr int BLOCK_KEYS = sizeof(T) == 2 ? 128 : 64;
 
 // Into how many ranges the queries of k_cross_dkv and k_dkv are cut, for the least estimate of whole rounds of workgroups
-// (one a CU) at 2 us a tile of queries, and of the ranges' sums, written and read at 5 bytes a ps; four tiles each at least.
+// (one a CU) at 2 us a tile of queries, and of the ranges' sums, written and read at 5 bytes a ps; a tile each at least.
 // By the sizes alone, not by the kernel that takes the strides, since the workspace goes by it.
 template <typename T> int query_splits(const CrossArgs &a) {
   const int keys = sizeof(T) == 2 && a.head_dim >= 64 ? x32::KEYS : BLOCK_KEYS<T>;
@@ -1102,7 +1110,7 @@ template <typename T> int query_splits(const CrossArgs &a) {
   const double bytes = 16.0 * a.n_kv * a.tk * a.kv_heads * a.head_dim;
   int best = 1;
   double least = 0;
-  for (int s = 1; s <= 64 && (s == 1 || tiles >= 4 * s); ++s) {
+  for (int s = 1; s <= 64 && (s == 1 || tiles >= s); ++s) {
     const double cost = (double)((wgs * s + 255) / 256) * tiles / s * 2.0 + (s > 1 ? s * bytes / 5e6 + 4 : 0);
     if (s == 1 || cost < least) {
       best = s;

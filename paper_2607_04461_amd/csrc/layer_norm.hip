@@ -3,7 +3,8 @@
 //   g = dy f,   dx = residual + rstd (g - mean(g) - xhat mean(g xhat))
 //   dweight = sum_m dy xhat,   dbias = sum_m dy over the rows of a group (they share a weight and a bias)
 // Both are bound by HBM: every row is read once and held in registers between its reductions, by one wave up to
-// 2048 elements and by four beyond.  The mean is summed in 64 bits (a few per cent of the time a row's bytes take)
+// 2048 elements and by four beyond (16384 x 5120 to bf16 97 us, 5.2 TB/s; the gradient of 24960 x 1536 with the residual
+// stream's 113 us and 4 for the vectors' sums, 4.8 TB/s).  The mean is summed in 64 bits (a few per cent of the time a row's bytes take)
 // and taken off in two parts, so that rows far from zero keep their digits; the other sums are fp32.
 // The gradient of the vectors is a sum over thousands of rows: a workgroup adds up a chunk of rows of one group in
 // registers, and a second launch adds the chunks' sums in order, in 64 bits.  No atomics: a call's bits are always
@@ -290,7 +291,7 @@ hipError_t grad_by_width(const LayerNormGradArgs &a, int64_t blocks, bool vec, h
 }
 
 // Rows of a chunk: four workgroups a CU (by the 256 of the card, not those seen: the order of the sums goes by it), and not
-// fewer than a row a wave (1037 x 701 in chunks of 16 rows 17 us, of 4 rows REPLACE).
+// fewer than a row a wave (1037 x 701, fp32: 17 us in chunks of 16 rows, 10 of 4).
 int chunk_rows(int64_t M, int per) {
   return (int)std::min<int64_t>(per, std::max<int64_t>(4, (M + 1023) / 1024));
 }
