@@ -112,7 +112,7 @@ flashbon_status flashbon_op_unpatch_sde(int32_t n, int32_t C, int32_t H, int32_t
  * linear layers in 8-bit integers (flashbon_draft_step itself does not).  A DiT branch runs as
  *   flashbon_op_norm_residual (int8 rows of the modulated norm) -> flashbon_op_linear_i8 (GELU) ->
  *   flashbon_op_quant_rows -> flashbon_op_linear_i8 -> flashbon_op_norm_residual (the next branch's rows),
- * on weights that flashbon_op_quant_rows made once.  There is no training path, as in the rest of the library.
+ * on weights that flashbon_op_quant_rows made once.  There is no training path through them.
  * Addresses need no more alignment than their elements (rows of odd length included); 16 bytes, K % 16 == 0 and
  * N % 8 == 0 are fastest. */
 
