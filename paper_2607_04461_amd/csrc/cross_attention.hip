@@ -9,7 +9,7 @@
 // they stand, with its k in an order that the left operand follows.  P and dS are rounded to the operands' type for that
 // product (bf16: 8 bits, as the values they meet; in two parts where that is free).
 //   * k_cross: a wave keeps 16 or 32 queries.  One pass over the keys with the running maximum and sum.
-//   * k_cross_dq: the same with dout and lse: two products give P and dP, the third dq.
+//   * k_cross_dq: the same with dout, lse and delta, which it forms: two products give P and dP, the third dq.
 //   * k_cross_dkv: a wave keeps keys and values; the queries and dout of all candidates of the prompt pass by.
 //   * x32::k_dq, x32::k_dkv: the same for bf16 and head dims 64 and 128, on 32 x 32 x 16 products.
 // bf16 of head dim 128 with more than 64 queries runs forward on k_attn_fa (attention.hip).
@@ -311,13 +311,18 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossP p) {
 // The keys that dq sums over: one key alone has P = 1 whatever its score, and dP - delta would be the rounding of both.
 __device__ __forceinline__ int scored_keys(int len) { return len == 1 ? 0 : len; }
 
-// delta of a row: each of head_dim / 8 neighbouring lanes takes eight elements, then their sums are added.  The same in
-// k_cross_delta and in k_dq, so that dk and dv do not depend on whether dq is asked for.
+// delta of a row: the sums of eight products each, added in pairs 8, 4, 2 and 1 eights apart.  The same in k_cross_delta and
+// in the kernels of dq, so that dk and dv do not depend on whether dq is asked for.
 template <typename T>
-__device__ __forceinline__ float row_delta(Frag<T> x, Frag<T> y, int lanes) {
+__device__ __forceinline__ float eight_products(Frag<T> x, Frag<T> y) {
   float s = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) s = fmaf(to_f32(x[e]), to_f32(y[e]), s);
+  return s;
+}
+template <typename T>
+__device__ __forceinline__ float row_delta(Frag<T> x, Frag<T> y, int lanes) {
+  float s = eight_products<T>(x, y);
   for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   return s;
 }
@@ -360,7 +365,18 @@ __global__ __launch_bounds__(256) void k_cross_dq(CrossP p) {
     row_frags<T, DH>(df[n], (const T *)p.dout + b * a.o_bs + (int64_t)at * a.o_rs + h * a.head_dim, a.head_dim, i < a.tq);
     const int64_t r = ((int64_t)b * a.heads + h) * a.tq + at;
     lse[n] = i < a.tq && a.lse[r] != -INFINITY ? a.lse[r] * LOG2E : INFINITY;
-    delta[n] = p.delta[r];
+    {   // delta in k_cross_delta's order: a lane has eights g, 4 + g, 8 + g, 12 + g of the row
+      Frag<T> of[NC];
+      row_frags<T, DH>(of, (const T *)a.out + b * a.o_bs + (int64_t)at * a.o_rs + h * a.head_dim, a.head_dim, i < a.tq);
+      float e[NC];
+#pragma unroll
+      for (int k = 0; k < NC; ++k) e[k] = eight_products<T>(of[k], df[n][k]);
+      float s = NC == 4 ? (e[0] + e[NC / 2]) + (e[NC > 1 ? 1 : 0] + e[NC - 1]) : NC == 2 ? e[0] + e[NC - 1] : e[0];
+      s += __shfl_xor(s, 32, 64);
+      s += __shfl_xor(s, 16, 64);
+      delta[n] = s;
+      if (g == 0 && i < a.tq) p.delta[r] = s;
+    }
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -1067,6 +1083,7 @@ __global__ __launch_bounds__(256) void k_cross_sum(CrossP p) {
     const int kh = x / (2 * a.head_dim), which = x / a.head_dim & 1, d = x % a.head_dim;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (i < keys_of(a, c))
+#pragma unroll 8
       for (int k = 0; k < p.splits; ++k) s += *reinterpret_cast<const f32x4 *>(p.part + k * total + e);
     T *dst = (T *)(which ? p.dv : p.dk) + c * a.kv_bs + (int64_t)i * a.kv_rs + kh * a.head_dim + d;
     if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4 *>(dst) = s;
@@ -1158,7 +1175,7 @@ hipError_t gradient(CrossP p, const CrossGradArgs &b, hipStream_t s) {
   hipError_t e = hipSuccess;
   constexpr size_t lds = tile_bytes<T, DH>();
   const bool wide = sizeof(T) == 2 && x32::takes(a);
-  if (!wide || !b.dq) {
+  if (!b.dq) {
     hipLaunchKernelGGL((k_cross_delta<T>), dim3((unsigned)std::min<int64_t>((rows * (a.head_dim / 8) + 255) / 256, 1 << 16)), dim3(256), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
