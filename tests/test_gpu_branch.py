@@ -698,3 +698,90 @@ def test_branch_on_another_stream():
     side.synchronize()
     for name, t in a.results().items():
         assert torch.equal(t, want[name]), name
+
+
+# ------------------------------------------------------------------------------------- offsets past 32 bits
+def room(elements, dtype=torch.bfloat16):
+    return torch.zeros(elements, dtype=dtype, device="cuda")
+
+
+def test_layer_norm_past_32_bits():
+    """The last rows of 2^31 elements and more have the bits that they have alone."""
+    d, tail = 4104, 3
+    m = (1 << 31) // d + 5
+    g = gen(41)
+    rows, dy, w = normal(g, tail, d).cuda(), normal(g, tail, d, dtype=torch.bfloat16).cuda(), normal(g, 1, d).cuda()
+    x, out = room(m * d, torch.float32).view(m, d), room(m * d).view(m, d)
+    x[-tail:] = rows
+    mean, rstd = torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+    fb.flashbon_op_layer_norm(fb.BF16, m, d, 1e-6, x, out, weight=w, mean=mean, rstd=rstd)
+    alone, mu, rs = torch.empty(tail, d, dtype=torch.bfloat16, device="cuda"), torch.empty(tail, device="cuda"), torch.empty(tail, device="cuda")
+    fb.flashbon_op_layer_norm(fb.BF16, tail, d, 1e-6, rows, alone, weight=w, mean=mu, rstd=rs)
+    assert torch.equal(out[-tail:], alone) and torch.equal(mean[-tail:], mu) and torch.equal(rstd[-tail:], rs)
+    out.zero_()
+    out[-tail:] = dy
+    dx, one = room(m * d, torch.float32).view(m, d), torch.empty(tail, d, device="cuda")
+    fb.flashbon_op_layer_norm_grad(fb.BF16, m, d, x, mean, rstd, out, dx, weight=w)
+    fb.flashbon_op_layer_norm_grad(fb.BF16, tail, d, rows, mu, rs, dy, one, weight=w)
+    assert torch.equal(dx[-tail:], one) and not dx[:-tail].any()
+
+
+@pytest.mark.parametrize("dh,tq,tk", [(128, 70, 70), (128, 2, 300), (32, 70, 20)])
+def test_cross_attention_past_32_bits(dh, tq, tk):
+    """Batch rows and prompts 2^31 elements apart: the bits of a call on dense buffers."""
+    q, kv, _, dout = cross_inputs("bf16", 2, 1, 1, dh, tq, tk, 2, [tk, tk - 1], 42)
+    kv = clean(kv, [tk, tk - 1])
+    far = (1 << 31) + 64
+    sizes, i32 = (fb.BF16, 2, 1, 1, dh, tq, tk), lambda t: torch.tensor(t, dtype=torch.int32, device="cuda")  # noqa: E731
+    index, lengths = i32([1, 0]), i32([tk, tk - 1])
+    dense = [t.contiguous().cuda() for t in (q[:, :, 0], kv[:, :, 0, 0], kv[:, :, 1, 0], dout[:, :, 0])]
+
+    def spread(t):
+        n, rows, _ = t.shape
+        view = room(far + rows * dh).as_strided((n, rows, dh), (far, dh, 1))
+        view.copy_(t)
+        return view
+
+    def run(tensors, q_bs, kv_bs):
+        qq, kk, vv, dd = tensors
+        # out, dq, dk and dv like the inputs whose strides they have
+        out, dq, dk, dv = (spread(torch.zeros(t.shape, dtype=t.dtype, device="cuda")) if q_bs > 1 << 20 else torch.zeros_like(t) for t in (qq, qq, kk, vv))
+        lse, ws = torch.empty(2, 1, tq, device="cuda"), torch.empty(fb.flashbon_op_cross_attention_workspace(*sizes), dtype=torch.uint8, device="cuda")
+        fb.flashbon_op_cross_attention(*sizes, qq, q_bs, dh, kk, vv, kv_bs, dh, index, 2, lengths, out, q_bs, dh, lse=lse, workspace=ws)
+        ws = torch.empty(fb.flashbon_op_cross_attention_grad_workspace(*sizes, 2), dtype=torch.uint8, device="cuda")
+        fb.flashbon_op_cross_attention_grad(*sizes, qq, q_bs, dh, kk, vv, kv_bs, dh, index, 2, lengths, out, q_bs, dh, lse, dd, dq, dk, dv, workspace=ws)
+        return [t.clone() for t in (out, lse, dq, dk, dv)]
+    want = run(dense, tq * dh, tk * dh)
+    for a, b in zip(run([spread(t) for t in dense], far, far), want):
+        assert torch.equal(a.contiguous(), b)
+
+
+def test_adapters_past_32_bits():
+    """The last rows of outputs (and of inputs) of 2^31 elements have the bits that they have alone."""
+    wide_, rank, tail = 1032, 8, 5
+    m = (1 << 31) // wide_ + 20
+    g = gen(43)
+    down, up = normal(g, 1, rank, 8, dtype=torch.bfloat16).cuda(), normal(g, 1, wide_, rank, dtype=torch.bfloat16).cuda()
+    x, base = room(m * 8).view(m, 8), room(m * wide_).view(m, wide_)
+    x[-tail:], base[-tail:] = normal(g, tail, 8, dtype=torch.bfloat16).cuda(), normal(g, tail, wide_, dtype=torch.bfloat16).cuda()
+    last, u, mid = base[-tail:].clone(), torch.empty(m, rank, device="cuda"), torch.empty(tail, rank, device="cuda")
+    alone = torch.empty_like(last)
+    fb.flashbon_op_adapters(fb.BF16, tail, wide_, 8, rank, 1, x[-tail:].contiguous(), down, up, None, None, tail, fb.EPI_STORE, last, alone, mid)
+    fb.flashbon_op_adapters(fb.BF16, m, wide_, 8, rank, 1, x, down, up, None, None, 1000, fb.EPI_STORE, base, base, u)
+    assert torch.equal(base[-tail:], alone) and torch.equal(u[-tail:], mid) and not base[:-tail].any()
+    # the wide side as the input: dx of x [m][1032], dy [m][8]
+    down, up = up.transpose(1, 2).contiguous(), normal(g, 1, 8, rank, dtype=torch.bfloat16).cuda()
+    dd, du = torch.empty(1, rank, wide_, device="cuda"), torch.empty(1, 8, rank, device="cuda")
+    sizes = (m, 8, wide_, rank, 1)
+    ws = torch.empty(fb.flashbon_op_adapters_grad_workspace(fb.BF16, *sizes, 1000), dtype=torch.uint8, device="cuda")
+    dx = room(m * wide_).view(m, wide_)
+    fb.flashbon_op_adapters_grad(fb.BF16, *sizes, base, down, up, None, None, 1000, u, x, fb.EPI_STORE, None, dx, dd, du, workspace=ws)
+    one, d1, u1 = torch.empty_like(alone), torch.empty_like(dd), torch.empty_like(du)
+    sizes = (tail, 8, wide_, rank, 1)
+    fb.flashbon_op_adapters_grad(fb.BF16, *sizes, alone, down, up, None, None, tail, mid, x[-tail:].contiguous(), fb.EPI_STORE, None, one, d1, u1,
+                                 workspace=ws)
+    assert torch.equal(dx[-tail:], one) and not dx[:-tail].any()
+    # every other row is zero: the sums are those of the last rows, in another order of
+    # five terms, whose magnitudes stay below sixty-four times the largest sum
+    for a, b in ((dd, d1), (du, u1)):
+        assert float((a - b).abs().max()) <= 5 * 64 * E * float(b.abs().max())
