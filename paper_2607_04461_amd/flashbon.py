@@ -716,12 +716,13 @@ def _rows_of_heads(device: Optional[int], *wanted) -> list:
             continue
         if t.dtype is not dtype:
             raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-        if min(batch_stride, row_stride) < 0 or max(batch_stride, row_stride) >= 1 << 36:
+        if not (0 <= batch_stride < 1 << 36 and 0 <= row_stride < 1 << 36):
             raise ValueError(f"strides of {name} must be in [0, 2^36), got {batch_stride} and {row_stride}")
         need = (n - 1) * batch_stride + (rows - 1) * row_stride + width
-        held = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
-        if held < need:
-            raise ValueError(f"{name} holds {held} elements from its first on, needs {need}")
+        if t.numel() < need or not t.is_contiguous():      # a view of wider rows: what its memory holds from its first element on
+            held = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+            if held < need:
+                raise ValueError(f"{name} holds {held} elements from its first on, needs {need}")
         if device is not None and t.get_device() != device:
             raise ValueError(f"{name} must be on the current device (cuda:{device}), got {t.device}")
         found.append(t.data_ptr())
@@ -786,9 +787,9 @@ def flashbon_op_layer_norm_grad(dtype, M, D, x, mean, rstd, dy, dx=None, *, weig
 
 
 def _cross_tensors(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv, device, rows, vectors) -> list:
-    _int32(batch, heads, kv_heads, head_dim, tq, tk, n_kv)
-    if min(batch, heads, kv_heads, head_dim, tq, tk, n_kv) < 1:
-        raise ValueError("batch, heads, kv_heads, head_dim, tq, tk and n_kv must be at least 1")
+    sizes = (batch, heads, kv_heads, head_dim, tq, tk, n_kv)
+    if min(sizes) < 1 or max(sizes) > 0x7FFFFFFF:
+        raise ValueError(f"batch, heads, kv_heads, head_dim, tq, tk and n_kv must be at least 1 and below 2^31, got {sizes}")
     return _rows_of_heads(device, *rows) + _pointers(device, *vectors)
 
 
