@@ -15,7 +15,7 @@
 // bf16 of head dim 128 with more than 64 queries runs forward on k_attn_fa (attention.hip).
 // Bound by the matrix cores for many queries, by the reading of k and v for few: then ranges of keys go to several
 // workgroups and k_cross_join joins them (one query of 40 heads to 4001 keys: 18 us and 4, 82 MB at 4.5 TB/s).  fp32, 4 x 12
-// heads of 1560 x 512, head dim 128: forward 211 us (93 TFLOP/s of 154), gradient 741.
+// heads of 1560 x 512, head dim 128: forward 189 us (104 TFLOP/s of 154), gradient 635.
 #include <algorithm>
 
 #include "fragments.h"
@@ -119,8 +119,11 @@ __device__ __forceinline__ bool unit_of(const CrossP &p, int id, int &b, int &h,
 
 template <typename T> constexpr int TILE = sizeof(T) == 2 ? 64 : 32;    // rows of a tile in LDS
 
+// Two waves a SIMD are asked for in all three kernels, which also keeps their accumulators out of the accumulation registers:
+// fp32, the sizes above, forward 211 -> 189 us, gradient 747 -> 635 (k_cross_dkv had 307 registers, one wave a SIMD).
+// k_cross_dkv for bf16 of head dim 128 keeps one: 487 registers would spill.
 template <typename T, int DH, int NQ, bool SPLIT>
-__global__ __launch_bounds__(256) void k_cross(CrossP p) {
+__global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
   constexpr int KT = TILE<T>, NS = KT / 16, NC = DH / 32, ND = DH / 16;
   // 16 queries a wave are bound by the reading of k and v, and small heads by the scores: there P goes in two parts
   constexpr int PARTS = sizeof(T) == 2 && (NQ == 1 || DH == 32) ? 2 : 1;
@@ -342,7 +345,7 @@ __global__ __launch_bounds__(256) void k_cross_delta(CrossP p) {
 }
 
 template <typename T, int DH, int NQ>
-__global__ __launch_bounds__(256) void k_cross_dq(CrossP p) {
+__global__ __launch_bounds__(256, 2) void k_cross_dq(CrossP p) {
   constexpr int KT = TILE<T>, NS = KT / 16, NC = DH / 32, ND = DH / 16;
   typedef Stage<T, KT, DH, 256> St;
   extern __shared__ __attribute__((aligned(16))) char s_mem[];
@@ -472,7 +475,7 @@ __device__ __forceinline__ void list_candidates(const CrossArgs &a, int c, int *
 
 // Keys [128 kb ...) of a prompt's key head against a range of the (candidate, head, query tile) triples that read them.
 template <typename T, int DH, int NK>
-__global__ __launch_bounds__(256, 1) void k_cross_dkv(CrossP p) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 && DH == 128 ? 1 : 2) void k_cross_dkv(CrossP p) {
   constexpr int QT = TILE<T>, NS = QT / 16, NC = DH / 32, ND = DH / 16, KB = 64 * NK;
   typedef Stage<T, QT, DH, 256> St;
   extern __shared__ __attribute__((aligned(16))) char s_mem[];
