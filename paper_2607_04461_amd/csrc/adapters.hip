@@ -461,11 +461,14 @@ struct OuterArgs {
 constexpr int OUTER_COLS = 256, OUTER_CHUNK = 1024;   // columns of a workgroup; most rows of a chunk
 
 template <typename T, int RT>
-__global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
+__global__ __launch_bounds__(256, 2) void k_outer(OuterArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 1 : 3;
   constexpr int XP = OUTER_COLS + 16 / sizeof(T), UP = 32 + 16 / sizeof(T);   // pitches, elements
   constexpr int PIECE = 16 / sizeof(T);                                       // elements of a 16-byte load
-  constexpr int XN = 32 * OUTER_COLS / PIECE / 256, UN = (32 * 4 * RT + 255) / 256;
+  // u's rows go to LDS the other way round, two rows of a rank a write and sixteen lanes beside each other, so that a write
+  // meets no bank twice (a row of u across the lanes: 24960 rows, 1536 to 1536, rank 128, bf16: the call 407 us for 330)
+  typedef T Two __attribute__((ext_vector_type(2)));
+  constexpr int XN = 32 * OUTER_COLS / PIECE / 256, UN = (64 * RT + 255) / 256;
   extern __shared__ __attribute__((aligned(16))) char s_mem[];
   T *sx = reinterpret_cast<T *>(s_mem), *su = sx + 32 * XP;                   // [32][XP], [PARTS][16 RT][UP]
   int32_t *rows = reinterpret_cast<int32_t *>(su + PARTS * 16 * RT * UP);     // [chunk]
@@ -481,7 +484,7 @@ __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
   int steps = a.chunk / 32;
   while (steps > 1 && rows[32 * (steps - 1)] < 0) --steps;     // lists end within a chunk
   u32x4 xv[XN];
-  f32x4 uv[UN];
+  f32x4 uv[UN][2];
   auto load = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < XN; ++i) {
@@ -490,8 +493,12 @@ __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < UN; ++i) {
-      const int p = tid + 256 * i, r = 4 * (p % (4 * RT)), m = p < 128 * RT ? rows[32 * s + p / (4 * RT)] : -1;
-      uv[i] = m >= 0 && r < a.rank ? *reinterpret_cast<const f32x4 *>(U + (int64_t)m * a.rank + r) : f32x4{0.f, 0.f, 0.f, 0.f};
+      const int p = tid + 256 * i, r = 4 * (p / 16);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int m = r < a.rank ? rows[32 * s + 2 * (p % 16) + y] : -1;
+        uv[i][y] = m >= 0 ? *reinterpret_cast<const f32x4 *>(U + (int64_t)m * a.rank + r) : f32x4{0.f, 0.f, 0.f, 0.f};
+      }
     }
   };
   auto land = [&]() __attribute__((always_inline)) {
@@ -502,15 +509,16 @@ __global__ __launch_bounds__(256) void k_outer(OuterArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < UN; ++i) {
-      const int p = tid + 256 * i, m = p / (4 * RT), r = 4 * (p % (4 * RT));
-      if (p >= 128 * RT) break;
+      const int p = tid + 256 * i, m = 2 * (p % 16), r = 4 * (p / 16);
+      if (p >= 64 * RT) break;
 #pragma unroll
       for (int k = 0; k < PARTS; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const T v = from_f32<T>(uv[i][e]);
-          su[(k * 16 * RT + r + e) * UP + m] = v;
-          uv[i][e] = rest(uv[i][e], to_f32(v));
+          const Two v = {from_f32<T>(uv[i][0][e]), from_f32<T>(uv[i][1][e])};
+          *reinterpret_cast<Two *>(su + (k * 16 * RT + r + e) * UP + m) = v;
+#pragma unroll
+          for (int y = 0; y < 2; ++y) uv[i][y][e] = rest(uv[i][y][e], to_f32(v[y]));
         }
     }
   };
