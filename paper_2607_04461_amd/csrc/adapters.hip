@@ -216,14 +216,13 @@ struct UpArgs {
 template <typename T, typename O> constexpr int PARTS = sizeof(T) == 4 ? 1 : sizeof(O) == 4 ? 3 : 2;
 
 // out = base + f u up^T for a tile's rows and the columns [from, to), 256 bytes of a row a turn from wave `first` of `waves` on.
-// uf: the parts of u, row li of each sixteen.  The products cross s_out, which only this wave uses, so that base and out pass
+// u(i, c, p): part p of u, row li of sixteen i, ranks 32 c + 8 g and on.  The products cross s_out, which only this wave uses, so that base and out pass
 // as 256 bytes of four rows at a time: in the products' own layout, 64 bytes of sixteen, 24960 x 1536 took 50 us for 38.
 template <typename O> constexpr int TURN = 256 / sizeof(O);
 template <typename O> constexpr int OUT_PITCH = TURN<O> + 4;
 template <typename O> constexpr size_t OUT_BYTES = 16 * OUT_PITCH<O> * 4;      // of a wave
-template <typename T, typename O, int MT, int RK>
-__device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, const Frag<T> (&uf)[MT][RK][PARTS<T, O>], float *s_out,
-                                           int from, int to, int first, int waves) {
+template <typename T, typename O, int MT, int RK, typename U>
+__device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, const U &u, float *s_out, int from, int to, int first, int waves) {
   constexpr int E = 16 / sizeof(O), Q = TURN<O> / 32;        // elements of a lane's piece; groups of 32 columns
   typedef O Piece __attribute__((ext_vector_type(E)));
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
@@ -265,9 +264,11 @@ __device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, const
 #pragma unroll
           for (int p = PARTS<T, O> - 1; p >= 0; --p)     // the small parts first
 #pragma unroll
-            for (int c = 0; c < RK; ++c)
+            for (int c = 0; c < RK; ++c) {
+              const Frag<T> uf = u(i, c, p);
 #pragma unroll
-              for (int h = 0; h < 2; ++h) acc[h] = mma(wf[q][h][c], uf[i][c][p], acc[h]);
+              for (int h = 0; h < 2; ++h) acc[h] = mma(wf[q][h][c], uf, acc[h]);
+            }
 #pragma unroll
           for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4 *>(s_out + li * OUT_PITCH<O> + 32 * q + 8 * g + 4 * h) = acc[h];
         }
@@ -307,12 +308,21 @@ __global__ __launch_bounds__(256) void k_up(UpArgs a) {
       split<T, PARTS<T, O>>(r < a.rank ? load_frag(a.u + t.row(min(16 * i + li, t.rows - 1)) * a.rank + r) : zero_frag<float>(), uf[i][c]);
     }
   const int from = blockIdx.x % a.parts * a.cols;
-  up_columns<T, O, MT, RK>(a, t, uf, s_part + w * (OUT_BYTES<O> / 4), from, min(from + a.cols, a.N), w, 4);
+  auto u = [&](int i, int c, int p) __attribute__((always_inline)) { return uf[i][c][p]; };
+  up_columns<T, O, MT, RK>(a, t, u, s_part + w * (OUT_BYTES<O> / 4), from, min(from + a.cols, a.N), w, 4);
 }
 
-template <typename O, int MT, int RT> constexpr size_t both_lds() {
+// Whether u's parts stay in LDS for the second product: 32 rows of 128 ranks leave no registers for them beside the weights'.
+// 24960 rows, rank 128, bf16: 8960 to 1536 435 us and 1536 to 8960 462; with the parts in registers 487 and 659 (spilled), in
+// tiles of 16 rows 650 and 638.
+template <int MT, int RT> constexpr bool LDS_PARTS = MT * RT > 8;
+constexpr int PART_PITCH = 128 + 8;
+template <typename T, typename O, int MT, int RT> constexpr size_t u_bytes() {
+  return LDS_PARTS<MT, RT> ? PARTS<T, O> * 16 * MT * PART_PITCH * sizeof(T) : 16 * MT * ((RT < 2 ? 32 : 16 * RT) + 4) * 4;
+}
+template <typename T, typename O, int MT, int RT> constexpr size_t both_lds() {
   const size_t shares = WAVES * MT * RT * 1024, outs = WAVES * OUT_BYTES<O>;
-  return (shares > outs ? shares : outs) + 16 * MT * ((RT < 2 ? 32 : 16 * RT) + 4) * 4;
+  return (shares > outs ? shares : outs) + u_bytes<T, O, MT, RT>();
 }
 
 // Both in one launch: u's tile stays in LDS.  d.u, its scales and the sums' order as in k_down, so the bits are the same.
@@ -321,17 +331,19 @@ __global__ __launch_bounds__(64 * WAVES) void k_both(DownArgs d, UpArgs a) {
   constexpr int RK = RT < 2 ? 1 : RT / 2, PITCH = 32 * RK + 4;
   extern __shared__ __attribute__((aligned(16))) float s_part[];
   // u's tile [16 MT][PITCH], zero past the rank, behind the larger of the shares and the waves' products
-  float *su = s_part + (both_lds<O, MT, RT>() / 4 - 16 * MT * PITCH);
+  float *su = s_part + (both_lds<T, O, MT, RT>() - u_bytes<T, O, MT, RT>()) / 4;
+  T *sp = reinterpret_cast<T *>(su);       // or its parts [PARTS][16 MT][PART_PITCH]
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4;
   const Tile t = tile_of<16 * MT, GATHER>(blockIdx.x, a.M, a.per, a.index, a.count);
   if (t.rows <= 0) return;
   const int ad = t.ad;
-  Frag<T> uf[MT][RK][PARTS<T, O>];
+  constexpr bool LDS = LDS_PARTS<MT, RT>;
+  Frag<T> uf[LDS ? 1 : MT][RK][PARTS<T, O>];
   if (ad < 0) {
     for (int i = threadIdx.x; i < t.rows * a.rank; i += 64 * WAVES) d.u[t.row(i / a.rank) * a.rank + i % a.rank] = 0.f;
     if (a.base == a.out) return;
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int i = 0; i < (LDS ? 1 : MT); ++i)
 #pragma unroll
       for (int c = 0; c < RK; ++c)
 #pragma unroll
@@ -344,18 +356,34 @@ __global__ __launch_bounds__(64 * WAVES) void k_both(DownArgs d, UpArgs a) {
       int row, r;
       const float v = down_sum<MT, RT>(s_part, p, row, r) * scale;
       if (row < t.rows && r < a.rank) d.u[t.row(row) * a.rank + r] = v;
-      su[row * PITCH + r] = r < a.rank ? v : 0.f;
-      if (RT == 1) su[row * PITCH + r + 16] = 0.f;
+      if constexpr (LDS) {
+        float left = r < a.rank ? v : 0.f;
+#pragma unroll
+        for (int k = 0; k < PARTS<T, O>; ++k) {
+          const T part = from_f32<T>(left);
+          sp[(k * 16 * MT + row) * PART_PITCH + r] = part;
+          left = rest(left, to_f32(part));
+        }
+      } else {
+        su[row * PITCH + r] = r < a.rank ? v : 0.f;
+        if (RT == 1) su[row * PITCH + r + 16] = 0.f;
+      }
     }
     __syncthreads();
+    if constexpr (!LDS) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int c = 0; c < RK; ++c) split<T, PARTS<T, O>>(load_frag(su + (16 * i + li) * PITCH + 32 * c + 8 * g), uf[i][c]);
+        for (int c = 0; c < RK; ++c) split<T, PARTS<T, O>>(load_frag(su + (16 * i + li) * PITCH + 32 * c + 8 * g), uf[i][c]);
+    }
   }
   // u's tile has been read; the shares' place serves the products
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  up_columns<T, O, MT, RK>(a, t, uf, s_part + w * (OUT_BYTES<O> / 4), 0, a.N, w, WAVES);
+  auto u = [&](int i, int c, int p) __attribute__((always_inline)) {
+    if constexpr (LDS) return load_frag(sp + (p * 16 * MT + 16 * i + li) * PART_PITCH + 32 * c + 8 * g);
+    else return uf[i][c][p];
+  };
+  up_columns<T, O, MT, RK>(a, t, u, s_part + w * (OUT_BYTES<O> / 4), 0, a.N, w, WAVES);
 }
 
 // What the gradient needs first, in one launch of [blocks][2 count + count]: the transposed weights, out[z][c][r] =
@@ -661,7 +689,7 @@ hipError_t launch_up(const UpArgs &a, hipStream_t s) {
 
 template <typename T, typename O, int MT, int RT, bool GATHER = false>
 hipError_t both_tile(const DownArgs &d, const UpArgs &a, hipStream_t s) {
-  constexpr size_t lds = both_lds<O, MT, RT>();
+  constexpr size_t lds = both_lds<T, O, MT, RT>();
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute((const void *)k_both<T, O, MT, RT, GATHER>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
@@ -685,9 +713,12 @@ hipError_t launch_both(const DownArgs &d, const UpArgs &a, hipStream_t s) {
   if (gather) return a.rank <= 16 ? both_tile<T, O, 1, 1, true>(d, a, s) : both_tile<T, O, 1, 2, true>(d, a, s);
   if (a.rank <= 16) return mt == 2 ? both_tile<T, O, 2, 1>(d, a, s) : both_tile<T, O, 1, 1>(d, a, s);
   if (a.rank <= 32) return mt == 2 ? both_tile<T, O, 2, 2>(d, a, s) : both_tile<T, O, 1, 2>(d, a, s);
-  if constexpr (sizeof(T) == 4) return both_tile<T, O, 1, 4>(d, a, s);
-  if (a.rank <= 64) return mt == 2 ? both_tile<T, O, 2, 4>(d, a, s) : both_tile<T, O, 1, 4>(d, a, s);
-  return both_tile<T, O, 1, 8>(d, a, s);
+  if constexpr (sizeof(T) == 4) {
+    return both_tile<T, O, 1, 4>(d, a, s);
+  } else {
+    if (a.rank <= 64) return mt == 2 ? both_tile<T, O, 2, 4>(d, a, s) : both_tile<T, O, 1, 4>(d, a, s);
+    return mt == 2 ? both_tile<T, O, 2, 8>(d, a, s) : both_tile<T, O, 1, 8>(d, a, s);
+  }
 }
 
 template <typename T, int RT>

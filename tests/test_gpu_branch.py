@@ -524,6 +524,14 @@ def test_adapters_grad(dtype, epi, shape):
     assert torch.equal(inplace, dx) and torch.equal(parts[0], dd) and torch.equal(parts[1], du)
 
 
+@pytest.mark.parametrize("dtype,epi", [("bf16", "store"), ("bf16", "f32"), ("fp32", "store")])
+@pytest.mark.parametrize("shape", [(8300, 136, 72, 128, 3, 997), (8250, 1160, 1096, 104, 2, 1031), (8300, 264, 1032, 64, 3, 8300)], ids=str)
+def test_adapters_of_many_rows(dtype, epi, shape):
+    """Enough rows that a workgroup takes 32 of them."""
+    test_adapters(dtype, epi, shape)
+    test_adapters_grad(dtype, epi, shape)
+
+
 def test_adapters_without_tables():
     x, down, up, _, _, _ = adapter_inputs("bf16", 50, 64, 48, 16, 1, 50, 23)
     a, b = (torch.empty(50, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
