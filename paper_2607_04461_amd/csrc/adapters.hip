@@ -293,8 +293,9 @@ __device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, const
   }
 }
 
+// Two waves a SIMD, but where that spills (919 rows, 1536 to 8960, rank 128, bf16 with an fp32 result: the call 48 us, for 44).
 template <typename T, typename O, int MT, int RK, bool GATHER>
-__global__ __launch_bounds__(256) void k_up(UpArgs a) {
+__global__ __launch_bounds__(256, MT * RK < 8 || (PARTS<T, O>) == 3 ? 2 : 1) void k_up(UpArgs a) {
   extern __shared__ __attribute__((aligned(16))) float s_part[];
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Tile t = tile_of<16 * MT, GATHER>(blockIdx.x / a.parts, a.M, a.per, a.index, a.count);      // a row's workgroups follow each other
