@@ -2,8 +2,8 @@
 // tokens, `per` of them), each group with an adapter a of its own or none:
 //   u = x down_a^T,   out = base + gate s_a u up_a^T
 //   du = s_a dy up_a,   dx = base + du down_a,   d_down_a = sum_m du^T x,   d_up_a = s_a sum_m dy^T u
-// A projection adds 2 r flops to each element it reads and writes, so with r <= 128 all of it is bound by memory: by HBM
-// for many rows, by the latency of its launches for few.  The kernels carry both directions:
+// A projection adds 2 r flops to each element it reads and writes, so all of it is bound by memory: by HBM for many rows (at
+// r = 128 by the weights' way out of L2), by the latency of its launches for few.  The kernels carry both directions:
 //   * k_both: a tile of rows of one adapter through both products.  x goes straight from memory to the matrix cores, every
 //     eighth block of columns on each of eight waves, whose sums meet in LDS; u's tile stays there for the second product.
 //     24960 rows, 1536 to 1536, rank 32, bf16: 59 us, 3.7 TB/s (as k_down and k_up 75, most of it rows in 64-byte pieces).
