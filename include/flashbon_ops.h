@@ -177,7 +177,8 @@ flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, f
  * 1 / sqrt(biased variance + eps) of the row, g = m / rows_per_group; f = weight, or 1 + weight where `modulated` (adaLN).
  * x: device fp32 [M][D]; weight, bias: device fp32 [ceil(M / rows_per_group)][D], each may be NULL (f = 1, bias = 0); out:
  * device act [M][D]; mean, rstd: device fp32 [M] or NULL (the mean is taken off in more bits than the saved one has).
- * rows_per_group >= 1; M shares one weight at rows_per_group >= M.  A row's bits do not depend on the other rows.  Outputs
+ * rows_per_group >= 1; M shares one weight at rows_per_group >= M.  A row's bits do not depend on the other rows.  Rows of any
+ * finite values; of a deviation past 2^126 the saved rstd lies below fp32's normal numbers and has fewer bits.  Outputs
  * must not overlap an input or each other (FLASHBON_EINVAL).  eps positive and finite.  M >= 1, 1 <= D <= 6144.  Addresses
  * need no more alignment than their elements; 16 bytes and D % 4 == 0 are fastest. */
 flashbon_status flashbon_op_layer_norm(int32_t dtype, int32_t M, int32_t D, float eps, const float *x, int32_t rows_per_group,

@@ -5,7 +5,8 @@
 // Both are bound by HBM: every row is read once and held in registers between its reductions, by one wave up to
 // 2048 elements and by four beyond (16384 x 5120 to bf16 97 us, 5.2 TB/s; the gradient of 24960 x 1536 with the residual
 // stream's 113 us and 4 for the vectors' sums, 4.8 TB/s).  The mean is summed in 64 bits (a few per cent of the time a row's bytes take)
-// and taken off in two parts, so that rows far from zero keep their digits; the other sums are fp32.
+// and taken off in two parts, so that rows far from zero keep their digits; the other sums are fp32.  Where the variance
+// and eps leave fp32's normal numbers (a deviation past 2^64, or eps below 2^-126), the row is formed anew in 64 bits.
 // The gradient of the vectors is a sum over thousands of rows: a workgroup adds up a chunk of rows of one group in
 // registers, and a second launch adds the chunks' sums in order, in 64 bits.  No atomics: a call's bits are always
 // the same.  A chunk is what gives four workgroups a CU (more rows: fewer partial sums, but an uneven last round).
@@ -85,7 +86,7 @@ __device__ __forceinline__ double wave_sum64(double v) {
 template <typename T, int WPR, int NC, bool VEC>
 __global__ __launch_bounds__(THREADS) void k_layer_norm(LayerNormArgs a) {
   using R = Row<64 * WPR, NC, VEC>;
-  __shared__ double s_sum[4];
+  __shared__ double s_sum[4], s_wide[4];
   __shared__ float s_sq[4];
   const int w = threadIdx.x >> 6, t = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
   constexpr int ROWS = 4 / WPR;
@@ -115,13 +116,32 @@ __global__ __launch_bounds__(THREADS) void k_layer_norm(LayerNormArgs a) {
       __syncthreads();
       sq = (s_sq[0] + s_sq[1]) + (s_sq[2] + s_sq[3]);
     }
-    const float rstd = 1.0f / sqrtf(sq / (float)a.D + a.eps);
+    const float var = sq / (float)a.D + a.eps;
+    float rstd = 1.0f / sqrtf(var), by = rstd;
+    if (!(var >= 0x1p-126f && var < INFINITY)) {      // every wave of the row alike
+      R::load(v, a.x + m * a.D, t, a.D);
+      double wide = 0;
+      R::each(t, a.D, [&](int i, int, bool in) {
+        const double c = in ? (double)v[i] - mean : 0.0;
+        wide = fma(c, c, wide);
+      });
+      wide = wave_sum64(wide);
+      if constexpr (WPR > 1) {      // apart from s_sum: the next row writes that before a barrier
+        if ((threadIdx.x & 63) == 0) s_wide[w] = wide;
+        __syncthreads();
+        wide = (s_wide[0] + s_wide[1]) + (s_wide[2] + s_wide[3]);
+      }
+      const double r = 1.0 / sqrt(wide / a.D + (double)a.eps);
+      R::each(t, a.D, [&](int i, int, bool in) { v[i] = in ? (float)(((double)v[i] - mean) * r) : 0.f; });
+      rstd = (float)r;
+      by = 1.f;
+    }
     const int64_t group = m / a.per;
     float f[4 * NC], b[4 * NC];
     R::load(f, a.weight ? a.weight + group * a.D : nullptr, t, a.D, 1.f - a.offset);
     R::load(b, a.bias ? a.bias + group * a.D : nullptr, t, a.D);
 #pragma unroll
-    for (int i = 0; i < 4 * NC; ++i) v[i] = fmaf(v[i] * rstd, f[i] + a.offset, b[i]);
+    for (int i = 0; i < 4 * NC; ++i) v[i] = fmaf(v[i] * by, f[i] + a.offset, b[i]);
     R::store((T *)a.out + m * a.D, v, t, a.D);
     if (t == 0) {
       if (a.mean) a.mean[m] = hi;
