@@ -150,6 +150,9 @@ __global__ __launch_bounds__(THREADS) void k_layer_norm(LayerNormArgs a) {
   }
 }
 
+// A saved mean is off by half a step of fp32, a shift that the whole row's xhat would share: rows of a mean of more than 256
+// deviations take off what it left too.  Rows of a deviation past 2^120 are taken in units of 2^16, since x - mean may be
+// past fp32's range.
 // One chunk of rows of one group: dx of its rows, and its share of dweight and dbias, to the chunk's row of `partial`
 // ([chunks][2][D]), or straight to the group's where a group is one chunk.
 // Two waves a SIMD: without asking, rows of 1537 to 2048 took 258 to 278 registers and one wave (8192 x 2048, bf16: 62 us for 58).
@@ -158,6 +161,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_layer_norm_grad(LayerNormGradArg
   using R = Row<64 * WPR, NC, VEC>;
   extern __shared__ float s_acc[];       // WPR 1: [2][256 NC] for the four waves' sums
   __shared__ float s_red[2][4][2];
+  __shared__ double s_rest[4];
   const int w = threadIdx.x >> 6, t = WPR == 1 ? threadIdx.x & 63 : threadIdx.x, D = a.D;
   const int64_t group = blockIdx.x / a.chunks;
   const int64_t first = group * a.per + (int64_t)(blockIdx.x % a.chunks) * a.rows;
@@ -174,10 +178,28 @@ __global__ __launch_bounds__(THREADS, 2) void k_layer_norm_grad(LayerNormGradArg
     float x[4 * NC], g[4 * NC];
     R::load(x, a.x + m * D, t, D);
     R::load(g, (const T *)a.dy + m * D, t, D);
-    const float mean = a.mean[m], rstd = a.rstd[m];
+    const float rstd = a.rstd[m];
+    float mean = a.mean[m], by = rstd, off = 0.f;
+    if (rstd < 0x1p-120f || fabsf(mean) * rstd > 256.f) {      // every wave of the row alike
+      const float unit = rstd < 0x1p-120f ? 0x1p-16f : 1.f;
+      mean *= unit;
+      by /= unit;
+      double rest = 0;
+      R::each(t, D, [&](int i, int, bool in) {
+        x[i] *= unit;
+        rest += in ? (double)(x[i] - mean) : 0.0;
+      });
+      rest = wave_sum64(rest);
+      if constexpr (WPR > 1) {
+        if ((threadIdx.x & 63) == 0) s_rest[w] = rest;
+        __syncthreads();
+        rest = (s_rest[0] + s_rest[1]) + (s_rest[2] + s_rest[3]);
+      }
+      off = (float)(rest / D) * by;
+    }
     float s1 = 0, s2 = 0;
     R::each(t, D, [&](int i, int, bool in) {
-      x[i] = in ? (x[i] - mean) * rstd : 0.f;
+      x[i] = in ? fmaf(x[i] - mean, by, -off) : 0.f;
       dw[i] = fmaf(g[i], x[i], dw[i]);
       db[i] += g[i];
       g[i] *= f[i];

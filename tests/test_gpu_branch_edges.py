@@ -57,3 +57,44 @@ def test_layer_norm_of_a_tiny_eps(d):
     # a mean below the normal numbers is taken off in parts that are off by 2^-150 at most
     near(rstd, rs, 24 * E * rs, "rstd")
     near(out, y, 40 * E * np.abs(y) + 2.0 ** -48 * np.abs(mu)[:, None] * rs[:, None] + 2.0 ** -149 * rs[:, None], "out")
+
+
+def norm_grad_case(x, dtype, per, modulated, eps=1e-6):
+    """The gradient of rows x from statistics saved in fp32, against that of the mean before its rounding."""
+    m, d = x.shape
+    groups, g = -(-m // per), gen(55)
+    w, dy, res = normal(g, groups, d), normal(g, m, d, dtype=ACT[dtype]), normal(g, m, d)
+    _, mu, rs = branch.layer_norm(x, w, None, per, modulated, eps)
+    mean, rstd = torch.tensor(mu, dtype=torch.float32), torch.tensor(rs, dtype=torch.float32)
+    dx, dw, db = torch.empty(m, d, device="cuda"), torch.empty(groups, d, device="cuda"), torch.empty(groups, d, device="cuda")
+    ws = torch.full((fb.flashbon_op_layer_norm_grad_workspace(m, d, per),), 255, dtype=torch.uint8, device="cuda")
+    fb.flashbon_op_layer_norm_grad(CODE[dtype], m, d, cuda(x), cuda(mean), cuda(rstd), cuda(dy), dx, weight=cuda(w),
+                                   rows_per_group=per, modulated=modulated, residual=cuda(res), dweight=dw, dbias=db, workspace=ws)
+    tx, tw, tb = branch.layer_norm_grad(x, w, per, modulated, mu, wide(rstd), dy.float(), res)
+    xh = np.abs((wide(x) - mu[:, None]) * wide(rstd)[:, None])
+    f = np.abs(wide(w)[np.arange(m) // per] + (1 if modulated else 0))
+    gr, ay = np.abs(wide(dy)) * f, np.abs(wide(dy))
+    n = 24 + 8 + 4           # sums along a row, as in test_layer_norm_grad
+    mean_g, mean_gx = gr.mean(1, keepdims=True), (gr * xh).mean(1, keepdims=True)
+    near(dx, tx, E * (2 * np.abs(tx) + wide(rstd)[:, None] * (6 * gr + (n + 4) * mean_g + xh * (n + 8) * mean_gx)), "dx")
+    rows = [slice(i * per, min(m, (i + 1) * per)) for i in range(groups)]
+    n = 16 + 4 + 4
+    near(dw, tw, n * E * np.stack([(ay * xh)[r].sum(0) for r in rows]), "dweight")
+    near(db, tb, n * E * np.stack([ay[r].sum(0) for r in rows]), "dbias")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [2, 40, 701, 2100, 6143])
+def test_layer_norm_grad_at_the_ends_of_the_range(dtype, d):
+    x = rows_at_the_ends(d)
+    norm_grad_case(x[:3], dtype, 3, False)
+    norm_grad_case(torch.cat([x[1:2], x[:1]]), dtype, 1, True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 701, 1536, 2100, 5120])
+def test_layer_norm_grad_of_rows_far_from_zero(dtype, d):
+    """A mean of 10^4 deviations, saved in fp32, is off by 2^-11 of one, which every element of the row would share."""
+    x = normal(gen(56), 40, d, std=0.5) + 5000.0 + torch.arange(40)[:, None] / 7.0
+    norm_grad_case(x, dtype, 40, False)
+    norm_grad_case(x, dtype, 7, True)
