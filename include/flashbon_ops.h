@@ -202,8 +202,9 @@ size_t flashbon_op_layer_norm_grad_workspace(int32_t M, int32_t D, int32_t rows_
 
 /* Cross-attention to encoder states of their own lengths: as flashbon_op_attention, but the queries of batch row b see only
  * the first kv_len[c] of the tk key rows of c = kv_index[b], and query head h reads key head h / (heads / kv_heads).
- * Key rows at or past kv_len[c] are never read.  A prompt of length 0 gives rows of zeros.  lse (device fp32
- * [batch][heads][tq], or NULL): log sum_j exp(q k_j / sqrt(head_dim)), -infinity for an empty prompt.
+ * Key rows at or past kv_len[c] are never read.  A prompt of length 0 gives rows of zeros, and so do scores that are all
+ * -infinity; a key whose score is counts for nothing.  lse (device fp32 [batch][heads][tq], or NULL): log sum_j
+ * exp(q k_j / sqrt(head_dim)), -infinity for such rows.
  * kv_index: device int32 [batch] or NULL (b; then n_kv = batch), kv_len: device int32 [n_kv] or NULL (tk); their values are
  * clamped into [0, n_kv) and [0, tk].  heads % kv_heads == 0; head_dim one of 8, 16, 32, 64, 128; 1 <= tq, tk <= 2^24;
  * batch heads ceil(tq / 64) < 2^24, n_kv kv_heads <= 65535.  Row i of batch row b is at q + b q_batch_stride + i

@@ -63,9 +63,10 @@ def cross_attention(q, k, v, index=None, lengths=None):
             kh = h * k.shape[2] // heads
             s = q[b, :, h] @ k[c, :n, kh].T / np.sqrt(dh)
             top = s.max(1, keepdims=True)
-            e = np.exp(s - top)
-            out[b, :, h] = e @ v[c, :n, kh] / e.sum(1, keepdims=True)
-            lse[b, h] = top[:, 0] + np.log(e.sum(1))
+            live = ~np.isneginf(top[:, 0])       # a row whose scores are all -infinity is that of an empty prompt
+            e = np.exp(s[live] - top[live])
+            out[b, live, h] = e @ v[c, :n, kh] / e.sum(1, keepdims=True)
+            lse[b, h, live] = top[live, 0] + np.log(e.sum(1))
     return out, lse
 
 
@@ -82,7 +83,7 @@ def cross_attention_grad(q, k, v, out, lse, dout, index=None, lengths=None):
         for h in range(heads):
             kh = h * k.shape[2] // heads
             keys, values, do = k[c, :n, kh], v[c, :n, kh], dout[b, :, h]
-            p = np.exp(q[b, :, h] @ keys.T / np.sqrt(dh) - lse[b, h][:, None])
+            p = np.exp(q[b, :, h] @ keys.T / np.sqrt(dh) - np.where(np.isneginf(lse[b, h]), np.inf, lse[b, h])[:, None])
             ds = p * (do @ values.T - (do * out[b, :, h]).sum(1, keepdims=True)) / np.sqrt(dh)
             dq[b, :, h] = ds @ keys
             dk[c, :n, kh] += ds.T @ q[b, :, h]

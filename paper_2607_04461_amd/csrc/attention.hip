@@ -241,7 +241,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[dt][j] = 0.f;
-  float mrun = -INFINITY, lsum = 0.f, mb = 0.f;
+  // OWN: from the least finite score on, so that a row or a tile whose scores are all -infinity has probabilities 0, not NaN
+  float mrun = OWN ? -3.4028235e38f : -INFINITY, lsum = 0.f, mb = 0.f;
   bf16x8 pp[4];   // probabilities of the current tile, 16 keys per chunk
 
   // one pair of exponentials: keys 8 (c & 1) + i, + 1 of chunk c of the scores sc into pp[c]; the row
@@ -418,7 +419,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
     step(S0{}, F_{}, j, sa, sb);
   }
   const float ltot = lsum + __shfl_xor(lsum, 32, 64);
-  const float inv = 1.0f / ltot;
+  const float inv = OWN && ltot == 0.f ? 0.f : 1.0f / ltot;
   if constexpr (OWN)
     if (p.lse && g == 0 && q0 + li < p.tq)
       p.lse[((int64_t)b * p.heads + h) * p.tq + q0 + li] = (mrun * p.qscale + log2f(ltot)) * 0.6931471805599453f;

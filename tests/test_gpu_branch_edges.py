@@ -98,3 +98,42 @@ def test_layer_norm_grad_of_rows_far_from_zero(dtype, d):
     x = normal(gen(56), 40, d, std=0.5) + 5000.0 + torch.arange(40)[:, None] / 7.0
     norm_grad_case(x, dtype, 40, False)
     norm_grad_case(x, dtype, 7, True)
+
+
+# ------------------------------------------------------------------------------------------------ cross-attention
+#          heads kv dh  tq   tk  the keys before which all count for nothing
+NOTHING = [(2, 1, 16, 70, 90, 70), (2, 2, 32, 3, 40, 33), (2, 2, 64, 100, 200, 130), (4, 2, 128, 70, 70, 64), (2, 2, 128, 129, 200, 129),
+           (2, 1, 128, 70, 700, 640), (1, 1, 128, 2, 900, 512)]
+
+
+def inputs_of_dead_keys(dtype, shape, seed):
+    """Three prompts whose first keys, all keys and every other key have scores of -infinity."""
+    heads, kvh, dh, tq, tk, first = shape
+    lengths = [tk, tk, tk - 1]
+    q, kv, index, dout = base.cross_inputs(dtype, 3, heads, kvh, dh, tq, tk, 3, lengths, seed)
+    q[..., 0] = q[..., 0].abs() + 0.25
+    kv[0, :first, 0, :, 0] = -float("inf")
+    kv[1, :, 0, :, 0] = -float("inf")
+    kv[2, 3::2, 0, :, 0] = -float("inf")
+    return q, kv, index, lengths, dout
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", NOTHING, ids=str)
+def test_cross_attention_of_keys_that_count_for_nothing(dtype, shape):
+    """Keys whose scores are -infinity have probability 0, be they whole tiles, and rows of no other keys are those of an empty
+    prompt, on every path."""
+    tk = shape[4]
+    q, kv, index, lengths, _ = inputs_of_dead_keys(dtype, shape, 57)
+    got, lse = base.cross_call(dtype, q, kv, index, lengths)
+    kv = base.clean(kv, lengths)
+    k, v = kv[:, :, 0], kv[:, :, 1]
+    out, want = branch.cross_attention(wide(q), wide(k), wide(v), index, lengths)
+    row = index.index(1)
+    assert not out[row].any() and np.isneginf(want[row]).all() and np.isfinite(want[index.index(0)]).all()
+    finite = torch.where(torch.isinf(k), torch.zeros_like(k), k)
+    rel = base.p_error(q, finite, index, want)
+    near(lse, want, rel + 8 * E * np.where(np.isfinite(want), np.abs(want), 0), "lse")
+    mass, _ = branch.cross_attention(wide(q), wide(k), np.abs(wide(v)), index, lengths)
+    u = U[ACT[dtype]]
+    near(got, out, u * np.abs(out) + (u + 2 * rel.transpose(0, 2, 1)[..., None] + (tk + 8) * E) * (1 + 2 * u) * mass, "out")
