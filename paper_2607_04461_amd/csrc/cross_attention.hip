@@ -506,9 +506,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DH == 128 ? 1 : 2) void k_cr
   const int64_t u0 = all * split / p.splits, u1 = all * (split + 1) / p.splits;
   St qs, ds;
   float ls = 0.f, de = 0.f;
+  int left = 0;               // queries of the tile loaded last, and what lies past it
   auto load = [&](int64_t u) __attribute__((always_inline)) {
     const int qt = (int)(u % nqt), h = kh * shared + (int)(u / nqt % shared), b = s_list[u / nqt / shared];
     const int64_t i0 = (int64_t)qt * QT;
+    left = a.tq - qt * QT;
     qs.load((const T *)a.q + b * a.q_bs + i0 * a.q_rs + h * a.head_dim, a.q_rs, a.tq - qt * QT, a.head_dim);
     ds.load((const T *)p.dout + b * a.o_bs + i0 * a.o_rs + h * a.head_dim, a.o_rs, a.tq - qt * QT, a.head_dim);
     if (threadIdx.x < QT) {
@@ -528,6 +530,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DH == 128 ? 1 : 2) void k_cr
       s_delta[threadIdx.x] = de;
     }
     __syncthreads();
+    if (left < QT) {          // the last query again in place of rows of zeros, which would meet an infinite key with a NaN
+      for (int e = threadIdx.x; e < (QT - left) * DH; e += 256) sq[(left + e / DH) * St::PITCH + e % DH] = sq[(left - 1) * St::PITCH + e % DH];
+      __syncthreads();
+    }
     if (u + 1 < u1) load(u + 1);
     if (key0 >= len) continue;
 #pragma unroll
@@ -924,8 +930,10 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
   const int q_rs = (int)a.q_rs, o_rs = (int)a.o_rs;
   int qt = (int)(u0 % nqt), hs = (int)(u0 / nqt % shared), bi = (int)(u0 / nqt / shared);   // the triple to load next
   float ls = 0.f, de = 0.f;
+  int left = 0;             // queries of the tile loaded last
   auto load = [&](int buf) __attribute__((always_inline)) {
     const int h = kh * shared + hs, b = __builtin_amdgcn_readfirstlane(s_list[bi]), valid = min(QT, a.tq - qt * QT);
+    left = valid;
     const __amdgpu_buffer_rsrc_t rq = rows_rsrc((const bf16 *)a.q + b * a.q_bs + (int64_t)qt * QT * a.q_rs + h * DH, q_rs, valid, DH);
     const __amdgpu_buffer_rsrc_t rd = rows_rsrc((const bf16 *)p.dout + b * a.o_bs + (int64_t)qt * QT * a.o_rs + h * DH, o_rs, valid, DH);
     const int at = fresh(lane);       // offsets are made anew for each tile: spilled ones would come back behind the loads
@@ -961,6 +969,12 @@ __global__ __launch_bounds__(512) void k_dkv(CrossP p) {
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this tile's rows
     __syncthreads();                      // ... of every wave; the last tile's copies have been read
+    if (left < QT) {          // the last query again in place of rows of zeros, which would meet an infinite key with a NaN
+      char *q = rows + buf * 2 * TILE_B;
+      for (int e = left * NCH + tid; e < QT * NCH; e += 512)
+        *reinterpret_cast<u32x4 *>(q + row_at<DH>(e / NCH, e % NCH)) = *reinterpret_cast<const u32x4 *>(q + row_at<DH>(left - 1, e % NCH));
+      lds_barrier();
+    }
     if (u + 1 < steps) load(buf ^ 1);
     {
       const int br = fresh(block_rows<DH>(dg, qg)), bc = fresh(block_columns(dg, qg));

@@ -137,3 +137,31 @@ def test_cross_attention_of_keys_that_count_for_nothing(dtype, shape):
     mass, _ = branch.cross_attention(wide(q), wide(k), np.abs(wide(v)), index, lengths)
     u = U[ACT[dtype]]
     near(got, out, u * np.abs(out) + (u + 2 * rel.transpose(0, 2, 1)[..., None] + (tk + 8) * E) * (1 + 2 * u) * mass, "out")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", NOTHING, ids=str)
+def test_cross_attention_grad_of_keys_that_count_for_nothing(dtype, shape):
+    """Such keys take no gradient, whatever the number of queries: rows past the last query meet them with zeros."""
+    heads, kvh, dh, tq, tk, first = shape
+    q, kv, index, lengths, dout = inputs_of_dead_keys(dtype, shape, 58)
+    out, lse = base.cross_call(dtype, q, kv, index, lengths)
+    kv = base.clean(kv, lengths)
+    sizes, qs, ks = (CODE[dtype], 3, heads, kvh, dh, tq, tk), (tq * heads * dh, heads * dh), (tk * 2 * kvh * dh, 2 * kvh * dh)
+    dkv, kvd = torch.full_like(kv, 9.0).cuda(), kv.cuda()
+    ws = torch.empty(fb.flashbon_op_cross_attention_grad_workspace(*sizes, 3), dtype=torch.uint8, device="cuda")
+    i32 = lambda t: torch.tensor(t, dtype=torch.int32, device="cuda")  # noqa: E731
+    fb.flashbon_op_cross_attention_grad(*sizes, q.cuda(), *qs, kvd[:, :, 0], kvd[:, :, 1], *ks, i32(index), 3, i32(lengths), out, *qs, lse,
+                                        dout.cuda(), None, dkv[:, :, 0], dkv[:, :, 1], workspace=ws)
+    assert not dkv[0, :first].any() and not dkv[1].any() and not dkv[2, 3::2].any()
+    assert bool(torch.isfinite(dkv).all()) and bool(dkv[0, first:].any()) and bool(dkv[2, :3].any())
+    # the keys that count have the gradient of a prompt of them alone
+    some = torch.arange(tk) % 2 == 0
+    some[:3], some[tk - 1:] = True, False
+    for c, rows in ((0, torch.arange(tk) >= first), (2, some)):
+        b = index.index(c)
+        k1, v1 = (kv[c:c + 1, rows, i] for i in (0, 1))
+        _, tk_, tv = branch.cross_attention_grad(wide(q[b:b + 1]), wide(k1), wide(v1), wide(out[b:b + 1]), wide(lse[b:b + 1]), wide(dout[b:b + 1]))
+        for got, want in ((dkv[c, rows.cuda(), 0], tk_[0]), (dkv[c, rows.cuda(), 1], tv[0])):
+            # P and dS rounded once and results once, and fp32's sums of order 10^3 terms
+            assert np.linalg.norm(wide(got) - want) <= (2 * U[ACT[dtype]] + 1000 * E) * np.linalg.norm(want)
