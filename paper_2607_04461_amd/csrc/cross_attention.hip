@@ -1219,7 +1219,9 @@ hipError_t gradient(CrossP p, const CrossGradArgs &b, hipStream_t s) {
         const int64_t sets = ((int64_t)a.n_kv * a.kv_heads * p.splits + 7) / 8 * 8 * ((a.tk + x32::KEYS - 1) / x32::KEYS);
         const size_t bytes = x32::dkv_lds<DH>() + (a.batch + 1) * 4;
         auto kern = x32::two_parts(a) ? x32::k_dkv<DH, true> : x32::k_dkv<DH, false>;
-        if ((e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes)) != hipSuccess) return e;
+        // the most that any call asks for: the attribute is the process's, and calls of other batches may run beside this one
+        constexpr int most = (int)x32::dkv_lds<DH>() + (CROSS_GRAD_BATCH + 1) * 4;
+        if ((e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, most)) != hipSuccess) return e;
         hipLaunchKernelGGL(kern, dim3((unsigned)sets), dim3(512), bytes, s, p);
       }
     }

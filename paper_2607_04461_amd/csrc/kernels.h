@@ -231,7 +231,8 @@ bool attention_own_takes(const CrossArgs &a);
 hipError_t launch_attention_own(const CrossArgs &a, hipStream_t s);
 size_t cross_attention_workspace(ActType t, const CrossArgs &a);
 hipError_t launch_cross_attention(ActType t, const CrossArgs &a, void *workspace, size_t workspace_bytes, hipStream_t s);
-// dq (as q), dk and dv (as k and v, every row of every prompt written); dq, or dk and dv, may be null.  batch <= 4096.
+// dq (as q), dk and dv (as k and v, every row of every prompt written); dq, or dk and dv, may be null.
+constexpr int CROSS_GRAD_BATCH = 4096;   // the most: a workgroup lists its prompt's batch rows in LDS
 struct CrossGradArgs {
   const void *dout;                 // as out
   void *dq, *dk, *dv;

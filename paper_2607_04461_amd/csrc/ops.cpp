@@ -394,7 +394,7 @@ flashbon_status flashbon_op_cross_attention(int32_t dtype, int32_t batch, int32_
 
 size_t flashbon_op_cross_attention_grad_workspace(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads,
                                                   int32_t head_dim, int32_t tq, int32_t tk, int32_t n_kv) {
-  if (cross_sizes(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv) != FLASHBON_OK || batch > 4096) return 0;
+  if (cross_sizes(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv) != FLASHBON_OK || batch > CROSS_GRAD_BATCH) return 0;
   CrossArgs a{};
   a.batch = batch; a.heads = heads; a.kv_heads = kv_heads; a.head_dim = head_dim; a.tq = tq; a.tk = tk; a.n_kv = n_kv;
   return cross_attention_grad_workspace(dtype == FLASHBON_BF16 ? ACT_BF16 : ACT_F32, a);
@@ -410,7 +410,7 @@ flashbon_status flashbon_op_cross_attention_grad(int32_t dtype, int32_t batch, i
                                                  size_t workspace_bytes, void *stream) {
   const flashbon_status st = cross_sizes(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv);
   if (st != FLASHBON_OK) return st;
-  if (batch > 4096) return fail(FLASHBON_ESHAPE, "batch must be at most 4096");
+  if (batch > CROSS_GRAD_BATCH) return fail(FLASHBON_ESHAPE, "batch must be at most 4096");
   if (!kv_index && n_kv != batch) return fail(FLASHBON_ESHAPE, "n_kv must be batch without kv_index");
   if (!q || !k || !v || !out || !lse || !dout) return fail(FLASHBON_EINVAL, "q, k, v, out, lse and dout are required");
   if ((dk == nullptr) != (dv == nullptr)) return fail(FLASHBON_EINVAL, "dk and dv go together");

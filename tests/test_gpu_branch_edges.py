@@ -2,6 +2,8 @@
 
 Tolerances count roundings as in test_gpu_branch: E is half a step of fp32, U[t] of the type t.
 """
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -165,3 +167,67 @@ def test_cross_attention_grad_of_keys_that_count_for_nothing(dtype, shape):
         for got, want in ((dkv[c, rows.cuda(), 0], tk_[0]), (dkv[c, rows.cuda(), 1], tv[0])):
             # P and dS rounded once and results once, and fp32's sums of order 10^3 terms
             assert np.linalg.norm(wide(got) - want) <= (2 * U[ACT[dtype]] + 1000 * E) * np.linalg.norm(want)
+
+
+# ------------------------------------------------------------------------------------------- two threads at once
+def together(works):
+    """Runs each of the works on a thread and a stream of its own, twenty times."""
+    failed = []
+
+    def run(work):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(20):
+                    work()
+            stream.synchronize()
+        except Exception as e:   # noqa: BLE001 - reported by the test's own thread
+            failed.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=run, args=(w,)) for w in works]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("tq,tk", [(2, 5), (65, 66)])
+def test_cross_attention_grad_of_two_batches_at_once(dh, tq, tk):
+    """The least and the largest batch, whose kernels ask for different amounts of LDS."""
+    works, results = [], []
+    for batch in (1, 4096):
+        q, kv, _, dout = base.cross_inputs("bf16", batch, 1, 1, dh, tq, tk, 1, [tk], 59 + batch)
+        index = torch.zeros(batch, dtype=torch.int32, device="cuda")
+        out, lse = base.cross_call("bf16", q, kv, [0] * batch, [tk])
+        sizes, qs, ks = (fb.BF16, batch, 1, 1, dh, tq, tk), (tq * dh, dh), (tk * 2 * dh, 2 * dh)
+        ws = torch.empty(fb.flashbon_op_cross_attention_grad_workspace(*sizes, 1), dtype=torch.uint8, device="cuda")
+        dq, dkv, q, kv, dout = torch.empty_like(out), torch.empty_like(kv).cuda(), q.cuda(), kv.cuda(), dout.cuda()
+
+        def work(sizes=sizes, qs=qs, ks=ks, q=q, kv=kv, index=index, out=out, lse=lse, dout=dout, dq=dq, dkv=dkv, ws=ws):
+            fb.flashbon_op_cross_attention_grad(*sizes, q, *qs, kv[:, :, 0], kv[:, :, 1], *ks, index, 1, None, out, *qs, lse, dout, dq,
+                                                dkv[:, :, 0], dkv[:, :, 1], workspace=ws)
+        work()
+        works.append(work)
+        results.append((dq, dkv, dq.clone(), dkv.clone()))
+    for dq, dkv, _, _ in results:
+        dq.zero_(), dkv.zero_()
+    together(works)
+    for dq, dkv, a, b in results:
+        assert torch.equal(dq, a) and torch.equal(dkv, b)
+
+
+def test_two_branches_at_once():
+    branches = [base.Branch(61).device(), base.Branch(62, tokens=70, heads=3, dh=128, text=90, rank=48).device()]
+    want = []
+    for b in branches:
+        b.step()
+        want.append(b.results())
+        for name in b.RESULTS:
+            getattr(b, name).zero_()
+    together([b.step for b in branches])
+    for b, w in zip(branches, want):
+        for name, t in b.results().items():
+            assert torch.equal(t, w[name]), name
