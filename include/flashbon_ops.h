@@ -209,7 +209,8 @@ size_t flashbon_op_layer_norm_grad_workspace(int32_t M, int32_t D, int32_t rows_
  * clamped into [0, n_kv) and [0, tk].  heads % kv_heads == 0; head_dim one of 8, 16, 32, 64, 128; 1 <= tq, tk <= 2^24;
  * batch heads ceil(tq / 64) < 2^24, n_kv kv_heads <= 65535.  Row i of batch row b is at q + b q_batch_stride + i
  * q_row_stride + h head_dim, keys, values and out as in flashbon_op_attention.  Every address, and every stride in bytes, is
- * a multiple of 16, strides lie in [0, 2^36), and out's keep its rows apart (FLASHBON_EINVAL).  out and lse must not
+ * a multiple of 16, strides lie in [0, 2^36), and out's keep its rows apart, batch rows behind each other or side by side: the
+ * larger stride passes all that the smaller one reaches (FLASHBON_EINVAL).  out and lse must not
  * overlap the extent of an input or each other (FLASHBON_EINVAL).
  * Few queries (tq heads) to long states run over several ranges of keys at once where a workspace of
  * flashbon_op_cross_attention_workspace bytes is given; without one, or with a smaller one, in one range.  A candidate's
@@ -229,10 +230,10 @@ size_t flashbon_op_cross_attention_workspace(int32_t dtype, int32_t batch, int32
  *   dq = dS k;   dk = dS^T q, dv = P^T dout, summed over the batch rows and the query heads that read the key head.
  * dq (act) has q's strides, dk and dv those of k and v; q's and k's strides must keep their rows apart.  Every row of dk and
  * dv up to tk is written, zeros at or past kv_len[c] and for prompts that no row reads.  The one key of a prompt of length 1
- * has P = 1: dq and dk are 0 there.  dq may be NULL, and so may dk
- * and dv together.  The outputs must not overlap the extent of an input or each other, but rows of dk and dv may alternate
- * as those of fused keys and values do (FLASHBON_EINVAL).  batch <= 4096; sizes and alignment otherwise as above; a
- * workspace of flashbon_op_cross_attention_grad_workspace bytes (FLASHBON_ESHAPE if it is smaller). */
+ * has P = 1: dq and dk are 0 there.  dq may be NULL, and so may dk and dv together.  The outputs must not overlap the extent
+ * of an input or each other, but dk and dv may lie in one buffer as fused keys and values do, their rows apart in the same
+ * sense, with the way from dk to dv as a third stride (FLASHBON_EINVAL).  batch <= 4096; sizes and alignment otherwise as
+ * above; a workspace of flashbon_op_cross_attention_grad_workspace bytes (FLASHBON_ESHAPE if it is smaller). */
 flashbon_status flashbon_op_cross_attention_grad(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads,
                                                  int32_t head_dim, int32_t tq, int32_t tk, const void *q,
                                                  int64_t q_batch_stride, int64_t q_row_stride, const void *k, const void *v,

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <climits>
 #include <cmath>
 #include <cstdlib>
@@ -54,9 +55,24 @@ bool overlaps(std::initializer_list<Span> outputs, std::initializer_list<Span> i
 size_t extent(int64_t n, int64_t batch_stride, int64_t rows, int64_t row_stride, int64_t width, size_t es) {
   return (size_t)((n - 1) * batch_stride + (rows - 1) * row_stride + width) * es;
 }
-// Whether [n][rows] rows of `width` elements share none.
+// Whether rows of `width` elements, one for each place along the dimensions, share none: each dimension's stride passes what
+// those of smaller strides fill.
+struct Dimension {
+  int64_t count, stride;
+};
+template <size_t N> bool apart(std::array<Dimension, N> along, int64_t width) {
+  std::sort(along.begin(), along.end(), [](const Dimension &x, const Dimension &y) { return x.stride < y.stride; });
+  int64_t filled = width;
+  for (const Dimension &d : along) {
+    if (d.count == 1) continue;
+    if (d.stride < filled) return false;
+    filled += (d.count - 1) * d.stride;
+  }
+  return true;
+}
+// [n][rows] rows
 bool apart(int64_t n, int64_t batch_stride, int64_t rows, int64_t row_stride, int64_t width) {
-  return (rows == 1 || row_stride >= width) && (n == 1 || batch_stride >= (rows - 1) * row_stride + width);
+  return apart<2>({{{n, batch_stride}, {rows, row_stride}}}, width);
 }
 bool aligned(std::initializer_list<const void *> addresses) {
   for (const void *p : addresses)
@@ -427,14 +443,11 @@ flashbon_status flashbon_op_cross_attention_grad(int32_t dtype, int32_t batch, i
   const size_t os = extent(batch, out_batch_stride, tq, out_row_stride, wide, es);
   const Span q_in{q, qs}, k_in{k, kv}, v_in{v, kv}, index{kv_index, (size_t)4 * batch}, len{kv_len, (size_t)4 * n_kv}, o_in{out, os},
       lse_in{lse, (size_t)4 * batch * heads * tq}, do_in{dout, os}, dq_out{dq, qs}, dk_out{dk, kv}, dv_out{dv, kv}, ws{workspace, need};
-  // dk and dv may alternate row by row; each of them is held against everything else
+  // dk and dv may share a buffer; each of them is held against everything else
   bool clash = overlaps({dq_out, dk_out, ws}, {q_in, k_in, v_in, index, len, o_in, lse_in, do_in}) ||
                overlaps({dq_out, dv_out, ws}, {q_in, k_in, v_in, index, len, o_in, lse_in, do_in});
-  if (dk && overlap(dk_out, dv_out)) {      // a row of both within a row's stride, and the last one within a prompt's
-    const int64_t row = narrow * es, away = std::abs((int64_t)((intptr_t)dv - (intptr_t)dk)), both = away + row;
-    clash = clash || away < row || (tk > 1 && both > kv_row_stride * es) ||
-            (n_kv > 1 && (tk - 1) * kv_row_stride * es + both > kv_batch_stride * es);
-  }
+  if (dk && overlap(dk_out, dv_out))        // rows of both in one buffer, dv's a third stride from dk's
+    clash = clash || !apart<3>({{{n_kv, kv_batch_stride}, {tk, kv_row_stride}, {2, std::abs((int64_t)((intptr_t)dv - (intptr_t)dk)) / es}}}, narrow);
   if (clash) return fail(FLASHBON_EINVAL, "outputs and workspace must not overlap an input or each other");
   CrossArgs a{};
   a.batch = batch; a.heads = heads; a.kv_heads = kv_heads; a.head_dim = head_dim; a.tq = tq; a.tk = tk; a.n_kv = n_kv;

@@ -1,0 +1,52 @@
+"""Strides that the cross-attention calls take and refuse; the calls here are refused in the end, and no GPU is touched."""
+import pytest
+
+from paper_2607_04461_amd import flashbon as fb
+from test_branch_validation import CROSS, CROSS_GRAD, at
+
+
+def call(name, base, **change):
+    args = dict(base, **change)
+    status = getattr(fb.load(), "flashbon_op_" + name)(*args.values())
+    return status, fb.load().flashbon_last_error().decode()
+
+
+# batch 2, 3 rows of 64
+APART = [(192, 64), (200, 64), (192 + 64, 72), (64, 128), (64, 192), (72, 136)]
+TOGETHER = [(128, 64), (64, 64), (192, 56), (64, 120), (56, 128), (0, 64), (64, 0), (96, 64)]
+
+
+@pytest.mark.parametrize("o_bs,o_rs", APART)
+def test_rows_of_out_apart(o_bs, o_rs):
+    """Batch rows behind each other, or side by side ([tq][batch][width]): refused here for lse alone, which lies on out."""
+    status, why = call("cross_attention", CROSS, o_bs=o_bs, o_rs=o_rs, lse=at(5))
+    assert status == fb.EINVAL and "overlap" in why, why
+
+
+@pytest.mark.parametrize("o_bs,o_rs", TOGETHER)
+def test_rows_of_out_together(o_bs, o_rs):
+    status, why = call("cross_attention", CROSS, o_bs=o_bs, o_rs=o_rs, lse=at(5))
+    assert status == fb.EINVAL and "apart" in why, why
+
+
+@pytest.mark.parametrize("bs,rs", APART)
+def test_rows_of_gradients_apart(bs, rs):
+    """Refused here for the workspace alone."""
+    assert call("cross_attention_grad", CROSS_GRAD, q_bs=bs, q_rs=rs, workspace=None)[0] == fb.ESHAPE
+    # keys of 5 rows of 32, two prompts: rows of both prompts side by side
+    assert call("cross_attention_grad", CROSS_GRAD, kv_bs=32, kv_rs=64, workspace=None)[0] == fb.ESHAPE
+
+
+@pytest.mark.parametrize("bs,rs", TOGETHER)
+def test_rows_of_gradients_together(bs, rs):
+    status, why = call("cross_attention_grad", CROSS_GRAD, q_bs=bs, q_rs=rs, workspace=None)
+    assert status == fb.EINVAL and "apart" in why, why
+
+
+@pytest.mark.parametrize("kv_bs,kv_rs,away", [(32, 120, 64), (32, 128, 32), (64, 128, 16), (64, 120, 32), (160, 32, 32), (160, 32, 128),
+                                              (312, 32, 160), (64, 128, 96)])
+def test_keys_and_values_together(kv_bs, kv_rs, away):
+    """Rows of dk and dv of which some share elements, or with no room between them for the others."""
+    for first, second in ((0, away), (away, 0)):
+        status, why = call("cross_attention_grad", CROSS_GRAD, kv_bs=kv_bs, kv_rs=kv_rs, dk=at(10) + 2 * first, dv=at(10) + 2 * second)
+        assert status == fb.EINVAL and ("apart" in why or "overlap" in why), (status, why)

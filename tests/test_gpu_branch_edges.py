@@ -169,6 +169,58 @@ def test_cross_attention_grad_of_keys_that_count_for_nothing(dtype, shape):
             assert np.linalg.norm(wide(got) - want) <= (2 * U[ACT[dtype]] + 1000 * E) * np.linalg.norm(want)
 
 
+# ------------------------------------------------------------------------------------------------- other layouts
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dh,tq,tk", [(16, 9, 7), (64, 70, 66), (128, 70, 66), (128, 3, 300)])
+@pytest.mark.parametrize("order", [("t", "n", "two"), ("t", "two", "n"), ("n", "two", "t"), ("two", "n", "t")], ids="-".join)
+def test_cross_attention_of_rows_side_by_side(dtype, dh, tq, tk, order):
+    """Queries as [tq][batch][width], keys and values in one buffer in any order of prompts, rows and the two: the bits of
+    dense buffers, and what lies between the rows is left as it was."""
+    batch, heads, kvh, prompts, lengths = 3, 2, 1, 2, [tk, tk - 2]
+    q, kv, index, dout = base.cross_inputs(dtype, batch, heads, kvh, dh, tq, tk, prompts, lengths, 63)
+    kv = base.clean(kv, lengths).cuda()
+    wide_, narrow, pad = heads * dh, kvh * dh, 16
+    i32 = lambda t: torch.tensor(t, dtype=torch.int32, device="cuda")  # noqa: E731
+    sizes = (CODE[dtype], batch, heads, kvh, dh, tq, tk)
+    counts, strides, step = {"n": prompts, "t": tk, "two": 2}, {}, narrow
+    for axis in reversed(order):
+        strides[axis] = step
+        step = step * counts[axis] + pad
+    room = step
+
+    def fused():
+        """A buffer of nines, and a view of it as [prompts][tk][2][narrow]."""
+        flat = torch.full((room,), 9.0, dtype=ACT[dtype], device="cuda")
+        return flat, flat.as_strided((prompts, tk, 2, narrow), (strides["n"], strides["t"], strides["two"], 1))
+
+    def run(side):
+        """Outputs as [batch][tq] and [prompts][tk][2] rows."""
+        qs = (wide_, batch * wide_) if side else (tq * wide_, wide_)
+        rows = lambda t: t.transpose(0, 1).contiguous() if side else t  # noqa: E731
+        qq, dd = (rows(t.flatten(2)).cuda() for t in (q, dout))
+        out, dq = torch.empty_like(qq), torch.empty_like(qq)
+        lse = torch.empty(batch, heads, tq, device="cuda")
+        if side:
+            (flat, keys), (dflat, dkeys), ks = fused(), fused(), (strides["n"], strides["t"])
+            keys.copy_(kv.flatten(3))
+            k, v, dk, dv = flat, flat[strides["two"]:], dflat, dflat[strides["two"]:]
+        else:
+            keys, dkeys, ks = kv.flatten(3), torch.empty_like(kv).flatten(3), (tk * 2 * narrow, 2 * narrow)
+            k, v, dk, dv = keys[:, :, 0], keys[:, :, 1], dkeys[:, :, 0], dkeys[:, :, 1]
+        ws = torch.empty(fb.flashbon_op_cross_attention_workspace(*sizes), dtype=torch.uint8, device="cuda")
+        fb.flashbon_op_cross_attention(*sizes, qq, *qs, k, v, *ks, i32(index), prompts, i32(lengths), out, *qs, lse=lse, workspace=ws)
+        ws = torch.empty(fb.flashbon_op_cross_attention_grad_workspace(*sizes, prompts), dtype=torch.uint8, device="cuda")
+        fb.flashbon_op_cross_attention_grad(*sizes, qq, *qs, k, v, *ks, i32(index), prompts, i32(lengths), out, *qs, lse, dd, dq, dk, dv, workspace=ws)
+        result = [rows(out), lse, rows(dq), dkeys.clone()]
+        if side:
+            dkeys.fill_(9.0)
+            assert bool((dflat == 9.0).all())
+        return result
+
+    for a, b in zip(run(True), run(False)):
+        assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------------------------------------- two threads at once
 def together(works):
     """Runs each of the works on a thread and a stream of its own, twenty times."""
