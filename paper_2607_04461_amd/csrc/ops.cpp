@@ -96,8 +96,9 @@ flashbon_status cross_sizes(int32_t dtype, int32_t batch, int32_t heads, int32_t
     return fail(FLASHBON_ESHAPE, "need batch, heads, kv_heads, n_kv >= 1, heads % kv_heads == 0 and 1 <= tq, tk <= 2^24");
   if (head_dim != 8 && head_dim != 16 && head_dim != 32 && head_dim != 64 && head_dim != 128)
     return fail(FLASHBON_ESHAPE, "head_dim must be one of 8, 16, 32, 64, 128");
-  if ((double)batch * heads * ((tq + 63) / 64) >= 16777216.0 || (int64_t)n_kv * kv_heads > 65535)
-    return fail(FLASHBON_ESHAPE, "need batch heads ceil(tq / 64) < 2^24 and n_kv kv_heads <= 65535");
+  const int64_t pairs = ((int64_t)batch * heads + 7) / 8 * 8;      // as launches take them, in blocks of 256 threads, below 2^32
+  if (pairs >= 1 << 24 || pairs * ((tq + 63) / 64) >= 1 << 24 || (int64_t)n_kv * kv_heads > 65535)
+    return fail(FLASHBON_ESHAPE, "need batch heads (to a multiple of 8) ceil(tq / 64) < 2^24 and n_kv kv_heads <= 65535");
   return FLASHBON_OK;
 }
 

@@ -50,3 +50,15 @@ def test_keys_and_values_together(kv_bs, kv_rs, away):
     for first, second in ((0, away), (away, 0)):
         status, why = call("cross_attention_grad", CROSS_GRAD, kv_bs=kv_bs, kv_rs=kv_rs, dk=at(10) + 2 * first, dv=at(10) + 2 * second)
         assert status == fb.EINVAL and ("apart" in why or "overlap" in why), (status, why)
+
+
+@pytest.mark.parametrize("batch,heads,tq,taken", [(7, 9, 1 << 24, False), (1, (1 << 24) - 1, 64, False), (3, 21, (1 << 24) - 63, False),
+                                                  (8, 8, (1 << 24) - 64, True), (7, 9, (1 << 24) - 64, True), (1, (1 << 24) - 8, 64, True)])
+def test_most_queries(batch, heads, tq, taken):
+    """Launches take the pairs of batch row and head by eights: 2^24 blocks of 64 queries are 2^32 threads, one too many."""
+    wide = heads * 8
+    sizes = dict(batch=batch, heads=heads, kv_heads=1, head_dim=8, tq=tq, tk=1, q_bs=tq * wide, q_rs=wide, o_bs=tq * wide, o_rs=wide, n_kv=1)
+    for name, base in (("cross_attention", CROSS), ("cross_attention_grad", CROSS_GRAD)):
+        status, why = call(name, base, **sizes, out=None)
+        assert status == (fb.EINVAL if taken else fb.ESHAPE), (name, why)       # refused for the missing out, or for its size
+        assert ("required" in why) == taken
