@@ -207,11 +207,11 @@ size_t flashbon_op_layer_norm_grad_workspace(int32_t M, int32_t D, int32_t rows_
  * exp(q k_j / sqrt(head_dim)), -infinity for such rows.
  * kv_index: device int32 [batch] or NULL (b; then n_kv = batch), kv_len: device int32 [n_kv] or NULL (tk); their values are
  * clamped into [0, n_kv) and [0, tk].  heads % kv_heads == 0; head_dim one of 8, 16, 32, 64, 128; 1 <= tq, tk <= 2^24;
- * batch heads, up to a multiple of 8, times ceil(tq / 64) < 2^24; n_kv kv_heads <= 65535.  Row i of batch row b is at q + b q_batch_stride + i
- * q_row_stride + h head_dim, keys, values and out as in flashbon_op_attention.  Every address, and every stride in bytes, is
- * a multiple of 16, strides lie in [0, 2^36), and out's keep its rows apart, batch rows behind each other or side by side: the
- * larger stride passes all that the smaller one reaches (FLASHBON_EINVAL).  out and lse must not
- * overlap the extent of an input or each other (FLASHBON_EINVAL).
+ * batch heads, up to a multiple of 8, times ceil(tq / 64) < 2^24; n_kv kv_heads <= 65535.  Row i of batch row b is at
+ * q + b q_batch_stride + i q_row_stride + h head_dim, keys, values and out as in flashbon_op_attention.  Every address, and
+ * every stride in bytes, is a multiple of 16 (lse, kv_index and kv_len of 4), strides lie in [0, 2^36), and out's keep its rows
+ * apart, batch rows behind each other or side by side: the larger stride passes all that the smaller one reaches
+ * (FLASHBON_EINVAL).  out and lse must not overlap the extent of an input or each other (FLASHBON_EINVAL).
  * Few queries (tq heads) to long states run over several ranges of keys at once where a workspace of
  * flashbon_op_cross_attention_workspace bytes is given; without one, or with a smaller one, in one range.  A candidate's
  * bits do not depend on the other candidates. */

@@ -387,8 +387,8 @@ flashbon_status flashbon_op_cross_attention(int32_t dtype, int32_t batch, int32_
   if (!q || !k || !v || !out) return fail(FLASHBON_EINVAL, "q, k, v and out are required");
   const int64_t wide = (int64_t)heads * head_dim, narrow = (int64_t)kv_heads * head_dim, es = dtype == FLASHBON_BF16 ? 2 : 4;
   if (!aligned({q, k, v, out}) || !aligned({q_batch_stride, q_row_stride, kv_batch_stride, kv_row_stride, out_batch_stride, out_row_stride}, es) ||
-      (uintptr_t)lse % 4)
-    return fail(FLASHBON_EINVAL, "addresses and strides must be multiples of 16 bytes, strides in [0, 2^36)");
+      ((uintptr_t)lse | (uintptr_t)kv_index | (uintptr_t)kv_len) % 4)
+    return fail(FLASHBON_EINVAL, "addresses and strides must be multiples of 16 bytes (lse, kv_index and kv_len of 4), strides in [0, 2^36)");
   if (!apart(batch, out_batch_stride, tq, out_row_stride, wide)) return fail(FLASHBON_EINVAL, "out's strides must keep its rows apart");
   const size_t kv = extent(n_kv, kv_batch_stride, tk, kv_row_stride, narrow, es);
   CrossArgs a{};
@@ -433,9 +433,9 @@ flashbon_status flashbon_op_cross_attention_grad(int32_t dtype, int32_t batch, i
   if ((dk == nullptr) != (dv == nullptr)) return fail(FLASHBON_EINVAL, "dk and dv go together");
   if (!dq && !dk) return fail(FLASHBON_EINVAL, "dq, or dk and dv, are required");
   const int64_t wide = (int64_t)heads * head_dim, narrow = (int64_t)kv_heads * head_dim, es = dtype == FLASHBON_BF16 ? 2 : 4;
-  if (!aligned({q, k, v, out, dout, dq, dk, dv, workspace}) || (uintptr_t)lse % 4 ||
+  if (!aligned({q, k, v, out, dout, dq, dk, dv, workspace}) || ((uintptr_t)lse | (uintptr_t)kv_index | (uintptr_t)kv_len) % 4 ||
       !aligned({q_batch_stride, q_row_stride, kv_batch_stride, kv_row_stride, out_batch_stride, out_row_stride}, es))
-    return fail(FLASHBON_EINVAL, "addresses and strides must be multiples of 16 bytes, strides in [0, 2^36)");
+    return fail(FLASHBON_EINVAL, "addresses and strides must be multiples of 16 bytes (lse, kv_index and kv_len of 4), strides in [0, 2^36)");
   if ((dq && !apart(batch, q_batch_stride, tq, q_row_stride, wide)) || (dk && !apart(n_kv, kv_batch_stride, tk, kv_row_stride, narrow)))
     return fail(FLASHBON_EINVAL, "the strides of q, k and v must keep the rows of their gradients apart");
   const size_t need = flashbon_op_cross_attention_grad_workspace(dtype, batch, heads, kv_heads, head_dim, tq, tk, n_kv);

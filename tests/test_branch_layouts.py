@@ -62,3 +62,12 @@ def test_most_queries(batch, heads, tq, taken):
         status, why = call(name, base, **sizes, out=None)
         assert status == (fb.EINVAL if taken else fb.ESHAPE), (name, why)       # refused for the missing out, or for its size
         assert ("required" in why) == taken
+
+
+@pytest.mark.parametrize("table", ["kv_index", "kv_len", "lse"])
+def test_tables_off_four_bytes(table):
+    """Where the address is right, refused for the output or the workspace that the call lacks."""
+    status, why = call("cross_attention", CROSS, **{table: CROSS[table] + 2, "out": CROSS["q"]})
+    assert status == fb.EINVAL and "multiples" in why, why
+    status, why = call("cross_attention_grad", CROSS_GRAD, **{table: CROSS_GRAD[table] + 2, "workspace": None})
+    assert status == fb.EINVAL and "multiples" in why, why
