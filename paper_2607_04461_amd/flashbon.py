@@ -759,8 +759,9 @@ def flashbon_op_layer_norm(dtype, M, D, eps, x, out, *, weight=None, bias=None, 
 
 def flashbon_op_layer_norm_grad_workspace(M, D, rows_per_group=None) -> int:
     """Bytes of the workspace flashbon_op_layer_norm_grad needs."""
-    _int32(M, D)
-    return int(load().flashbon_op_layer_norm_grad_workspace(M, D, max(int(M), 1) if rows_per_group is None else rows_per_group))
+    per = max(int(M), 1) if rows_per_group is None else rows_per_group
+    _int32(M, D, per)
+    return int(load().flashbon_op_layer_norm_grad_workspace(M, D, per))
 
 
 def validate_layer_norm_grad(dtype, M, D, x, mean, rstd, dy, dx=None, weight=None, rows_per_group=1, residual=None,

@@ -71,3 +71,10 @@ def test_tables_off_four_bytes(table):
     assert status == fb.EINVAL and "multiples" in why, why
     status, why = call("cross_attention_grad", CROSS_GRAD, **{table: CROSS_GRAD[table] + 2, "workspace": None})
     assert status == fb.EINVAL and "multiples" in why, why
+
+
+def test_workspace_of_sizes_past_32_bits():
+    """The binding's function refuses what the call's arguments would wrap, as the call does."""
+    with pytest.raises(ValueError):
+        fb.flashbon_op_layer_norm_grad_workspace(4096, 64, (1 << 32) + 4096)
+    assert fb.flashbon_op_layer_norm_grad_workspace(4096, 64, 4096) > 0
