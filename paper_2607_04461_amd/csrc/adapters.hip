@@ -293,9 +293,10 @@ __device__ __forceinline__ void up_columns(const UpArgs &a, const Tile &t, const
   }
 }
 
-// Two waves a SIMD, but where that spills (919 rows, 1536 to 8960, rank 128, bf16 with an fp32 result: the call 48 us, for 44).
+// Two waves a SIMD (919 rows, 1536 to 8960, rank 128, bf16 with an fp32 result: the call 38 us, without asking 41), but for 32
+// rows of 128 ranks, which would spill (24960 rows, 1536 to 1536, fp32: 452 us for 432).
 template <typename T, typename O, int MT, int RK, bool GATHER>
-__global__ __launch_bounds__(256, MT * RK < 8 || (PARTS<T, O>) == 3 ? 2 : 1) void k_up(UpArgs a) {
+__global__ __launch_bounds__(256, MT * RK < 8 ? 2 : 1) void k_up(UpArgs a) {
   extern __shared__ __attribute__((aligned(16))) float s_part[];
   const int lane = threadIdx.x & 63, li = lane & 15, g = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Tile t = tile_of<16 * MT, GATHER>(blockIdx.x / a.parts, a.M, a.per, a.index, a.count);      // a row's workgroups follow each other
@@ -679,13 +680,12 @@ template <typename T, typename O>
 hipError_t launch_up(const UpArgs &a, hipStream_t s) {
   if (gathers(a.M, a.per, a.count))
     return a.rank <= 32 ? up_tile<T, O, 1, 1, true>(a, s) : a.rank <= 64 ? up_tile<T, O, 1, 2, true>(a, s) : up_tile<T, O, 1, 4, true>(a, s);
-  if (a.rank <= 32) {
-    const int mt = tile_rows(a.M, a.per, 4);
-    return mt == 4 ? up_tile<T, O, 4, 1>(a, s) : mt == 2 ? up_tile<T, O, 2, 1>(a, s) : up_tile<T, O, 1, 1>(a, s);
-  }
-  const int mt = tile_rows(a.M, a.per, 2);
-  if (a.rank <= 64) return mt == 2 ? up_tile<T, O, 2, 2>(a, s) : up_tile<T, O, 1, 2>(a, s);
-  return mt == 2 ? up_tile<T, O, 2, 4>(a, s) : up_tile<T, O, 1, 4>(a, s);
+  // As many rows as 256 tiles come here in fp32 of rank above 64 alone (launch_both), fewer have tiles of 16.
+  if (a.rank <= 32) return up_tile<T, O, 1, 1>(a, s);
+  if (a.rank <= 64) return up_tile<T, O, 1, 2>(a, s);
+  if constexpr (sizeof(T) == 4)
+    if (tile_rows(a.M, a.per, 2) == 2) return up_tile<T, O, 2, 4>(a, s);
+  return up_tile<T, O, 1, 4>(a, s);
 }
 
 template <typename T, typename O, int MT, int RT, bool GATHER = false>

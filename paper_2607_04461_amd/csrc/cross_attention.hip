@@ -1157,20 +1157,21 @@ template <typename T> int query_splits(const CrossArgs &a) {
 template <typename T, int DH, int NQ>
 hipError_t forward(CrossP p, void *workspace, size_t bytes, hipStream_t s) {
   p.nqb = (p.a.tq + 64 * NQ - 1) / (64 * NQ);
-  const int splits = key_splits<T>(p.a);
-  if (splits > 1 && workspace && bytes >= cross_attention_workspace(sizeof(T) == 2 ? ACT_BF16 : ACT_F32, p.a)) {
-    p.splits = splits;
-    p.part = (float *)workspace;
-    hipLaunchKernelGGL((k_cross<T, DH, NQ, true>), dim3(unit_grid(p), splits), dim3(256), (tile_bytes<T, DH>()), s, p);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int64_t rows = (int64_t)p.a.batch * p.a.heads * p.a.tq;
-    hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16)), dim3(256), 0, s, p);
-  } else if (NQ == 2 && attention_own_takes(p.a)) {
-    return launch_attention_own(p.a, s);
-  } else {
-    hipLaunchKernelGGL((k_cross<T, DH, NQ, false>), dim3(unit_grid(p)), dim3(256), (tile_bytes<T, DH>()), s, p);
+  if constexpr (NQ == 1) {        // 32 queries a wave are more than key_splits cuts
+    const int splits = key_splits<T>(p.a);
+    if (splits > 1 && workspace && bytes >= cross_attention_workspace(sizeof(T) == 2 ? ACT_BF16 : ACT_F32, p.a)) {
+      p.splits = splits;
+      p.part = (float *)workspace;
+      hipLaunchKernelGGL((k_cross<T, DH, NQ, true>), dim3(unit_grid(p), splits), dim3(256), (tile_bytes<T, DH>()), s, p);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      const int64_t rows = (int64_t)p.a.batch * p.a.heads * p.a.tq;
+      hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16)), dim3(256), 0, s, p);
+      return hipGetLastError();
+    }
   }
+  if (NQ == 2 && attention_own_takes(p.a)) return launch_attention_own(p.a, s);
+  hipLaunchKernelGGL((k_cross<T, DH, NQ, false>), dim3(unit_grid(p)), dim3(256), (tile_bytes<T, DH>()), s, p);
   return hipGetLastError();
 }
 
