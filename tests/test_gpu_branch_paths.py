@@ -37,6 +37,34 @@ def test_long_prompts_grad(dtype, shape):
     base.test_cross_attention_grad(dtype, shape)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", [(9, 2046, 4), (6, 4094, 6), (7, 5117, 2)], ids=str)
+def test_layer_norm_rows_in_single_elements(dtype, shape):
+    """Odd rows of every number of pieces a lane."""
+    base.test_layer_norm(dtype, *shape)
+    base.test_layer_norm_grad(dtype, *shape)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_keys_farther_apart_than_tiles_take(dh):
+    """Key rows past 2^23 elements apart, whose offsets within a tile pass 31 bits."""
+    heads, tq, tk, n, far = 2, 100, 67, 66, (1 << 23) + 8
+    q, kv, _, _ = base.cross_inputs("bf16", 1, heads, heads, dh, tq, tk, 1, [n], 72)
+    wide_ = heads * dh
+    flat = torch.zeros((tk - 1) * far + 2 * wide_, dtype=torch.bfloat16, device="cuda")
+    flat.as_strided((tk, 2 * wide_), (far, 1)).copy_(kv.reshape(tk, -1))
+    out, lse = torch.empty(tq, wide_, dtype=torch.bfloat16, device="cuda"), torch.empty(1, heads, tq, device="cuda")
+    fb.flashbon_op_cross_attention(fb.BF16, 1, heads, heads, dh, tq, tk, q.cuda(), 0, wide_, flat, flat[wide_:], 0, far, None, 1,
+                                   torch.tensor([n], dtype=torch.int32, device="cuda"), out, 0, wide_, lse=lse)
+    k, v = (base.clean(kv, [n])[:, :, i] for i in (0, 1))
+    want, wl = branch.cross_attention(wide(q), wide(k), wide(v), [0], [n])
+    rel = base.p_error(q, k, [0], wl)
+    near(lse, wl, rel + 8 * E * np.abs(wl), "lse")
+    mass, _ = branch.cross_attention(wide(q), wide(k), np.abs(wide(v)), [0], [n])
+    u = U[torch.bfloat16]
+    near(out.reshape(q.shape), want, u * np.abs(want) + (u + 2 * rel.transpose(0, 2, 1)[..., None] + (n + 8) * E) * (1 + 2 * u) * mass, "out")
+
+
 def grad_bounds(q, k, v, out, lse, dout, n, u):
     """How far dq, dk and dv of one candidate may be off before they are rounded, as in test_cross_attention_grad."""
     _, tq, heads, dh = q.shape
@@ -116,6 +144,15 @@ def test_weight_gradients_alone_of_many_rows(dtype, rank):
     """Without dx the first product runs by itself, on up to 64 rows a tile."""
     base.test_adapters_grad(dtype, "store", (16500, 40, 24, rank, 2, 4130))
     base.test_adapters_grad(dtype, "store", (16384, 24, 72, rank, 1, 16384))
+
+
+@pytest.mark.parametrize("dtype,epi", FORMS)
+@pytest.mark.parametrize("shape", [(8300, 72, 40, 16, 2, 4150), (8300, 40, 72, 32, 2, 4150), (4400, 72, 40, 32, 2, 2200),
+                                   (4400, 40, 72, 64, 2, 2200), (4400, 72, 40, 128, 2, 2200), (130, 2056, 264, 32, 2, 65)], ids=str)
+def test_adapters_by_rows_of_a_tile(dtype, epi, shape):
+    """32 rows a tile, 16, and so few that both products run by themselves."""
+    base.test_adapters(dtype, epi, shape)
+    base.test_adapters_grad(dtype, epi, shape)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
