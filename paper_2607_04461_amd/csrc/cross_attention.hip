@@ -117,6 +117,12 @@ __device__ __forceinline__ bool unit_of(const CrossP &p, int id, int &b, int &h,
   return true;
 }
 
+// a b, rounded: never one operation with the sum it goes into
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
 template <typename T> constexpr int TILE = sizeof(T) == 2 ? 64 : 32;    // rows of a tile in LDS
 
 // Two waves a SIMD are asked for in all three kernels, which also keeps their accumulators out of the accumulation registers:
@@ -147,10 +153,11 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
     row_frags<T, DH>(qf[n], (const T *)a.q + b * a.q_bs + (int64_t)min(i, a.tq - 1) * a.q_rs + h * a.head_dim, a.head_dim, i < a.tq);
   }
   f32x4 o[NQ][ND];
-  float top[NQ], sum[NQ];
+  float top[NQ], off[NQ], sum[NQ];        // the running maximum, what exponents are taken less (base 2), and the sum
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     top[n] = -INFINITY;
+    off[n] = -3.4028235e38f;
     sum[n] = 0.f;
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -198,9 +205,11 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) m = fmaxf(m, s[n][j][e]);
       m = across(m, true);
-      const float off = m == -INFINITY ? 0.f : m * p.qscale;     // a row of -inf only: all of it 0
-      const float shrink = __builtin_amdgcn_exp2f(fmaf(top[n], p.qscale, -off));
+      // as the exponents have it, rounding and all: a maximum that stays leaves the sums as they are
+      const float next = m == -INFINITY ? off[n] : rounded_product(m, p.qscale);     // a row of -inf only: all of it 0
+      const float shrink = __builtin_amdgcn_exp2f(off[n] - next);
       top[n] = m;
+      off[n] = next;
       sum[n] *= shrink;
 #pragma unroll
       for (int d = 0; d < ND; ++d)
@@ -210,7 +219,7 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
       for (int j = 0; j < NS; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s[n][j][e] = __builtin_amdgcn_exp2f(fmaf(s[n][j][e], p.qscale, -off));
+          s[n][j][e] = __builtin_amdgcn_exp2f(fmaf(s[n][j][e], p.qscale, -off[n]));
           sum[n] += s[n][j][e];
         }
     }
@@ -246,7 +255,7 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
       for (int d = 0; d < ND; ++d)
         if (16 * d + 4 * g < a.head_dim) *reinterpret_cast<f32x4 *>(dst + 16 * d + 4 * g) = o[n][d];
       if (g == 0) {
-        dst[a.head_dim] = top[n] * p.qscale;
+        dst[a.head_dim] = off[n];
         dst[a.head_dim + 1] = l;
       }
     } else {
@@ -263,7 +272,7 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
                                                        (bf16)(o[n][d][2] * inv), (bf16)(o[n][d][3] * inv)};
       }
       if (a.lse && g == 0)
-        a.lse[((int64_t)b * a.heads + h) * a.tq + i] = l == 0.f ? -INFINITY : (top[n] * p.qscale + log2f(l)) * LN2;
+        a.lse[((int64_t)b * a.heads + h) * a.tq + i] = l == 0.f ? -INFINITY : (off[n] + log2f(l)) * LN2;
     }
   }
 }

@@ -169,6 +169,35 @@ def test_cross_attention_grad_of_keys_that_count_for_nothing(dtype, shape):
             assert np.linalg.norm(wide(got) - want) <= (2 * U[ACT[dtype]] + 1000 * E) * np.linalg.norm(want)
 
 
+# ------------------------------------------------------------------------------- sums over many tiles, large scores
+def equal_keys(dtype, dh, tq, tk, score, seed):
+    """Queries of ones and keys whose scores (before the scale) are all `score`, exactly; values of order one."""
+    q = torch.zeros(1, tq, 2, dh, dtype=ACT[dtype])
+    q[..., 0] = 1.0
+    kv = torch.zeros(1, tk, 2, 1, dh, dtype=ACT[dtype])
+    kv[:, :, 0, :, 0] = score
+    kv[:, :, 1] = normal(gen(seed), 1, tk, 1, dh, dtype=ACT[dtype])
+    return q, kv
+
+
+PATHS = [(16, 70, 4096), (64, 100, 4096), (128, 70, 4096), (128, 100, 300), (128, 2, 4096), (32, 3, 8000)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dh,tq,tk", PATHS)
+@pytest.mark.parametrize("workspace", [False, True])
+def test_cross_attention_weighs_all_tiles_alike(dtype, dh, tq, tk, workspace):
+    """Values of 1 before the middle and of -1 behind it, under equal scores: their sums are whole multiples of one probability,
+    exact in fp32, and cancel."""
+    for score in (37.0, 117.0, 1000.0):
+        q, kv = equal_keys(dtype, dh, tq, tk, score, 73)
+        kv[:, :tk // 2, 1], kv[:, tk // 2:, 1] = 1.0, -1.0
+        got, lse = base.cross_call(dtype, q, kv, [0], [tk], workspace=workspace)
+        want = score / np.sqrt(dh) + np.log(tk)
+        near(lse, np.full(lse.shape, want), 8 * E * want, "lse")
+        assert float(got.abs().max()) <= 8 * E       # ranges of keys are joined with factors of one rounding each
+
+
 # ------------------------------------------------------------------------------------------------- other layouts
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("dh,tq,tk", [(16, 9, 7), (64, 70, 66), (128, 70, 66), (128, 3, 300)])
