@@ -203,8 +203,8 @@ size_t flashbon_op_layer_norm_grad_workspace(int32_t M, int32_t D, int32_t rows_
 /* Cross-attention to encoder states of their own lengths: as flashbon_op_attention, but the queries of batch row b see only
  * the first kv_len[c] of the tk key rows of c = kv_index[b], and query head h reads key head h / (heads / kv_heads).
  * Key rows at or past kv_len[c] are never read.  A prompt of length 0 gives rows of zeros, and so do scores that are all
- * -infinity; a key whose score is counts for nothing.  lse (device fp32 [batch][heads][tq], or NULL): log sum_j
- * exp(q k_j / sqrt(head_dim)), -infinity for such rows.
+ * -infinity; a key whose score is counts for nothing.  Scores of any finite size (fp32) are told apart.  lse (device fp32
+ * [batch][heads][tq], or NULL): log sum_j exp(q k_j / sqrt(head_dim)), -infinity for rows of zeros.
  * kv_index: device int32 [batch] or NULL (b; then n_kv = batch), kv_len: device int32 [n_kv] or NULL (tk); their values are
  * clamped into [0, n_kv) and [0, tk].  heads % kv_heads == 0; head_dim one of 8, 16, 32, 64, 128; 1 <= tq, tk <= 2^24;
  * batch heads, up to a multiple of 8, times ceil(tq / 64) < 2^24; n_kv kv_heads <= 65535.  Row i of batch row b is at
@@ -225,7 +225,8 @@ flashbon_status flashbon_op_cross_attention(int32_t dtype, int32_t batch, int32_
 size_t flashbon_op_cross_attention_workspace(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim,
                                              int32_t tq, int32_t tk);
 
-/* Gradient of flashbon_op_cross_attention from dout (act, out's strides), with out and lse as the forward call left them:
+/* Gradient of flashbon_op_cross_attention from dout (act, out's strides), with out and lse as the forward call left them
+ * (P then is off by |lse| 2^-24 of itself):
  *   P = exp(S - lse), S = q k^T / sqrt(head_dim);   dS = P (dout v^T - sum_d dout out) / sqrt(head_dim);
  *   dq = dS k;   dk = dS^T q, dv = P^T dout, summed over the batch rows and the query heads that read the key head.
  * dq (act) has q's strides, dk and dv those of k and v; q's and k's strides must keep their rows apart.  Every row of dk and

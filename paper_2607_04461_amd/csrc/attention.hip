@@ -241,15 +241,19 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[dt][j] = 0.f;
-  // OWN: from the least finite score on, so that a row or a tile whose scores are all -infinity has probabilities 0, not NaN
-  float mrun = OWN ? -3.4028235e38f : -INFINITY, lsum = 0.f, mb = 0.f;
+  // OWN: from the least finite score on, so that a row or a tile whose scores are all -infinity has probabilities 0, not NaN.
+  // Exponents (base 2) past 2^30: scores differ by 2^8 or not at all, and the rounding of their product with the scale would pass
+  // any power's range, so their differences are taken as they are (scale 1).
+  float mrun = OWN ? -3.4028235e38f : -INFINITY, lsum = 0.f, mb = OWN ? mrun : 0.f;
+  [[maybe_unused]] float own_scale = 1.f;
   bf16x8 pp[4];   // probabilities of the current tile, 16 keys per chunk
 
   // one pair of exponentials: keys 8 (c & 1) + i, + 1 of chunk c of the scores sc into pp[c]; the row
   // sum takes the pairs chunk by chunk
   auto epair = [&](const f32x16 (&sc)[2], int c, int i) __attribute__((always_inline)) {
-    const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[c >> 1][8 * (c & 1) + i], p.qscale, -mb));
-    const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[c >> 1][8 * (c & 1) + i + 1], p.qscale, -mb));
+    const float scale = OWN ? own_scale : p.qscale;
+    const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[c >> 1][8 * (c & 1) + i], scale, -mb));
+    const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[c >> 1][8 * (c & 1) + i + 1], scale, -mb));
     lsum += e0 + e1;
     const bf16x2 pr = __builtin_convertvector((float __attribute__((ext_vector_type(2)))){e0, e1}, bf16x2);
     pp[c][i] = pr[0];
@@ -281,7 +285,19 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
     }
     if (__any(tmax > mrun + p.lazy_thr)) {
       const float mnew = fmaxf(mrun, tmax);
-      const float corr = __builtin_amdgcn_exp2f((mrun - mnew) * p.qscale);
+      float corr;
+      if constexpr (OWN) {
+        float next = rounded_product(mnew, p.qscale);
+        own_scale = p.qscale;
+        if (fabsf(next) > 0x1p30f) {
+          next = mnew;
+          own_scale = 1.f;
+        }
+        corr = __builtin_amdgcn_exp2f(mb - next);
+        mb = next;
+      } else {
+        corr = __builtin_amdgcn_exp2f((mrun - mnew) * p.qscale);
+      }
       lsum *= corr;
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt)
@@ -289,7 +305,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
         for (int q = 0; q < 16; ++q) o[dt][q] *= corr;
       mrun = mnew;
     }
-    mb = mrun * p.qscale;
+    if constexpr (!OWN) mb = mrun * p.qscale;
   };
 
   using S0 = std::integral_constant<int, 0>;
@@ -422,7 +438,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fa(AttnP p) {
   const float inv = OWN && ltot == 0.f ? 0.f : 1.0f / ltot;
   if constexpr (OWN)
     if (p.lse && g == 0 && q0 + li < p.tq)
-      p.lse[((int64_t)b * p.heads + h) * p.tq + q0 + li] = (mrun * p.qscale + log2f(ltot)) * 0.6931471805599453f;
+      p.lse[((int64_t)b * p.heads + h) * p.tq + q0 + li] = ((own_scale == 1.f ? mrun * p.qscale : mb) + log2f(ltot)) * 0.6931471805599453f;
   __syncthreads();   // every wave has read its last K and V fragments: the rings are free
   // the wave's 32 x 128 output block goes through LDS (16-byte chunk c of row r at c ^ (r & 15)), so that
   // each global store writes 4 whole rows

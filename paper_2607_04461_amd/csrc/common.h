@@ -41,6 +41,12 @@ __device__ __forceinline__ float silu(float x) { return x / (1.0f + __expf(-x));
 __device__ __forceinline__ float dot4(float4 a, float4 b) { return fmaf(a.y, b.y, a.x * b.x) + fmaf(a.z, b.z, a.w * b.w); }
 __device__ __forceinline__ float sum_sq4(float a, float b, float c, float d) { return fmaf(a, a, b * b) + fmaf(c, c, d * d); }
 
+// a b, rounded: never one operation with the sum it goes into
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
 // wave64 reductions
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll

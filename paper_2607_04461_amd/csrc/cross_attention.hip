@@ -117,11 +117,9 @@ __device__ __forceinline__ bool unit_of(const CrossP &p, int id, int &b, int &h,
   return true;
 }
 
-// a b, rounded: never one operation with the sum it goes into
-__device__ __forceinline__ float rounded_product(float a, float b) {
-#pragma clang fp contract(off)
-  return a * b;
-}
+// Scores whose exponents (base 2) pass 2^30 differ by 2^8 or not at all, and the rounding of a product with the scale would pass
+// any power's range: their differences are taken as they are.
+__device__ __forceinline__ bool far(float exponent) { return fabsf(exponent) > 0x1p30f; }
 
 template <typename T> constexpr int TILE = sizeof(T) == 2 ? 64 : 32;    // rows of a tile in LDS
 
@@ -206,7 +204,11 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
         for (int e = 0; e < 4; ++e) m = fmaxf(m, s[n][j][e]);
       m = across(m, true);
       // as the exponents have it, rounding and all: a maximum that stays leaves the sums as they are
-      const float next = m == -INFINITY ? off[n] : rounded_product(m, p.qscale);     // a row of -inf only: all of it 0
+      float next = m == -INFINITY ? off[n] : rounded_product(m, p.qscale), scale = p.qscale;     // a row of -inf only: all of it 0
+      if (far(next)) {
+        next = m == -INFINITY ? off[n] : m;
+        scale = 1.f;
+      }
       const float shrink = __builtin_amdgcn_exp2f(off[n] - next);
       top[n] = m;
       off[n] = next;
@@ -219,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
       for (int j = 0; j < NS; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s[n][j][e] = __builtin_amdgcn_exp2f(fmaf(s[n][j][e], p.qscale, -off[n]));
+          s[n][j][e] = __builtin_amdgcn_exp2f(fmaf(s[n][j][e], scale, -next));
           sum[n] += s[n][j][e];
         }
     }
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
     const float l = across(sum[n], false);
     if (i >= a.tq) continue;
     if constexpr (SPLIT) {
-      // [row][split][dh + 2]: the sums as they stand, the maximum (base 2) and the sum
+      // [row][split][dh + 4]: the sums as they stand, what their exponents were taken less, the sum and the maximum
       float *dst = p.part + ((((int64_t)b * a.heads + h) * a.tq + i) * p.splits + blockIdx.y) * (a.head_dim + 4);
 #pragma unroll
       for (int d = 0; d < ND; ++d)
@@ -257,6 +259,7 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
       if (g == 0) {
         dst[a.head_dim] = off[n];
         dst[a.head_dim + 1] = l;
+        dst[a.head_dim + 2] = top[n];
       }
     } else {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -272,7 +275,7 @@ __global__ __launch_bounds__(256, 2) void k_cross(CrossP p) {
                                                        (bf16)(o[n][d][2] * inv), (bf16)(o[n][d][3] * inv)};
       }
       if (a.lse && g == 0)
-        a.lse[((int64_t)b * a.heads + h) * a.tq + i] = l == 0.f ? -INFINITY : (off[n] + log2f(l)) * LN2;
+        a.lse[((int64_t)b * a.heads + h) * a.tq + i] = l == 0.f ? -INFINITY : ((far(off[n]) ? top[n] * p.qscale : off[n]) + log2f(l)) * LN2;
     }
   }
 }
@@ -289,7 +292,8 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossP p) {
     const float *src = p.part + r * p.splits * pitch;
     // lane s: the maximum and sum of range s (at most 64), then its factor and the row's sum
     const float ls = lane < p.splits ? src[lane * pitch + a.head_dim + 1] : 0.f;
-    const float ms = lane < p.splits ? src[lane * pitch + a.head_dim] : -INFINITY;
+    float ms = lane < p.splits ? src[lane * pitch + a.head_dim] : -INFINITY;
+    const float raw = lane < p.splits ? src[lane * pitch + a.head_dim + 2] : -INFINITY;
     float v[16][2];        // the first ranges' sums, on their way meanwhile
     auto load = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
@@ -298,6 +302,10 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossP p) {
         for (int e = 0; e < 2; ++e) v[s][e] = s0 + s < p.splits && lane + 64 * e < a.head_dim ? src[(s0 + s) * pitch + lane + 64 * e] : 0.f;
     };
     load(0);
+    // far scores' ranges are told apart by their maxima themselves
+    const float most = wave_max(ls != 0.f ? raw : -INFINITY);
+    const bool apart = far(most * p.qscale);
+    if (apart) ms = raw;
     const float top = wave_max(ls != 0.f ? ms : -INFINITY);
     const float mine = ls != 0.f ? __builtin_amdgcn_exp2f(ms - (top == -INFINITY ? 0.f : top)) : 0.f;
     const float l = wave_sum(mine * ls);
@@ -316,7 +324,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossP p) {
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       if (lane + 64 * e < a.head_dim) O[lane + 64 * e] = from_f32<T>(o[e] * inv);
-    if (a.lse && lane == 0) a.lse[r] = l == 0.f ? -INFINITY : (top + log2f(l)) * LN2;
+    if (a.lse && lane == 0) a.lse[r] = l == 0.f ? -INFINITY : ((apart ? top * p.qscale : top) + log2f(l)) * LN2;
   }
 }
 

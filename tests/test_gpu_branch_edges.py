@@ -198,6 +198,37 @@ def test_cross_attention_weighs_all_tiles_alike(dtype, dh, tq, tk, workspace):
         assert float(got.abs().max()) <= 8 * E       # ranges of keys are joined with factors of one rounding each
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dh,tq,tk", PATHS)
+@pytest.mark.parametrize("score", [-1e37, -1e12, 1e10, 1e37, 2.0 ** 31, -2.0 ** 30, 2.0 ** 24, 3e9, -1.1e9, 1.7e7, -3e6])
+def test_cross_attention_of_large_scores(dtype, dh, tq, tk, score):
+    """Scores of any finite size: equal ones have equal probabilities, lower ones none."""
+    u = U[ACT[dtype]]
+    q, kv = equal_keys(dtype, dh, tq, tk, score, 74)
+    score = float(kv[0, 0, 0, 0, 0])
+    got, lse = base.cross_call(dtype, q, kv, [0], [tk])
+    v = wide(kv[0, :, 1, 0])
+    want = score / np.sqrt(dh) + np.log(tk)
+    near(lse, np.full(lse.shape, want), 8 * E * abs(want), "lse")
+    tol = u * np.abs(v.mean(0)) + (2 * u + (tk + 8) * E) * np.abs(v).mean(0)
+    near(got, np.broadcast_to(v.mean(0), got.shape), tol, "out")
+    # most keys far below, in whole tiles and between the others
+    low = score * 1.5 if score < 0 else score * 0.5
+    kv[0, :tk // 2, 0, 0, 0] = low
+    kv[0, tk // 2::3, 0, 0, 0] = low
+    got, lse = base.cross_call(dtype, q, kv, [0], [tk])
+    on = wide(kv[0, :, 0, 0, 0]) == score
+    want, v = score / np.sqrt(dh) + np.log(on.sum()), v[on]
+    near(lse, np.full(lse.shape, want), 8 * E * abs(want), "lse")
+    near(got, np.broadcast_to(v.mean(0), got.shape), u * np.abs(v.mean(0)) + (2 * u + (tk + 8) * E) * np.abs(v).mean(0), "out")
+    # and one ordinary key above them all where they are negative
+    if score < 0:
+        kv[0, tk - 1, 0, 0, 0] = 1.0
+        got, lse = base.cross_call(dtype, q, kv, [0], [tk])
+        near(lse, np.full(lse.shape, 1 / np.sqrt(dh)), 8 * E, "lse")
+        near(got, np.broadcast_to(wide(kv[0, tk - 1, 1, 0]), got.shape), 4 * E, "out")
+
+
 # ------------------------------------------------------------------------------------------------- other layouts
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("dh,tq,tk", [(16, 9, 7), (64, 70, 66), (128, 70, 66), (128, 3, 300)])
