@@ -188,7 +188,7 @@ flashbon_status flashbon_op_layer_norm(int32_t dtype, int32_t M, int32_t D, floa
 /* Gradient of flashbon_op_layer_norm from dy, device act [M][D].  With xhat = (x - mean) rstd and g = dy f:
  *   dx[m][d] = residual[m][d] + rstd[m] (g - mean_d(g) - xhat mean_d(g xhat));   dweight[g][d] = sum_m dy xhat, dbias[g][d] =
  *   sum_m dy over the group's rows.
- * mean, rstd: device fp32 [M], as the forward call left them (the mean of a row of more than 256 deviations is formed anew,
+ * mean, rstd: device fp32 [M], as the forward call left them (the mean of a row of more than 4096 deviations is formed anew,
  * in more bits than the saved one has).  residual: device fp32 [M][D] (the gradient that reaches x
  * past the norm) or NULL (0).  dx: device fp32 [M][D], may be residual itself; dweight, dbias: device fp32, as weight; each
  * output may be NULL, one at least is given.  Outputs must not otherwise overlap an input or each other (FLASHBON_EINVAL).
