@@ -617,7 +617,7 @@ __global__ __launch_bounds__(256) void k_outer_sum(int count, int64_t down, int6
       for (int k = 0; k < 4; ++k) s_part[w - 1][lane][k] = s[k];
     __syncthreads();
     if (w == 0 && e < all) {
-      const double scale = e < down ? 1.0 : (double)(scales ? scales[a] : 1.f);
+      const double scale = e < down || !scales || n == 0 ? 1.0 : (double)scales[a];      // 0 without rows, whatever the scale
       f32x4 v;
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = (float)((((s[k] + s_part[0][lane][k]) + s_part[1][lane][k]) + s_part[2][lane][k]) * scale);

@@ -281,6 +281,33 @@ def test_cross_attention_of_rows_side_by_side(dtype, dh, tq, tk, order):
         assert torch.equal(a, b)
 
 
+# ------------------------------------------------------------------------------------------------------- adapters
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rank", [8, 128])
+@pytest.mark.parametrize("per,scale", [(1, float("inf")), (7, float("nan")), (40, -float("inf"))])
+def test_adapters_that_no_row_uses(dtype, rank, per, scale):
+    """Weights and a scale of anything: they reach no row, and their gradients are 0."""
+    m, n, k, count = 75, 72, 40, 4
+    x, down, up, s, _, g = base.adapter_inputs(dtype, m, n, k, rank, count, per, 75)
+    index = torch.tensor([2 if i % 3 else -1 if i % 2 else 0 for i in range(-(-m // per))], dtype=torch.int32)
+    b, dy, bx = (normal(g, m, w, dtype=ACT[dtype]).cuda() for w in (n, n, k))
+    sizes, results = (CODE[dtype], m, n, k, rank, count), []
+    for bad in (False, True):
+        if bad:
+            for a in (1, 3):
+                s[a], down[a], up[a] = scale, float("nan"), float("inf")
+        args = (x.cuda(), down.cuda(), up.cuda(), s.cuda(), index.cuda(), per)
+        out, u = torch.empty_like(b), torch.empty(m, rank, device="cuda")
+        fb.flashbon_op_adapters(*sizes, *args, fb.EPI_STORE, b, out, u)
+        dx, dd, du = torch.empty_like(bx), torch.empty(count, rank, k, device="cuda"), torch.empty(count, n, rank, device="cuda")
+        ws = torch.full((fb.flashbon_op_adapters_grad_workspace(*sizes, per),), 255, dtype=torch.uint8, device="cuda")
+        fb.flashbon_op_adapters_grad(*sizes, *args, u, dy, fb.EPI_STORE, bx, dx, dd, du, workspace=ws)
+        results.append((out, u, dx, dd, du))
+    for clean, got in zip(*results):
+        assert torch.equal(clean, got)
+    assert not results[1][3][1::2].any() and not results[1][4][1::2].any()
+
+
 # ------------------------------------------------------------------------------------------- two threads at once
 def together(works):
     """Runs each of the works on a thread and a stream of its own, twenty times."""
