@@ -165,8 +165,8 @@ flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, f
 
 /* ---- The cross-attention branch with a prompt and an adapter per candidate, and its gradients.  A pool may hold
  * candidates of several requests: prompts of different lengths, timesteps of their own, and fine-tuned low-rank adapters.
- * The same calls train such adapters on drafts (Sec. 5): the base weights stay frozen, and the gradient of a frozen linear
- * layer's input is flashbon_op_linear on its transposed weights.  A branch h + gate W_o attention(W_q LN(h)) runs as
+ * Their gradients are those of this one branch (Sec. 5 trains such adapters on drafts): the base weights stay frozen, and the
+ * gradient of a frozen linear layer's input is flashbon_op_linear on its transposed weights.  A branch h + gate W_o attention(W_q LN(h)) runs as
  *   flashbon_op_layer_norm -> flashbon_op_linear + flashbon_op_adapters -> flashbon_op_cross_attention ->
  *   flashbon_op_linear (FLASHBON_EPI_RESIDUAL) + flashbon_op_adapters,
  * and backwards through the _grad calls.  A workspace is the caller's (device, on 16 bytes); a _workspace function returns
@@ -192,8 +192,8 @@ flashbon_status flashbon_op_layer_norm(int32_t dtype, int32_t M, int32_t D, floa
  * in more bits than the saved one has).  residual: device fp32 [M][D] (the gradient that reaches x
  * past the norm) or NULL (0).  dx: device fp32 [M][D], may be residual itself; dweight, dbias: device fp32, as weight; each
  * output may be NULL, one at least is given.  Outputs must not otherwise overlap an input or each other (FLASHBON_EINVAL).
- * Sizes as above; a workspace of flashbon_op_layer_norm_grad_workspace bytes wherever dweight or dbias is given
- * (FLASHBON_ESHAPE if it is smaller). */
+ * Sizes as above, and fewer than 2^24 groups of rows; a workspace of flashbon_op_layer_norm_grad_workspace bytes wherever
+ * dweight or dbias is given (FLASHBON_ESHAPE if it is smaller). */
 flashbon_status flashbon_op_layer_norm_grad(int32_t dtype, int32_t M, int32_t D, const float *x, int32_t rows_per_group,
                                             const float *weight, int32_t modulated, const float *mean, const float *rstd,
                                             const void *dy, const float *residual, float *dx, float *dweight, float *dbias,
@@ -214,7 +214,8 @@ size_t flashbon_op_layer_norm_grad_workspace(int32_t M, int32_t D, int32_t rows_
  * (FLASHBON_EINVAL).  out and lse must not overlap the extent of an input or each other (FLASHBON_EINVAL).
  * Few queries (tq heads) to long states run over several ranges of keys at once where a workspace of
  * flashbon_op_cross_attention_workspace bytes is given; without one, or with a smaller one, in one range.  A candidate's
- * bits do not depend on the other candidates. */
+ * bits do not depend on the other candidates; they may on tk, past its prompt's end too, by which the ranges go.  bf16 P goes
+ * into the product in two parts for tq <= 64 and for head_dim <= 32, else in one of 8 bits. */
 flashbon_status flashbon_op_cross_attention(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim,
                                             int32_t tq, int32_t tk, const void *q, int64_t q_batch_stride,
                                             int64_t q_row_stride, const void *k, const void *v, int64_t kv_batch_stride,
@@ -234,7 +235,8 @@ size_t flashbon_op_cross_attention_workspace(int32_t dtype, int32_t batch, int32
  * has P = 1: dq and dk are 0 there.  dq may be NULL, and so may dk and dv together.  The outputs must not overlap the extent
  * of an input or each other, but dk and dv may lie in one buffer as fused keys and values do, their rows apart in the same
  * sense, with the way from dk to dv as a third stride (FLASHBON_EINVAL).  batch <= 4096; sizes and alignment otherwise as
- * above; a workspace of flashbon_op_cross_attention_grad_workspace bytes (FLASHBON_ESHAPE if it is smaller). */
+ * above; a workspace of flashbon_op_cross_attention_grad_workspace bytes (FLASHBON_ESHAPE if it is smaller).  bf16 P and dS go
+ * into the products in one part of 8 bits for head dims 64 and 128 with more than 64 queries and tk, else in two. */
 flashbon_status flashbon_op_cross_attention_grad(int32_t dtype, int32_t batch, int32_t heads, int32_t kv_heads,
                                                  int32_t head_dim, int32_t tq, int32_t tk, const void *q,
                                                  int64_t q_batch_stride, int64_t q_row_stride, const void *k, const void *v,

@@ -7,7 +7,8 @@
 // All kernels keep one side in registers and take the other in tiles through LDS, and form the scores so that a lane's
 // values belong to one row of the side it keeps: the products of two tiles then are the right operand of the next product as
 // they stand, with its k in an order that the left operand follows.  P and dS are rounded to the operands' type for that
-// product (bf16: 8 bits, as the values they meet; in two parts where that is free).
+// product (bf16: 8 bits, as the values they meet; in two parts where that is free: forward with 16 queries a wave or heads of
+// at most 32, in the gradient everywhere but in x32 with more than 64 keys and queries).
 //   * k_cross: a wave keeps 16 or 32 queries.  One pass over the keys with the running maximum and sum.
 //   * k_cross_dq: the same with dout, lse and delta, which it forms: two products give P and dP, the third dq.
 //   * k_cross_dkv: a wave keeps keys and values; the queries and dout of all candidates of the prompt pass by.
@@ -15,7 +16,7 @@
 // bf16 of head dim 128 with more than 64 queries runs forward on k_attn_fa (attention.hip).
 // Bound by the matrix cores for many queries, by the reading of k and v for few: then ranges of keys go to several
 // workgroups and k_cross_join joins them (one query of 40 heads to 4001 keys: 18 us and 4, 82 MB at 4.5 TB/s).  fp32, 4 x 12
-// heads of 1560 x 512, head dim 128: forward 189 us (104 TFLOP/s of 154), gradient 635.
+// heads of 1560 x 512, head dim 128: forward 193 us (102 TFLOP/s of 154), gradient 635.
 #include <algorithm>
 
 #include "fragments.h"

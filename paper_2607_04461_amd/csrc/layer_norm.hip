@@ -3,9 +3,9 @@
 //   g = dy f,   dx = residual + rstd (g - mean(g) - xhat mean(g xhat))
 //   dweight = sum_m dy xhat,   dbias = sum_m dy over the rows of a group (they share a weight and a bias)
 // Both are bound by HBM: every row is read once and held in registers between its reductions, by one wave up to
-// 2048 elements and by four beyond (16384 x 5120 to bf16 97 us, 5.2 TB/s; the gradient of 24960 x 1536 with the residual
-// stream's 113 us and 4 for the vectors' sums, 4.8 TB/s).  The mean is summed in 64 bits (a few per cent of the time a row's bytes take)
-// and taken off in two parts, so that rows far from zero keep their digits; the other sums are fp32.  Where the variance
+// 2048 elements and by four beyond (16384 x 5120 to bf16 98 us, 5.2 TB/s; the gradient of 24960 x 1536 with the residual
+// stream's 113 us and 5 for the vectors' sums, 4.7 TB/s).  The mean is summed in 64 bits (a few per cent of the time a
+// row's bytes take) and taken off in two parts, so that rows far from zero keep their digits; the other sums are fp32.  Where the variance
 // and eps leave fp32's normal numbers (a deviation past 2^64, or eps below 2^-126), the row is formed anew in 64 bits.
 // The gradient of the vectors is a sum over thousands of rows: a workgroup adds up a chunk of rows of one group in
 // registers, and a second launch adds the chunks' sums in order, in 64 bits.  No atomics: a call's bits are always
@@ -307,7 +307,11 @@ hipError_t launch_grad(const LayerNormGradArgs &a, int64_t blocks, bool vec, hip
   return hipGetLastError();
 }
 
-// pieces a lane of one or of four waves holds
+// Pieces a lane of one or of four waves holds, few enough to hold the row.  What the edges are worth, beside the next class (us,
+// bf16 unless fp32 is named): 24960 x 512 two pieces 16, its gradient 37, six 23 and 47; 24960 x 1536 six 42 and 121 (fp32 54 and
+// 137), eight 45 and 124 (52 and 141); 8192 x 2048 one wave 23 and 51, four 22 and 54; 16384 x 5120 five 98 and 265 (fp32 122 and
+// 287), six 102 and 250 (118 and 284).  Rows of 513 to 1024 would need a class of their own: 1037 x 701 takes 24 single loads a
+// lane where 11 hold the row.
 #define FB_BY_WIDTH(call)                          \
   do {                                             \
     if (D <= 512) { return call(1, 2); }           \
