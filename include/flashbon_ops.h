@@ -165,8 +165,9 @@ flashbon_status flashbon_op_norm_residual(int32_t dtype, int32_t M, int32_t D, f
 
 /* ---- The cross-attention branch with a prompt and an adapter per candidate, and its gradients.  A pool may hold
  * candidates of several requests: prompts of different lengths, timesteps of their own, and fine-tuned low-rank adapters.
- * Their gradients are those of this one branch (Sec. 5 trains such adapters on drafts): the base weights stay frozen, and the
- * gradient of a frozen linear layer's input is flashbon_op_linear on its transposed weights.  A branch h + gate W_o attention(W_q LN(h)) runs as
+ * The gradients are those of this one branch (Sec. 5 trains such adapters on drafts): the base weights stay frozen, and the
+ * gradient of a frozen linear layer's input is flashbon_op_linear on its transposed weights.  A branch
+ * h + gate W_o attention(W_q LN(h)) runs as
  *   flashbon_op_layer_norm -> flashbon_op_linear + flashbon_op_adapters -> flashbon_op_cross_attention ->
  *   flashbon_op_linear (FLASHBON_EPI_RESIDUAL) + flashbon_op_adapters,
  * and backwards through the _grad calls.  A workspace is the caller's (device, on 16 bytes); a _workspace function returns
